@@ -9,6 +9,7 @@
  *   pulsar_lse_merge       online-softmax merge alone      (Appendix H, Eq. 12-13)
  *   pulsar_causal_varlen_attn    causal attention over assembled inputs of any lengths (Alg. 1 l.8)
  *   pulsar_phase2_generate_step  one generation step: append KV(q), attend, merge (Alg. 1 l.11-16)
+ *   pulsar_pages_*, pulsar_tree_attn, pulsar_sparse_attn  a paged cache of continuations, drafted trees and page selection on it
  *
  * Conventions that hold for every call
  * ------------------------------------
@@ -61,6 +62,9 @@ typedef enum pulsar_status {
 #define PULSAR_DEV_TIMEOUT     0x4 /* an mbarrier wait exceeded its bound (results invalid)   */
 #define PULSAR_DEV_BAD_LENGTH  0x8 /* prefix_len[i] outside [0, prefix_total] (clamped)       */
 #define PULSAR_DEV_BAD_POSITION 0x10 /* negative position id (0 used)                          */
+#define PULSAR_DEV_BAD_PAGE    0x20 /* page id outside [0, n_pages) where a row lies (the row counts as absent) */
+#define PULSAR_DEV_BAD_TREE    0x40 /* parent not before its node (taken as -1), accepted nodes not ascending (the rest ignored) */
+#define PULSAR_DEV_NO_PAGES    0x80 /* no free page, or no room in the page table (the entry is -1)   */
 
 /* Static, human-readable name of a status code (host pointer, never NULL). */
 const char *pulsar_status_string(int32_t status);
@@ -535,6 +539,135 @@ int32_t pulsar_rope_apply_qk(const uint16_t *Q, uint16_t *Q_out, int32_t Hq,
                              const uint16_t *K, uint16_t *K_out, int32_t Hkv,
                              int64_t rows, int32_t d, const int32_t *positions, double theta,
                              int32_t *device_status, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A paged key/value cache for the continuations of an encoded context (what a serving loop keeps beside the generation shard
+ * of Algorithm 1 l.15; the paper has no counterpart).
+ *
+ *   K_pages, V_pages  [n_layers, n_pages, page_size, Hkv, d] bf16: the pool, page p of every layer belongs together
+ *   page_table        [n_slots, max_pages] int32 device: row r of slot s lies in page page_table[s, r / page_size], at row
+ *                     r % page_size of it.  Retained context KV [L, Hkv, d] is a run of L / page_size pages as it stands.
+ *   cache_len         [n_slots] int32 device: rows that slot s holds.  Values outside [0, max_pages*page_size] set
+ *                     PULSAR_DEV_BAD_LENGTH and are clamped.
+ * Rows from cache_len on are never read (they may hold anything, NaN included).  A page id outside [0, n_pages) where a row lies
+ * sets PULSAR_DEV_BAD_PAGE: the row counts as absent, and what would be written there is dropped.  Several slots may hold the
+ * same page; then they agree on its rows, and a page that is still written to is held by one slot.
+ *
+ * Requirements of all the calls (else PULSAR_ERR_SHAPE): page_size in {16, 32, 64, 128}; d in {64, 128}; 1 <= n_slots <= 1024;
+ * max_pages * page_size <= 2^30; n_slots * max_pages < 2^31; 1 <= n_pages < 2^24; n_layers >= 1; Hkv <= 1024.
+ *
+ * pulsar_pages_fork    copy, fork, reorder and free continuations, and reserve pages: a pure function of table and lengths
+ *   parent      in  [n_new] int32 device: slot i of the result continues slot parent[i] of page_table; -1 = an empty slot.  NULL =
+ *               identity (n_new = n_slots).  Other values set PULSAR_DEV_BAD_TREE and count as -1.
+ *   new_table   out [n_new, max_pages], new_len out [n_new]: the parent's length, and its first ceil(len / page_size) pages,
+ *               shared.  Where len % page_size != 0 the last of them is still written to: the first child (lowest i) keeps it, every
+ *               other child gets a page of its own, into which the len % page_size rows of every layer of K_pages and V_pages are
+ *               copied.  Then as many pages as reserve_rows more rows need.  Entries past those are -1.  An empty slot has no pages.
+ *   n_free      out [1] int32 device: pages that no slot of the result holds
+ * A page is free if and only if no slot of the result holds it from its parent: pages of slots that nobody continues are free
+ * within the same call.  Free pages are handed out in ascending order to the slots in ascending order.  Where none is left, or
+ * max_pages is too small, PULSAR_DEV_NO_PAGES is set and the entry is -1 (or missing).
+ *   page_table, cache_len and parent must not overlap the outputs (else PULSAR_ERR_INVALID_ARG).  1 <= n_new <= 1024,
+ *   reserve_rows >= 0.
+ *
+ * pulsar_pages_compact  after a drafted tree was verified: the accepted nodes move up behind the sequence, in every layer
+ *   accept      in  [n_slots, T] int32 device, 1 <= T <= 64: the accepted nodes of the slot's tree in ascending order, then -1.  Row
+ *               cache_len + accept[j] moves to row cache_len + j.
+ *   new_len     out [n_slots]: cache_len + accepted nodes (may not overlap cache_len)
+ *
+ * pulsar_pages_append   rows from packed tensors into one layer's pages: row u of slot s goes to row cache_len + u
+ *   Knew, Vnew  in  [n_slots, T, Hkv, d] bf16, K_pages, V_pages [n_pages, page_size, Hkv, d] (one layer)
+ *   n_new       in  [n_slots] int32 device: rows of the slot that exist (clamped to [0, T]); NULL = T
+ *   Rows past the last page of the table set PULSAR_DEV_BAD_LENGTH and are dropped.  cache_len is the caller's to advance.
+ *
+ * pulsar_pages_summarize  key bounds of full pages, for pulsar_sparse_attn
+ *   row_begin, row_end  in [n_slots] int32 device, row_begin may be NULL (0): the pages of the slot that are full at row_end and have
+ *               a row from row_begin on are summarised
+ *   summary     out [n_layers, n_pages, Hkv, 2, d] bf16: smallest and largest key component over the page's rows (a NaN
+ *               among them makes both NaN); other pages' entries are left as they were
+ * ------------------------------------------------------------------------------------------ */
+size_t pulsar_pages_fork_workspace_bytes(int32_t n_new, int32_t n_pages);
+
+int32_t pulsar_pages_fork(const int32_t *page_table, const int32_t *cache_len, int32_t n_slots, int32_t max_pages,
+                          const int32_t *parent, int32_t n_new, uint16_t *K_pages, uint16_t *V_pages,
+                          int32_t n_layers, int32_t n_pages, int32_t page_size, int32_t Hkv, int32_t d, int32_t reserve_rows,
+                          int32_t *new_table, int32_t *new_len, int32_t *n_free,
+                          void *workspace, size_t workspace_bytes, int32_t *device_status, void *stream);
+
+int32_t pulsar_pages_compact(uint16_t *K_pages, uint16_t *V_pages, int32_t n_layers, int32_t n_pages, int32_t page_size,
+                             int32_t Hkv, int32_t d, const int32_t *page_table, const int32_t *cache_len, int32_t n_slots,
+                             int32_t max_pages, const int32_t *accept, int32_t T, int32_t *new_len,
+                             int32_t *device_status, void *stream);
+
+int32_t pulsar_pages_append(const uint16_t *Knew, const uint16_t *Vnew, int32_t T, const int32_t *n_new,
+                            uint16_t *K_pages, uint16_t *V_pages, int32_t n_pages, int32_t page_size, int32_t Hkv, int32_t d,
+                            const int32_t *page_table, const int32_t *cache_len, int32_t n_slots, int32_t max_pages,
+                            int32_t *device_status, void *stream);
+
+int32_t pulsar_pages_summarize(const uint16_t *K_pages, int32_t n_layers, int32_t n_pages, int32_t page_size, int32_t Hkv,
+                               int32_t d, const int32_t *page_table, const int32_t *row_begin, const int32_t *row_end,
+                               int32_t n_slots, int32_t max_pages, uint16_t *summary, int32_t *device_status, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Attention of drafted trees over a paged cache: pulsar_phase2_generate_step for many sequences at once, whose new tokens are the
+ * nodes of a tree each (a chain is the causal case, T = 1 a decoding step).
+ *
+ * Node t of slot s has row cache_len[s] + t and sees rows [0, cache_len[s]), its ancestors and itself:
+ *   visible(t) = [0, cache_len) + {cache_len + a : a = t, parent(t), parent(parent(t)), ...}
+ *   O[s,t] = softmax over visible(t) of q.k * scale, times V;  LSE[s,t] = ln sum exp(q.k * scale).
+ * The nodes' keys and values are written to their rows of the pages by this call.
+ *
+ *   Q           in  [n_slots, T, Hq, d] bf16     Knew, Vnew  in [n_slots, T, Hkv, d] bf16
+ *   K_pages, V_pages in/out [n_pages, page_size, Hkv, d] bf16: one layer of the pool
+ *   parent      in  [n_slots, T] int32 device: -1 (a root: sees the cache and itself) or an earlier node; NULL = a chain
+ *               (parent of t is t - 1).  Other values set PULSAR_DEV_BAD_TREE and count as -1.
+ *   n_draft     in  [n_slots] int32 device: nodes of the slot (clamped to [0, T]); NULL = T.  Nothing is computed or written for
+ *               the nodes past it: their rows of O and LSE stay as they were.
+ *   O           out [n_slots, T, Hq, d]: float32 if out_is_f32 != 0 (a part of a later merge, e.g. with pulsar_phase2_attn's partials
+ *               of a context that all slots share), else bf16
+ *   LSE         out [n_slots, T, Hq] float32 or NULL
+ *   Nodes whose row lies past the table's last page set PULSAR_DEV_BAD_LENGTH; they are attended to, but not written.  A row
+ *   without a visible key cannot occur (a node sees itself).
+ *
+ * Requirements (else PULSAR_ERR_SHAPE): those of the paged cache, 1 <= T <= 64, Hq % Hkv == 0, Hq/Hkv in {1,2,4,8,16}.
+ * ------------------------------------------------------------------------------------------ */
+size_t pulsar_tree_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t Hq, int32_t Hkv, int32_t d);
+
+int32_t pulsar_tree_attn(const uint16_t *Q, const uint16_t *Knew, const uint16_t *Vnew, int32_t T,
+                         uint16_t *K_pages, uint16_t *V_pages, int32_t n_pages, int32_t page_size,
+                         const int32_t *page_table, const int32_t *cache_len, int32_t n_slots, int32_t max_pages,
+                         const int32_t *parent, const int32_t *n_draft, int32_t Hq, int32_t Hkv, int32_t d,
+                         float softmax_scale, void *O, int32_t out_is_f32, float *LSE,
+                         void *workspace, size_t workspace_bytes, int32_t *device_status, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Attention over the pages that a query selects: a decoding step that reads key bounds of the whole cache, but keys and values of
+ * k pages only (the selection of Section 3.1 made again for every token, by the token itself).
+ *
+ * For token u of slot s and KV head h, full page b (all its rows below cache_len) has the score
+ *   max over the query heads q of h's group of  sum_j (q_j > 0 ? q_j * max_bj : q_j * min_bj),
+ * with the bounds of pulsar_pages_summarize: no key of the page has a larger q.k.  Products and sums are formed in float64; a score
+ * that is not a number ranks like -inf.  Selected are the first `sink` and the last `window` full pages and the best others, k
+ * in all (all full pages if there are no more than k), equal scores going to the lower page.  Token u then attends to the rows
+ * of the selected pages, the rows after the last full page, and the new tokens 0 .. u, whose keys and values are written to
+ * their rows of the pages by this call.
+ *
+ *   Q, Knew, Vnew, K_pages, V_pages, n_draft, LSE as in pulsar_tree_attn; O out [n_slots, T, Hq, d] bf16
+ *   summary     in  [n_pages, Hkv, 2, d] bf16 (one layer of pulsar_pages_summarize)
+ *   sel         out [n_slots, T, Hkv, k] int32: ordinals of the selected pages within their slot, ascending, then -1
+ *
+ * Requirements (else PULSAR_ERR_SHAPE): those of pulsar_tree_attn, 1 <= k, 0 <= sink, 0 <= window, sink + window <= k <= 65536,
+ * n_slots * T * Hkv <= 2^20.
+ * ------------------------------------------------------------------------------------------ */
+size_t pulsar_sparse_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t max_pages, int32_t k, int32_t Hq, int32_t Hkv,
+                                          int32_t d);
+
+int32_t pulsar_sparse_attn(const uint16_t *Q, const uint16_t *Knew, const uint16_t *Vnew, int32_t T,
+                           uint16_t *K_pages, uint16_t *V_pages, const uint16_t *summary, int32_t n_pages, int32_t page_size,
+                           const int32_t *page_table, const int32_t *cache_len, int32_t n_slots, int32_t max_pages,
+                           const int32_t *n_draft, int32_t k, int32_t sink, int32_t window,
+                           int32_t Hq, int32_t Hkv, int32_t d, float softmax_scale, uint16_t *O, float *LSE, int32_t *sel,
+                           void *workspace, size_t workspace_bytes, int32_t *device_status, void *stream);
 
 #ifdef __cplusplus
 }

@@ -26,6 +26,7 @@ STATUS_NAMES = {
     7: "PULSAR_ERR_TIMEOUT", 8: "PULSAR_ERR_DEVICE_CHECK",
 }
 DEV_BAD_TOKEN, DEV_BAD_PREFIX, DEV_TIMEOUT, DEV_BAD_LENGTH, DEV_BAD_POSITION = 0x1, 0x2, 0x4, 0x8, 0x10
+DEV_BAD_PAGE, DEV_BAD_TREE, DEV_NO_PAGES = 0x20, 0x40, 0x80
 
 EXPORTS = (
     "pulsar_status_string", "pulsar_abi_version", "pulsar_launch_count", "pulsar_wait_selftest",
@@ -39,6 +40,9 @@ EXPORTS = (
     "pulsar_phase2_generate_workspace_bytes", "pulsar_phase2_generate_step",
     "pulsar_lse_merge", "pulsar_lse_merge_strided", "pulsar_lse_merge_peers",
     "pulsar_assemble_positions", "pulsar_rope_apply", "pulsar_rope_apply_qk", "pulsar_encode_step",
+    "pulsar_pages_fork_workspace_bytes", "pulsar_pages_fork", "pulsar_pages_compact", "pulsar_pages_append",
+    "pulsar_pages_summarize", "pulsar_tree_attn_workspace_bytes", "pulsar_tree_attn",
+    "pulsar_sparse_attn_workspace_bytes", "pulsar_sparse_attn",
 )
 
 
@@ -129,6 +133,26 @@ def load_library(build_if_missing: bool = False):
     lib.pulsar_rope_apply.restype = i32
     lib.pulsar_rope_apply_qk.argtypes = [vp, vp, i32, vp, vp, i32, i64, i32, vp, ctypes.c_double, vp, vp]
     lib.pulsar_rope_apply_qk.restype = i32
+    lib.pulsar_pages_fork_workspace_bytes.argtypes = [i32, i32]
+    lib.pulsar_pages_fork_workspace_bytes.restype = sz
+    lib.pulsar_pages_fork.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp, vp]
+    lib.pulsar_pages_fork.restype = i32
+    lib.pulsar_pages_compact.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, i32, i32, vp, i32, vp, vp, vp]
+    lib.pulsar_pages_compact.restype = i32
+    lib.pulsar_pages_append.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, i32, i32, vp, vp, i32, i32, vp, vp]
+    lib.pulsar_pages_append.restype = i32
+    lib.pulsar_pages_summarize.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp, vp, i32, i32, vp, vp, vp]
+    lib.pulsar_pages_summarize.restype = i32
+    lib.pulsar_tree_attn_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+    lib.pulsar_tree_attn_workspace_bytes.restype = sz
+    lib.pulsar_tree_attn.argtypes = [vp, vp, vp, i32, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp, i32, i32, i32, f32, vp, i32, vp,
+                                     vp, sz, vp, vp]
+    lib.pulsar_tree_attn.restype = i32
+    lib.pulsar_sparse_attn_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i32]
+    lib.pulsar_sparse_attn_workspace_bytes.restype = sz
+    lib.pulsar_sparse_attn.argtypes = [vp, vp, vp, i32, vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, i32, i32, i32, i32, i32, i32, f32,
+                                       vp, vp, vp, vp, sz, vp, vp]
+    lib.pulsar_sparse_attn.restype = i32
     from . import _native
     _native.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS}, PulsarError)
     _ext = _native
@@ -416,3 +440,60 @@ def pulsar_retain_block_kv(K, V, cu_seqlens, block_size: int):
     """The retained KV of assembled inputs: the last ``block_size`` rows of every input.  K, V
     [total_rows,Hkv,d] CUDA bf16, cu_seqlens a host sequence.  Returns (K_ret, V_ret) [n_seq*block_size,Hkv,d]."""
     return _native_module().retain_block_kv(K, V, cu_seqlens, block_size)
+
+
+def pulsar_pages_fork(page_table, cache_len, parent, K_pages, V_pages, reserve_rows: int = 0, out=None, workspace=None, status=None):
+    """Fork, reorder and free the continuations of a paged cache, and reserve pages: slot i of the result continues slot
+    ``parent[i]`` (CUDA int32 [n_new]; -1 = empty; None = every slot continues itself) and has pages for ``reserve_rows`` more rows.
+    page_table int32 [n_slots, max_pages], cache_len int32 [n_slots], K_pages, V_pages bf16 [n_layers, n_pages, page_size, Hkv, d]
+    (the half-filled last pages of forked slots are copied in every layer).  ``out``: (new_table, new_len, n_free) preallocated,
+    apart from the inputs.  Returns (new_table [n_new, max_pages], new_len [n_new], n_free [1])."""
+    table, length, free = out if out is not None else (None, None, None)
+    return _native_module().pages_fork(K_pages, V_pages, page_table, cache_len, parent, reserve_rows, table, length, free, workspace,
+                                       status)
+
+
+def pulsar_pages_compact(K_pages, V_pages, page_table, cache_len, accept, out=None, status=None):
+    """Move the accepted nodes of verified trees up behind their sequences, in every layer: row cache_len + accept[s, j] to row
+    cache_len + j.  ``accept``: CUDA int32 [n_slots, T], ascending, then -1.  Returns the new lengths (``out``, or a new tensor)."""
+    return _native_module().pages_compact(K_pages, V_pages, page_table, cache_len, accept, out, status)[0]
+
+
+def pulsar_pages_append(Knew, Vnew, K_pages, V_pages, page_table, cache_len, n_new=None, status=None):
+    """Write Knew, Vnew [n_slots, T, Hkv, d] to rows cache_len .. of one layer's pages [n_pages, page_size, Hkv, d]; ``n_new``: CUDA
+    int32 [n_slots], the rows of each slot (None: all T).  The caller advances cache_len."""
+    _native_module().pages_append(Knew, Vnew, K_pages, V_pages, page_table, cache_len, n_new, status)
+
+
+def pulsar_pages_summarize(K_pages, page_table, row_begin, row_end, summary, status=None):
+    """Key bounds of the pages that are full at ``row_end`` and have a row from ``row_begin`` on (CUDA int32 [n_slots]; None: from
+    the start): K_pages [n_layers, n_pages, page_size, Hkv, d] -> ``summary`` bf16 [n_layers, n_pages, Hkv, 2, d], smallest and
+    largest component.  Both also without the first dimension."""
+    _native_module().pages_summarize(K_pages, page_table, row_begin, row_end, summary, status)
+
+
+def tree_attn_workspace_bytes(n_slots, T, Hq, Hkv, d) -> int:
+    return load_library().pulsar_tree_attn_workspace_bytes(n_slots, T, Hq, Hkv, d)
+
+
+def pulsar_tree_attn(Q, Knew, Vnew, K_pages, V_pages, page_table, cache_len, parent=None, n_draft=None, softmax_scale: float = 0.0,
+                     out=None, lse_out=None, workspace=None, status=None):
+    """Attention of drafted trees: node t of slot s sees the slot's cached rows, its ancestors and itself; its KV is written to row
+    cache_len[s] + t.  Q [n_slots, T, Hq, d], Knew, Vnew [n_slots, T, Hkv, d] CUDA bf16, K_pages, V_pages [n_pages, page_size,
+    Hkv, d] (one layer, updated in place), ``parent`` int32 [n_slots, T] (-1 or an earlier node; None: a chain), ``n_draft``
+    int32 [n_slots] (None: T nodes everywhere).  ``out`` may be float32.  Returns (O [n_slots, T, Hq, d], LSE f32 [n_slots, T, Hq])."""
+    return _native_module().tree_attn(Q, Knew, Vnew, K_pages, V_pages, page_table, cache_len, parent, n_draft, softmax_scale, out,
+                                      lse_out, workspace, status)
+
+
+def sparse_attn_workspace_bytes(n_slots, T, max_pages, k, Hq, Hkv, d) -> int:
+    return load_library().pulsar_sparse_attn_workspace_bytes(n_slots, T, max_pages, k, Hq, Hkv, d)
+
+
+def pulsar_sparse_attn(Q, Knew, Vnew, K_pages, V_pages, summary, page_table, cache_len, k: int, sink: int = 0, window: int = 0,
+                       n_draft=None, softmax_scale: float = 0.0, out=None, lse_out=None, sel_out=None, workspace=None, status=None):
+    """Attention of new tokens over the ``k`` full pages that each of them selects by the key bounds in ``summary`` [n_pages, Hkv, 2, d]
+    (the first ``sink`` and the last ``window`` always), the rows after the last full page and the new tokens up to itself.
+    Other arguments as in ``pulsar_tree_attn``.  Returns (O, LSE, sel int32 [n_slots, T, Hkv, k])."""
+    return _native_module().sparse_attn(Q, Knew, Vnew, K_pages, V_pages, summary, page_table, cache_len, k, sink, window, n_draft,
+                                        softmax_scale, out, lse_out, sel_out, workspace, status)

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -25,7 +26,9 @@ namespace {
     X(pulsar_gather_kv_rows) X(pulsar_phase1_attn_sharded) X(pulsar_causal_varlen_attn) X(pulsar_retain_block_kv)  \
     X(pulsar_phase2_choose_splits) X(pulsar_phase2_workspace_bytes) X(pulsar_phase2_attn)                          \
     X(pulsar_phase2_generate_workspace_bytes) X(pulsar_phase2_generate_step) X(pulsar_lse_merge_strided)           \
-    X(pulsar_rope_apply_qk) X(pulsar_encode_step)
+    X(pulsar_rope_apply_qk) X(pulsar_encode_step) X(pulsar_pages_fork_workspace_bytes) X(pulsar_pages_fork)           \
+    X(pulsar_pages_compact) X(pulsar_pages_append) X(pulsar_pages_summarize) X(pulsar_tree_attn_workspace_bytes)      \
+    X(pulsar_tree_attn) X(pulsar_sparse_attn_workspace_bytes) X(pulsar_sparse_attn)
 
 struct Entries {
 #define X(name) decltype(&::name) name = nullptr;
@@ -490,6 +493,242 @@ PyObject* rope_apply_qk(Args& a) {
     return result({Qo, Ko});
 }
 
+// ---- a paged cache ----------------------------------------------------------------------------------------------------
+int32_t as32(int64_t x, const char* name) {
+    if (x > INT32_MAX) raise(PyExc_OverflowError, std::string(name) + ": a size does not fit 32 bits");
+    return static_cast<int32_t>(x);
+}
+
+// Tensors of one call: all on the device of the first, which is made the current one.
+struct OneDevice {
+    at::Device device;
+    c10::cuda::CUDAGuard guard;
+    explicit OneDevice(const at::Tensor& first) : device(first.device()), guard(device) {}
+    const at::Tensor& operator()(const at::Tensor& t, const char* name) const {
+        if (t.defined() && t.device() != device) raise(PyExc_ValueError, std::string(name) + ": expected a tensor on " + device.str());
+        return t;
+    }
+    // An int32 tensor of n entries, or none.
+    at::Tensor ints(Args& a, const char* name, int64_t n, bool optional = false) const {
+        if (optional && a.i < a.n && a.v[a.i] == Py_None) return a.tensor();
+        at::Tensor t = (*this)(a.i32s(name), name);
+        if (t.numel() != n) raise(PyExc_ValueError, std::string(name) + ": expected " + std::to_string(n) + " entries");
+        return t;
+    }
+    // A tensor that the call writes, given by the caller or none.
+    at::Tensor out(Args& a, const char* name, at::IntArrayRef sizes, std::initializer_list<at::ScalarType> dtypes) const {
+        if (a.i < a.n && a.v[a.i] == Py_None) return a.tensor();
+        at::Tensor t = a.tensor();
+        bool ok = t.is_cuda() && t.is_contiguous() && t.sizes() == sizes;
+        bool type = false;
+        for (at::ScalarType d : dtypes) type |= t.scalar_type() == d;
+        if (!ok || !type) raise(PyExc_TypeError, std::string(name) + ": expected a contiguous CUDA tensor of the result's shape and type");
+        return (*this)(t, name);
+    }
+    at::Tensor workspace(Args& a) const {
+        at::Tensor t = a.tensor();
+        if (t.defined() && (!t.is_cuda() || !t.is_contiguous() || t.scalar_type() != at::kByte)) raise(PyExc_TypeError, "workspace: expected a contiguous CUDA tensor of Byte");
+        return (*this)(t, "workspace");
+    }
+    at::Tensor status(Args& a) const {
+        if (a.i < a.n && a.v[a.i] == Py_None) return a.tensor();
+        at::Tensor t = (*this)(a.i32s("status"), "status");
+        if (t.numel() < 1) raise(PyExc_ValueError, "status: expected one entry");
+        return t;
+    }
+};
+
+// Pages of every layer [n_layers, n_pages, page_size, Hkv, d], or of one (4 dimensions).
+struct Pool {
+    at::Tensor K, V;
+    int32_t n_layers = 1, n_pages, page_size, Hkv, d;
+    Pool(Args& a, bool values, bool layers) : K(a.bf16("K_pages")) {
+        if (values) V = a.bf16("V_pages");
+        const int64_t lead = K.dim() - 4;
+        if (lead < 0 || lead > (layers ? 1 : 0))
+            raise(PyExc_ValueError, layers ? "K_pages: expected [n_layers, n_pages, page_size, Hkv, d]" : "K_pages: expected [n_pages, page_size, Hkv, d]");
+        if (values && (V.sizes() != K.sizes() || V.device() != K.device())) raise(PyExc_ValueError, "V_pages: expected the shape and the device of K_pages");
+        if (lead == 1) n_layers = as32(K.size(0), "K_pages");
+        n_pages = as32(K.size(lead), "K_pages");
+        page_size = as32(K.size(lead + 1), "K_pages");
+        Hkv = as32(K.size(lead + 2), "K_pages");
+        d = as32(K.size(lead + 3), "K_pages");
+    }
+};
+
+struct Table {
+    at::Tensor table;
+    int32_t n_slots, max_pages;
+    Table(Args& a, const OneDevice& on) : table(on(a.i32s("page_table"), "page_table")) {
+        if (table.dim() != 2) raise(PyExc_ValueError, "page_table: expected [n_slots, max_pages]");
+        n_slots = as32(table.size(0), "page_table");
+        max_pages = as32(table.size(1), "page_table");
+    }
+};
+
+// (K_pages, V_pages, page_table, cache_len, parent, reserve_rows, out_table, out_len, out_free, workspace, status)
+PyObject* pages_fork(Args& a) {
+    Pool p(a, true, true);
+    const OneDevice on(p.K);
+    Table t(a, on);
+    at::Tensor len = on.ints(a, "cache_len", t.n_slots);
+    at::Tensor parent;
+    if (a.i < a.n && a.v[a.i] == Py_None) parent = a.tensor();
+    else parent = on(a.i32s("parent"), "parent");
+    const int32_t n_new = parent.defined() ? as32(parent.numel(), "parent") : t.n_slots, reserve = a.i32();
+    at::Tensor table = on.out(a, "out", {n_new, t.max_pages}, {at::kInt}), new_len = on.out(a, "out", {n_new}, {at::kInt}),
+               n_free = on.out(a, "out", {1}, {at::kInt}), ws = on.workspace(a), status = on.status(a);
+    if (!table.defined()) table = empty({n_new, t.max_pages}, at::kInt, len);
+    if (!new_len.defined()) new_len = empty({n_new}, at::kInt, len);
+    if (!n_free.defined()) n_free = empty({1}, at::kInt, len);
+    ws = workspace_or(ws, ws.defined() ? 0 : g.pulsar_pages_fork_workspace_bytes(n_new, p.n_pages), p.K);
+    call("pulsar_pages_fork", [&, st = stream()] {
+        return g.pulsar_pages_fork(ptr<int32_t>(t.table), ptr<int32_t>(len), t.n_slots, t.max_pages, ptr<int32_t>(parent), n_new,
+                                   ptr<uint16_t>(p.K), ptr<uint16_t>(p.V), p.n_layers, p.n_pages, p.page_size, p.Hkv, p.d, reserve,
+                                   ptr<int32_t>(table), ptr<int32_t>(new_len), ptr<int32_t>(n_free), ptr<void>(ws),
+                                   static_cast<size_t>(ws.numel()), ptr<int32_t>(status), st);
+    });
+    return result({table, new_len, n_free});
+}
+
+// (K_pages, V_pages, page_table, cache_len, accept, out_len, status)
+PyObject* pages_compact(Args& a) {
+    Pool p(a, true, true);
+    const OneDevice on(p.K);
+    Table t(a, on);
+    at::Tensor len = on.ints(a, "cache_len", t.n_slots), accept = on(a.i32s("accept"), "accept");
+    if (accept.dim() != 2 || accept.size(0) != t.n_slots) raise(PyExc_ValueError, "accept: expected [n_slots, T]");
+    const int32_t T = as32(accept.size(1), "accept");
+    at::Tensor new_len = on.out(a, "out", {t.n_slots}, {at::kInt}), status = on.status(a);
+    if (!new_len.defined()) new_len = empty({t.n_slots}, at::kInt, len);
+    call("pulsar_pages_compact", [&, st = stream()] {
+        return g.pulsar_pages_compact(ptr<uint16_t>(p.K), ptr<uint16_t>(p.V), p.n_layers, p.n_pages, p.page_size, p.Hkv, p.d,
+                                      ptr<int32_t>(t.table), ptr<int32_t>(len), t.n_slots, t.max_pages, ptr<int32_t>(accept), T,
+                                      ptr<int32_t>(new_len), ptr<int32_t>(status), st);
+    });
+    return result({new_len});
+}
+
+// New tokens of every slot [n_slots, T, Hkv, d].
+struct Fresh {
+    at::Tensor K, V;
+    int32_t n_slots, T;
+    Fresh(Args& a, const OneDevice* on) : K(a.bf16("Knew", 4)), V(a.bf16("Vnew", 4)) {
+        n_slots = as32(K.size(0), "Knew");
+        T = as32(K.size(1), "Knew");
+        if (V.sizes() != K.sizes() || V.device() != K.device()) raise(PyExc_ValueError, "Vnew: expected the shape and the device of Knew");
+        if (on) (*on)(K, "Knew");
+    }
+    void fits(const Pool& p, const Table& t) const {
+        if (n_slots != t.n_slots) raise(PyExc_ValueError, "Knew: expected n_slots as many as in page_table");
+        if (K.size(2) != p.Hkv || K.size(3) != p.d) raise(PyExc_ValueError, "Knew: expected the heads and the head size of K_pages");
+    }
+};
+
+// (Knew, Vnew, K_pages, V_pages, page_table, cache_len, n_new, status)
+PyObject* pages_append(Args& a) {
+    Fresh f(a, nullptr);
+    const OneDevice on(f.K);
+    Pool p(a, true, false);
+    on(p.K, "K_pages");
+    Table t(a, on);
+    f.fits(p, t);
+    at::Tensor len = on.ints(a, "cache_len", t.n_slots), n_new = on.ints(a, "n_new", t.n_slots, true), status = on.status(a);
+    call("pulsar_pages_append", [&, st = stream()] {
+        return g.pulsar_pages_append(in16(f.K), in16(f.V), f.T, ptr<int32_t>(n_new), ptr<uint16_t>(p.K), ptr<uint16_t>(p.V), p.n_pages,
+                                     p.page_size, p.Hkv, p.d, ptr<int32_t>(t.table), ptr<int32_t>(len), t.n_slots, t.max_pages,
+                                     ptr<int32_t>(status), st);
+    });
+    Py_RETURN_NONE;
+}
+
+// (K_pages, page_table, row_begin, row_end, summary, status)
+PyObject* pages_summarize(Args& a) {
+    Pool p(a, false, true);
+    const OneDevice on(p.K);
+    Table t(a, on);
+    at::Tensor first = on.ints(a, "row_begin", t.n_slots, true), last = on.ints(a, "row_end", t.n_slots),
+               summary = on(a.bf16("summary"), "summary"), status = on.status(a);
+    std::vector<int64_t> want = p.K.sizes().vec();
+    want[want.size() - 3] = p.Hkv;
+    want[want.size() - 2] = 2;
+    if (summary.sizes() != at::IntArrayRef(want)) raise(PyExc_ValueError, "summary: expected [n_layers, n_pages, Hkv, 2, d]");
+    call("pulsar_pages_summarize", [&, st = stream()] {
+        return g.pulsar_pages_summarize(in16(p.K), p.n_layers, p.n_pages, p.page_size, p.Hkv, p.d, ptr<int32_t>(t.table), ptr<int32_t>(first),
+                                        ptr<int32_t>(last), t.n_slots, t.max_pages, ptr<uint16_t>(summary), ptr<int32_t>(status), st);
+    });
+    Py_RETURN_NONE;
+}
+
+struct PagedQuery {
+    at::Tensor Q;
+    int32_t Hq;
+    explicit PagedQuery(Args& a) : Q(a.bf16("Q", 4)), Hq(as32(Q.size(2), "Q")) {}
+    void fits(const Fresh& f, const Pool& p) const {
+        if (Q.size(0) != f.n_slots || Q.size(1) != f.T || Q.size(3) != p.d) raise(PyExc_ValueError, "Q: expected [n_slots, T, Hq, d] as Knew");
+    }
+};
+
+// (Q, Knew, Vnew, K_pages, V_pages, page_table, cache_len, parent, n_draft, scale, out, lse_out, workspace, status)
+PyObject* tree_attn(Args& a) {
+    PagedQuery q(a);
+    const OneDevice on(q.Q);
+    Fresh f(a, &on);
+    Pool p(a, true, false);
+    on(p.K, "K_pages");
+    Table t(a, on);
+    f.fits(p, t);
+    q.fits(f, p);
+    at::Tensor len = on.ints(a, "cache_len", t.n_slots), parent = on.ints(a, "parent", static_cast<int64_t>(f.n_slots) * f.T, true),
+               n_draft = on.ints(a, "n_draft", t.n_slots, true);
+    const float scale = static_cast<float>(a.real());
+    at::Tensor out = on.out(a, "out", q.Q.sizes(), {at::kBFloat16, at::kFloat}),
+               lse = on.out(a, "lse_out", {f.n_slots, f.T, q.Hq}, {at::kFloat}), ws = on.workspace(a), status = on.status(a);
+    if (!out.defined()) out = at::empty_like(q.Q);
+    if (!lse.defined()) lse = empty({f.n_slots, f.T, q.Hq}, at::kFloat, q.Q);
+    ws = workspace_or(ws, ws.defined() ? 0 : g.pulsar_tree_attn_workspace_bytes(f.n_slots, f.T, q.Hq, p.Hkv, p.d), q.Q);
+    call("pulsar_tree_attn", [&, st = stream()] {
+        return g.pulsar_tree_attn(in16(q.Q), in16(f.K), in16(f.V), f.T, ptr<uint16_t>(p.K), ptr<uint16_t>(p.V), p.n_pages, p.page_size,
+                                  ptr<int32_t>(t.table), ptr<int32_t>(len), t.n_slots, t.max_pages, ptr<int32_t>(parent),
+                                  ptr<int32_t>(n_draft), q.Hq, p.Hkv, p.d, scale, ptr<void>(out), out.scalar_type() == at::kFloat ? 1 : 0,
+                                  ptr<float>(lse), ptr<void>(ws), static_cast<size_t>(ws.numel()), ptr<int32_t>(status), st);
+    });
+    return result({out, lse});
+}
+
+// (Q, Knew, Vnew, K_pages, V_pages, summary, page_table, cache_len, k, sink, window, n_draft, scale, out, lse_out, sel_out, workspace, status)
+PyObject* sparse_attn(Args& a) {
+    PagedQuery q(a);
+    const OneDevice on(q.Q);
+    Fresh f(a, &on);
+    Pool p(a, true, false);
+    on(p.K, "K_pages");
+    at::Tensor summary = on(a.bf16("summary", 4), "summary");
+    if (summary.size(0) != p.n_pages || summary.size(1) != p.Hkv || summary.size(2) != 2 || summary.size(3) != p.d)
+        raise(PyExc_ValueError, "summary: expected [n_pages, Hkv, 2, d]");
+    Table t(a, on);
+    f.fits(p, t);
+    q.fits(f, p);
+    at::Tensor len = on.ints(a, "cache_len", t.n_slots);
+    const int32_t k = a.i32(), sink = a.i32(), window = a.i32();
+    at::Tensor n_draft = on.ints(a, "n_draft", t.n_slots, true);
+    const float scale = static_cast<float>(a.real());
+    const int64_t width = k > 0 ? k : 0;
+    at::Tensor out = on.out(a, "out", q.Q.sizes(), {at::kBFloat16}), lse = on.out(a, "lse_out", {f.n_slots, f.T, q.Hq}, {at::kFloat}),
+               sel = on.out(a, "sel_out", {f.n_slots, f.T, p.Hkv, width}, {at::kInt}), ws = on.workspace(a), status = on.status(a);
+    if (!out.defined()) out = at::empty_like(q.Q);
+    if (!lse.defined()) lse = empty({f.n_slots, f.T, q.Hq}, at::kFloat, q.Q);
+    if (!sel.defined()) sel = empty({f.n_slots, f.T, p.Hkv, width}, at::kInt, q.Q);
+    ws = workspace_or(ws, ws.defined() ? 0 : g.pulsar_sparse_attn_workspace_bytes(f.n_slots, f.T, t.max_pages, k, q.Hq, p.Hkv, p.d), q.Q);
+    call("pulsar_sparse_attn", [&, st = stream()] {
+        return g.pulsar_sparse_attn(in16(q.Q), in16(f.K), in16(f.V), f.T, ptr<uint16_t>(p.K), ptr<uint16_t>(p.V), in16(summary), p.n_pages,
+                                    p.page_size, ptr<int32_t>(t.table), ptr<int32_t>(len), t.n_slots, t.max_pages, ptr<int32_t>(n_draft),
+                                    k, sink, window, q.Hq, p.Hkv, p.d, scale, ptr<uint16_t>(out), ptr<float>(lse), ptr<int32_t>(sel),
+                                    ptr<void>(ws), static_cast<size_t>(ws.numel()), ptr<int32_t>(status), st);
+    });
+    return result({out, lse, sel});
+}
+
 // bind({name: address}, error class): the library build to call.
 PyObject* bind(Args& a) {
     PyObject* table = a.next();
@@ -511,7 +750,8 @@ PyObject* bind(Args& a) {
 #define M(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {M(bind), M(maxidf_select), M(chunk_select), M(phase1_attn), M(phase1_attn_sharded), M(causal_varlen_attn),
                          M(retain_block_kv), M(pack_summary_kv), M(gather_kv_rows), M(phase2_attn), M(phase2_generate_step),
-                         M(lse_merge_strided), M(rope_apply_qk), M(encode_step), {nullptr, nullptr, 0, nullptr}};
+                         M(lse_merge_strided), M(rope_apply_qk), M(encode_step), M(pages_fork), M(pages_compact), M(pages_append),
+                         M(pages_summarize), M(tree_attn), M(sparse_attn), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,933 @@
+// Attention over a paged key/value cache: drafted trees (every cached row) and selected pages (include/pulsar.h).
+//
+// Lengths live on the device, so a launch does not know how much work it has.  A work item is up to eight query rows of one KV
+// head (tree: nodes x heads of the group; selected pages: the group's heads of one token) against a list of keys, cut into pieces
+// of 16 keys (d = 128; 32 with d = 64).  Every CTA adds up the pieces of all slots, takes an equal share of them, whichever items they
+// belong to, and leaves a partial (normalised output and l = ln sum exp) where it holds an item only in part; a second
+// launch joins those.
+#include <algorithm>
+
+#include "mma.cuh"
+#include "paged.cuh"
+
+namespace pulsar {
+
+namespace {
+
+constexpr int kWarps = 8;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kRows = 8;                        // query rows of an item: the columns of a matrix fragment
+constexpr int kUnitBytes = 4096;
+constexpr int kUnits = 3;                       // of a warp's ring: one in use, two on their way
+constexpr int kRingBytes = kWarps * kUnits * kUnitBytes;
+constexpr int kMaxSlots = 1024, kMaxTree = 64;
+constexpr int kLeastPieces = 3 * kWarps;        // of a CTA: three per warp, unless all CTAs have fewer
+
+struct Meta {                                   // the item that begins in a CTA and goes on in the next ones
+    int first, parts;                           // first partial (those of the CTAs after it are their first ones); 0: there is none
+    int token0, head0, row0, rows;              // of its rows: see row_of
+};
+
+struct PagedArgs {
+    const uint16_t *Q, *Knew, *Vnew;             // [n_slots, T, Hq | Hkv, D]
+    uint16_t *K, *V;                             // [n_pages, page_size, Hkv, D]
+    const int32_t *table, *len, *n_draft, *parent;
+    const int32_t* list;                         // selected pages: [n_slots, T, Hkv, k + 1] page ids, the last row's page among them
+    int n_slots, T, Hq, Hkv, g_shift, page_shift, n_pages, max_pages, k;
+    float scale_log2;
+    void* O;
+    int out_f32;
+    float* LSE;
+    float *part_O, *part_LSE;                    // [2 * CTAs, kRows, D], [2 * CTAs, kRows]
+    Meta* meta;                                  // [CTAs]
+    int32_t* status;
+};
+
+// Bookkeeping of a slot, the same in every CTA.
+struct SlotWork {
+    int len, n;                                  // rows in the cache; new tokens
+    int keys;                                    // cached rows an item reads
+    int cache_pieces, pieces, items;
+};
+template <bool kSparse, int kKeys>
+__device__ __forceinline__ SlotWork slot_work(const PagedArgs& a, int slot, bool tell) {
+    SlotWork w;
+    w.len = checked_len(a.len[slot], static_cast<int64_t>(a.max_pages) << a.page_shift, tell, a.status);
+    w.n = a.n_draft != nullptr ? min(max(a.n_draft[slot], 0), a.T) : a.T;
+    const int full = w.len >> a.page_shift;
+    w.keys = kSparse ? (min(a.k, full) << a.page_shift) + (w.len - (full << a.page_shift)) : w.len;
+    w.cache_pieces = (w.keys + kKeys - 1) / kKeys;
+    w.pieces = w.cache_pieces + (w.n + kKeys - 1) / kKeys;
+    const int g = 1 << a.g_shift;
+    w.items = kSparse ? w.n * a.Hkv * ((g + kRows - 1) / kRows) : a.Hkv * ((w.n * g + kRows - 1) / kRows);
+    return w;
+}
+
+// Row r of an item: token token0 + r' / g and head head0 + r' % g, with r' = row0 + r.
+__device__ __forceinline__ int64_t row_of(int token0, int head0, int row0, int r, int g_shift, int Hq) {
+    const int x = row0 + r;
+    return static_cast<int64_t>(token0 + (x >> g_shift)) * Hq + head0 + (x & ((1 << g_shift) - 1));
+}
+
+// Two CTAs per SM: while the keys of one are on their way, the other computes.
+template <int D, bool kSparse>
+__global__ void __launch_bounds__(kThreads, 2)
+paged_rows_kernel(const __grid_constant__ PagedArgs a) {
+    constexpr int kKeys = kUnitBytes / (2 * D);                // keys of a piece: 16 (d = 128), 32 (d = 64)
+    constexpr int kHalves = kKeys / 16;                        // runs of 16 keys lie in one page
+    constexpr int kVecs = D / 8;                               // 16-byte vectors of a row
+    constexpr int kRowsPerCopy = 32 / kVecs;                   // rows a warp copies with one instruction
+    constexpr int kCopies = kKeys / kRowsPerCopy;
+    constexpr int kPitch = D + 4;                              // floats of a partial row: 2 * kPitch = 8 modulo the banks
+    static_assert(kWarps * kRows * kPitch * 4 <= kRingBytes, "the warps' partials take the ring's place");
+    extern __shared__ __align__(1024) uint8_t smem[];
+    float2* w_ml = reinterpret_cast<float2*>(smem + kRingBytes);               // [kRows][kWarps]
+    uint64_t* s_sees = reinterpret_cast<uint64_t*>(w_ml + kRows * kWarps);     // [kMaxTree] a node's ancestors and itself
+    int64_t* s_pieces = reinterpret_cast<int64_t*>(s_sees + kMaxTree);         // [n_slots + 1] pieces of the slots before
+    int64_t* s_warp = s_pieces + kMaxSlots + 1;                                // [kWarps]
+    int* s_up = reinterpret_cast<int*>(s_warp + kWarps);                       // [kMaxTree]
+    float* w_o = reinterpret_cast<float*>(smem);                               // [kWarps][kRows][kPitch], where the rings were
+
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int gid = lane >> 2, tig = lane & 3;
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    // ---- all pieces of all slots, and this CTA's share ----
+    int64_t total = 0;
+    for (int s0 = 0; s0 < a.n_slots; s0 += kThreads) {
+        const int s = s0 + threadIdx.x;
+        int64_t x = 0;
+        if (s < a.n_slots) {
+            const SlotWork w = slot_work<kSparse, kKeys>(a, s, blockIdx.x == 0);
+            x = static_cast<int64_t>(w.pieces) * w.items;
+        }
+        int64_t y = x;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t z = __shfl_up_sync(0xffffffffu, y, d);
+            if (lane >= d) y += z;
+        }
+        if (lane == 31) s_warp[warp] = y;
+        __syncthreads();
+        int64_t before = total;
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) before += s_warp[w];
+            total += s_warp[w];
+        }
+        if (s < a.n_slots) s_pieces[s] = before + y - x;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) s_pieces[a.n_slots] = total;
+    __syncthreads();
+    const int64_t n_ctas = max(static_cast<int64_t>(1), min(static_cast<int64_t>(gridDim.x), total / kLeastPieces));
+    const int64_t begin = blockIdx.x < n_ctas ? total * blockIdx.x / n_ctas : total;
+    const int64_t end = blockIdx.x < n_ctas ? total * (blockIdx.x + 1) / n_ctas : total;
+    if (begin >= end) {
+        if (threadIdx.x == 0) a.meta[blockIdx.x].parts = 0;
+        return;
+    }
+    int slot = 0;
+    {
+        int hi = a.n_slots - 1;                                // the last slot that begins at or before this CTA's first piece
+        while (slot < hi) {
+            const int mid = (slot + hi + 1) >> 1;
+            if (s_pieces[mid] <= begin) slot = mid;
+            else hi = mid - 1;
+        }
+    }
+
+    const uint32_t ring = smem_u32(smem) + warp * (kUnits * kUnitBytes);
+    const int copy_row = lane / kVecs, copy_vec = lane % kVecs;
+    const int64_t pitch = static_cast<int64_t>(a.Hkv) * D;     // elements between the rows of a head
+    const int page_mask = (1 << a.page_shift) - 1;
+    const int g = 1 << a.g_shift;
+    const int mi = lane >> 3, l8 = lane & 7;
+    const uint32_t k_lane = ring + ((mi & 1) * 8 + l8) * (D * 2), k_x = ((mi >> 1) ^ l8) << 4;     // K: rows are keys
+    const uint32_t v_lane = ring + ((mi >> 1) * 8 + l8) * (D * 2), v_x = ((mi & 1) ^ l8) << 4;     // V: read transposed
+    bool meta_written = false;
+
+    for (int64_t at = begin; at < end;) {
+        // ---- the next item and this CTA's pieces of it ----
+        while (s_pieces[slot + 1] <= at) ++slot;
+        const SlotWork w = slot_work<kSparse, kKeys>(a, slot, false);
+        const int item = static_cast<int>((at - s_pieces[slot]) / w.pieces);
+        const int64_t item_at = s_pieces[slot] + static_cast<int64_t>(item) * w.pieces;
+        const int p_begin = static_cast<int>(at - item_at), p_end = static_cast<int>(min(end - item_at, static_cast<int64_t>(w.pieces)));
+        const int row_blocks = kSparse ? (g + kRows - 1) / kRows : (w.n * g + kRows - 1) / kRows;
+        const int row0 = (item % row_blocks) * kRows, unit = item / row_blocks;      // unit: KV head, or token and KV head
+        const int kvh = kSparse ? unit % a.Hkv : unit, token = kSparse ? unit / a.Hkv : 0;
+        const int n_rows = min(kRows, (kSparse ? g : w.n * g) - row0);
+        const int token0 = slot * a.T + token, head0 = kvh << a.g_shift;
+        const bool appends = row0 == 0 && token == 0;
+        const int head_at = kvh * D + copy_vec * 8;
+        const int32_t* list = kSparse ? a.list + (static_cast<int64_t>(token0) * a.Hkv + kvh) * (a.k + 1)
+                                      : a.table + static_cast<int64_t>(slot) * a.max_pages;
+        const uint16_t* fresh_k = a.Knew + (static_cast<int64_t>(slot) * a.T) * pitch + head_at;
+        const uint16_t* fresh_v = a.Vnew + (static_cast<int64_t>(slot) * a.T) * pitch + head_at;
+
+        // Page ids of a piece; -1 where there is no row.
+        struct Ids { int id[kHalves]; };
+        const auto pages_of = [&](int p) {
+            Ids x;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                const int row = p * kKeys + 16 * h;
+                x.id[h] = p < p_end && row < w.keys ? list[row >> a.page_shift] : -1;
+            }
+            return x;
+        };
+        // Bit h: the rows of half h exist.
+        const auto good = [&](const Ids& x, int p) {
+            uint32_t ok = 0;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                const bool in = x.id[h] >= 0 && x.id[h] < a.n_pages;
+                if (!in && p < p_end && p * kKeys + 16 * h < w.keys && lane == 0) report(a.status, PULSAR_DEV_BAD_PAGE);
+                ok |= (in ? 1u : 0u) << h;
+            }
+            return ok;
+        };
+        // A unit is K or V of a piece.  Row r goes to line r, its vector v to place v ^ (r & 7), so that the eight rows of a
+        // matrix fragment lie in different banks.  Rows that do not exist are zeros.
+        const auto load = [&](const uint16_t* pool, const uint16_t* fresh, const Ids& x, uint32_t ok, int p, int place) {
+            if (p < p_end) {
+                const uint32_t dst = ring + place * kUnitBytes + copy_row * (D * 2);
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i) {
+                    const int r = i * kRowsPerCopy + copy_row, h = i / (kCopies / kHalves);
+                    const uint32_t to = dst + i * (kRowsPerCopy * D * 2) + ((copy_vec ^ (r & 7)) << 4);
+                    bool in;
+                    const uint16_t* src;
+                    if (p < w.cache_pieces) {
+                        const int row = p * kKeys + r;
+                        in = row < w.keys && ((ok >> h) & 1u) != 0u;
+                        src = pool + ((static_cast<int64_t>(x.id[h]) << a.page_shift) + (row & page_mask)) * pitch + head_at;
+                    } else {
+                        const int row = (p - w.cache_pieces) * kKeys + r;
+                        in = row < w.n;
+                        src = fresh + row * pitch;
+                    }
+                    cp_async16(to, in ? src : pool, in ? 16 : 0);
+                }
+            }
+            cp_async_commit();                                     // an empty group past the end keeps the count
+        };
+
+        const int p_first = p_begin + warp;
+        Ids now_ids = pages_of(p_first), next_ids = pages_of(p_first + kWarps);
+        uint32_t now_ok = good(now_ids, min(p_first, w.cache_pieces)), next_ok = 0;
+        load(a.K, fresh_k, now_ids, now_ok, p_first, 0);
+        load(a.V, fresh_v, now_ids, now_ok, p_first, 1);
+
+        // ---- which nodes a node sees: pointers to ancestors are doubled ----
+        const bool has_new = p_end > w.cache_pieces;
+        if (!kSparse && has_new && a.parent != nullptr) {
+            const int t = threadIdx.x;
+            int up = -1;
+            if (t < w.n) {
+                up = a.parent[static_cast<int64_t>(slot) * a.T + t];
+                if (up < -1 || up >= t) {
+                    report(a.status, PULSAR_DEV_BAD_TREE);
+                    up = -1;
+                }
+            }
+            uint64_t sees = t < kMaxTree ? 1ull << t : 0ull;
+#pragma unroll 1
+            for (int step = 1; step < kMaxTree; step <<= 1) {
+                if (t < kMaxTree) {
+                    s_sees[t] = sees;
+                    s_up[t] = up;
+                }
+                __syncthreads();
+                if (t < kMaxTree && up >= 0) {
+                    sees |= s_sees[up];
+                    up = s_up[up];
+                }
+                __syncthreads();
+            }
+            if (t < kMaxTree) s_sees[t] = sees;
+            __syncthreads();
+        }
+        uint64_t sees[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int r = 2 * tig + k, x = kSparse ? token : (row0 + r) >> a.g_shift;
+            sees[k] = r >= n_rows || !has_new ? 0ull : kSparse || a.parent == nullptr ? ~0ull >> (63 - x) : s_sees[x];
+        }
+
+        // ---- the query rows as B fragments ----
+        uint32_t q[D / 16][2];
+        {
+            const uint32_t* src = reinterpret_cast<const uint32_t*>(a.Q + row_of(token0, head0, row0, gid < n_rows ? gid : 0, a.g_shift, a.Hq) * D) + tig;
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                q[kk][0] = gid < n_rows ? src[kk * 8] : 0u;
+                q[kk][1] = gid < n_rows ? src[kk * 8 + 4] : 0u;
+            }
+        }
+        // rows 2 tig and 2 tig + 1; o[c]: outputs 16 c + gid and 16 c + 8 + gid of both
+        float o[D / 16][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[c][k] = 0.f;
+
+        // Units are consumed in the order K, V, K, V, ... and refilled in that order, each where the unit before it was.
+        int place = 0, free_place = kUnits - 1;
+        const auto next_unit = [&](const uint16_t* pool, const uint16_t* fresh, int p) {
+            cp_async_wait<kUnits - 2>();
+            __syncwarp();
+            load(pool, fresh, next_ids, next_ok, p, free_place);
+            const int here = place;
+            free_place = here;
+            place = here + 1 == kUnits ? 0 : here + 1;
+            return here * kUnitBytes;
+        };
+        for (int p = p_first; p < p_end; p += kWarps) {
+            next_ok = good(next_ids, min(p + kWarps, w.cache_pieces));
+            const int at_k = next_unit(a.K, fresh_k, p + kWarps);
+            const Ids later_ids = pages_of(p + 2 * kWarps);
+            // ---- S^T = K Q^T: keys gid and gid + 8 of each 16, rows 2 tig and 2 tig + 1 ----
+            float s[kKeys / 16][4];
+#pragma unroll
+            for (int j = 0; j < kKeys / 16; ++j) {
+                float t[2][4] = {};                                // two chains of products
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    uint32_t f[4];
+                    ldmatrix4(k_lane + at_k + j * (16 * D * 2) + ((kk * 32) ^ k_x), f);
+                    mma_bf16(t[kk & 1], f, q[kk][0], q[kk][1]);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[j][k] = t[0][k] + t[1][k];
+            }
+            // keys that do not exist, or that the node of a row must not see
+            if (p >= w.cache_pieces) {
+                const int first = (p - w.cache_pieces) * kKeys;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t bits = static_cast<uint32_t>(sees[k] >> first);        // (node rows past n are nobody's ancestors)
+#pragma unroll
+                    for (int j = 0; j < kKeys / 16; ++j) {
+                        if (((bits >> (16 * j + gid)) & 1u) == 0u) s[j][k] = -INFINITY;
+                        if (((bits >> (16 * j + gid + 8)) & 1u) == 0u) s[j][k + 2] = -INFINITY;
+                    }
+                }
+            } else if (w.keys - p * kKeys < kKeys || now_ok != (1u << kHalves) - 1u) {
+                const int n_vis = w.keys - p * kKeys;
+#pragma unroll
+                for (int j = 0; j < kKeys / 16; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (16 * j + gid + (k >> 1) * 8 >= n_vis || ((now_ok >> j) & 1u) == 0u) s[j][k] = -INFINITY;
+            }
+            float x[2], alpha[2], neg[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                x[k] = fmaxf(s[0][k], s[0][k + 2]);
+#pragma unroll
+                for (int j = 1; j < kKeys / 16; ++j) x[k] = max3(x[k], s[j][k], s[j][k + 2]);
+            }
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) {
+                x[0] = fmaxf(x[0], __shfl_xor_sync(0xffffffffu, x[0], d));
+                x[1] = fmaxf(x[1], __shfl_xor_sync(0xffffffffu, x[1], d));
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float m_new = fmaxf(m[k], x[k] * a.scale_log2);
+                alpha[k] = m_new == -INFINITY ? 1.f : ex2(m[k] - m_new);
+                neg[k] = m_new == -INFINITY ? 0.f : -m_new;
+                m[k] = m_new;
+            }
+            uint32_t pb[kKeys / 16][2];
+            l[0] *= alpha[0];
+            l[1] *= alpha[1];
+#pragma unroll
+            for (int j = 0; j < kKeys / 16; ++j) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[j][k] = ex2(fmaf(s[j][k], a.scale_log2, neg[k & 1]));
+                l[0] += s[j][0] + s[j][2];
+                l[1] += s[j][1] + s[j][3];
+                pb[j][0] = movmatrix(pack_bf16x2(s[j][0], s[j][1]));      // [key][row] -> [row][key]
+                pb[j][1] = movmatrix(pack_bf16x2(s[j][2], s[j][3]));
+            }
+            if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) o[c][k] *= alpha[k & 1];
+            }
+            // ---- O^T += V^T P^T ----
+            const int at_v = next_unit(a.V, fresh_v, p + kWarps);
+            bool plain = true;
+            if (p >= w.cache_pieces) {
+                // A node that a row does not see has weight 0, and 0 times an infinity or a NaN in its value would still reach the
+                // row.  Units with such values are added up one visible product at a time.
+                const uint16_t* unit_v = reinterpret_cast<const uint16_t*>(smem + warp * (kUnits * kUnitBytes) + at_v);
+                uint32_t odd = 0;
+                for (int i = lane; i < kUnitBytes / 4; i += 32) {
+                    const uint32_t x = reinterpret_cast<const uint32_t*>(unit_v)[i];
+                    odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u ? 1u : 0u;
+                }
+                plain = !__any_sync(0xffffffffu, odd != 0u);
+                if (!plain) {
+                    const int first = (p - w.cache_pieces) * kKeys;
+#pragma unroll 1
+                    for (int key = 0; key < kKeys; ++key) {
+                        const uint16_t* v = unit_v + key * D + (gid & 7);
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const float a0 = s[0][k], a1 = s[0][k + 2];
+                            float x = key & 8 ? a1 : a0;
+                            if (kKeys > 16) x = key & 16 ? (key & 8 ? s[kKeys / 16 - 1][k + 2] : s[kKeys / 16 - 1][k]) : x;
+                            x = __shfl_sync(0xffffffffu, x, (key & 7) * 4 + tig);
+                            if (((sees[k] >> (first + key)) & 1u) == 0u) continue;
+#pragma unroll
+                            for (int c = 0; c < D / 16; ++c) {
+                                const uint32_t v0 = v[((2 * c) ^ (key & 7)) * 8], v1 = v[((2 * c + 1) ^ (key & 7)) * 8];
+                                o[c][k] = fmaf(x, __uint_as_float(v0 << 16), o[c][k]);
+                                o[c][k + 2] = fmaf(x, __uint_as_float(v1 << 16), o[c][k + 2]);
+                            }
+                        }
+                    }
+                }
+            }
+            if (plain) {
+#pragma unroll
+                for (int j = 0; j < kKeys / 16; ++j)
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c) {
+                        uint32_t f[4];
+                        ldmatrix4_trans(v_lane + at_v + j * (16 * D * 2) + ((c * 32) ^ v_x), f);
+                        mma_bf16(o[c], f, pb[j][0], pb[j][1]);
+                    }
+            }
+            // The new tokens' rows go to their pages from the warp that has just read them (nobody reads those rows in this launch).
+            if (appends && p >= w.cache_pieces) {
+#pragma unroll 1
+                for (int i = 0; i < kCopies; ++i) {
+                    const int row = (p - w.cache_pieces) * kKeys + i * kRowsPerCopy + copy_row;
+                    if (row >= w.n) continue;
+                    const int64_t to_row = static_cast<int64_t>(w.len) + row;
+                    if ((to_row >> a.page_shift) >= a.max_pages) {
+                        report(a.status, PULSAR_DEV_BAD_LENGTH);
+                        continue;
+                    }
+                    const int page = a.table[static_cast<int64_t>(slot) * a.max_pages + (to_row >> a.page_shift)];
+                    if (page < 0 || page >= a.n_pages) {
+                        report(a.status, PULSAR_DEV_BAD_PAGE);
+                        continue;
+                    }
+                    const int64_t to = ((static_cast<int64_t>(page) << a.page_shift) + (to_row & page_mask)) * pitch + head_at;
+                    *reinterpret_cast<uint4*>(a.K + to) = *reinterpret_cast<const uint4*>(fresh_k + row * pitch);
+                    *reinterpret_cast<uint4*>(a.V + to) = *reinterpret_cast<const uint4*>(fresh_v + row * pitch);
+                }
+            }
+            now_ok = next_ok;
+            next_ids = later_ids;
+        }
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+            l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
+            l[1] += __shfl_xor_sync(0xffffffffu, l[1], d);
+        }
+
+        // ---- the warps' partials, brought to the CTA's maximum and added up, 32 outputs of a row per warp ----
+        if (gid == 0) {
+            w_ml[(2 * tig) * kWarps + warp] = make_float2(m[0], l[0]);
+            w_ml[(2 * tig + 1) * kWarps + warp] = make_float2(m[1], l[1]);
+        }
+        __syncthreads();
+        float f[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) f[k] = w_ml[(2 * tig + k) * kWarps + gid].x;
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+            f[0] = fmaxf(f[0], __shfl_xor_sync(0xffffffffu, f[0], d));
+            f[1] = fmaxf(f[1], __shfl_xor_sync(0xffffffffu, f[1], d));
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            f[k] = weight(m[k], f[k]);
+            if (2 * tig + k < n_rows) {
+                float* dst = w_o + (warp * kRows + 2 * tig + k) * kPitch + gid;
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    dst[16 * c] = o[c][k] * f[k];
+                    dst[16 * c + 8] = o[c][k + 2] * f[k];
+                }
+            }
+        }
+        __syncthreads();
+        const bool whole = p_begin == 0 && p_end == w.pieces;
+        const int64_t part = 2 * static_cast<int64_t>(blockIdx.x) + (at == begin ? 0 : 1);
+        for (int c = warp; c < n_rows * (D / 32); c += kWarps) {
+            const int r = c / (D / 32), at_d = (c % (D / 32)) * 32 + lane;
+            const float* src = w_o + r * kPitch + at_d;
+            float y[2] = {0.f, 0.f};
+#pragma unroll
+            for (int v = 0; v < kWarps; ++v) y[v & 1] += src[v * (kRows * kPitch)];
+            const float2 ml = lane < kWarps ? w_ml[r * kWarps + lane] : make_float2(-INFINITY, 0.f);
+            const float M = warp_max(ml.x), sum = low_lanes_sum<kWarps>(weight(ml.x, M) * ml.y);
+            const float out = (y[0] + y[1]) * (sum == 0.f ? 0.f : 1.f / sum);
+            const float lse = sum == 0.f ? -INFINITY : (M + log2f(sum)) * 0.6931471805599453f;
+            if (!whole) {
+                a.part_O[(part * kRows + r) * D + at_d] = out;
+                if (at_d == 0) a.part_LSE[part * kRows + r] = lse;
+                continue;
+            }
+            const int64_t row = row_of(token0, head0, row0, r, a.g_shift, a.Hq);
+            if (a.out_f32) {
+                static_cast<float*>(a.O)[row * D + at_d] = out;
+            } else {
+                const float z = __shfl_xor_sync(0xffffffffu, out, 1);
+                if ((lane & 1) == 0) *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.O) + row * D + at_d) = pack_bf16x2(out, z);
+            }
+            if (at_d == 0 && a.LSE != nullptr) a.LSE[row] = lse;
+        }
+        // An item that begins here and goes on elsewhere is this CTA's last; the CTAs up to the one with its last piece have a part each.
+        if (p_begin == 0 && p_end < w.pieces) {
+            if (threadIdx.x == 0) {
+                const int64_t last = ((item_at + w.pieces) * n_ctas - 1) / total;         // the last CTA that begins before the item's end
+                a.meta[blockIdx.x] = {static_cast<int>(part), static_cast<int>(last - blockIdx.x) + 1, token0, head0, row0, n_rows};
+            }
+            meta_written = true;
+        }
+        at = item_at + p_end;
+        __syncthreads();                         // the ring is loaded into again
+    }
+    if (!meta_written && threadIdx.x == 0) a.meta[blockIdx.x].parts = 0;
+}
+
+// The parts of an item that several CTAs share: O = sum_j e^{l_j - l} A_j (Appendix H's closed form).  One CTA per item and row; its
+// warps share the parts.
+template <int D>
+__global__ void __launch_bounds__(kThreads)
+paged_merge_kernel(const Meta* __restrict__ meta, const float* __restrict__ part_O, const float* __restrict__ part_LSE, int g_shift, int Hq,
+                   void* O, int out_f32, float* LSE) {
+    constexpr int kPer = D / 32;
+    __shared__ float s_o[kWarps][D];
+    __shared__ float s_m[kWarps], s_l[kWarps];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const Meta x = meta[blockIdx.x];
+    const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (x.parts < 2 || r >= x.rows) return;
+    const auto slot_of = [&](int j) { return j == 0 ? x.first : 2 * (static_cast<int>(blockIdx.x) + j); };
+    float m = -INFINITY;
+    for (int j = threadIdx.x; j < x.parts; j += kThreads) m = fmaxf(m, part_LSE[slot_of(j) * kRows + r]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    if (lane == 0) s_m[warp] = m;
+    __syncthreads();
+    m = s_m[0];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s_m[w]);
+    float acc[kPer] = {}, sum = 0.f;
+    if (m > -INFINITY) {
+#pragma unroll 4
+        for (int j = warp; j < x.parts; j += kWarps) {
+            const int64_t at = static_cast<int64_t>(slot_of(j)) * kRows + r;
+            const float w = ex2((part_LSE[at] - m) * 1.4426950408889634f);
+            sum += w;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) acc[i] = fmaf(w, part_O[at * D + i * 32 + lane], acc[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) s_o[warp][i * 32 + lane] = acc[i];
+    if (lane == 0) s_l[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    float y = 0.f, total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        y += s_o[w][threadIdx.x];
+        total += s_l[w];
+    }
+    y = total > 0.f ? y / total : 0.f;
+    const int64_t row = row_of(x.token0, x.head0, x.row0, r, g_shift, Hq);
+    if (out_f32) static_cast<float*>(O)[row * D + threadIdx.x] = y;
+    else reinterpret_cast<__nv_bfloat16*>(O)[row * D + threadIdx.x] = __float2bfloat16_rn(y);
+    if (threadIdx.x == 0 && LSE != nullptr) LSE[row] = total > 0.f ? m + logf(total) : -INFINITY;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Scores of the full pages and the k best.  Keys are the scores' bit patterns in an order that compares like the numbers.
+// ---------------------------------------------------------------------------------------------
+constexpr uint64_t kForced = ~0ull;
+constexpr int kScorePages = 128;                // pages of a CTA, a thread each
+__device__ __forceinline__ uint64_t order_key(double x) {
+    if (x != x) x = -INFINITY;
+    const uint64_t b = static_cast<uint64_t>(__double_as_longlong(x + 0.0));      // (-0 counts as 0)
+    return b >> 63 ? ~b : b | (1ull << 63);
+}
+
+struct SelectArgs {
+    const uint16_t *Q, *summary;
+    const int32_t *table, *len, *n_draft;
+    int T, Hq, Hkv, g_shift, page_shift, n_pages, max_pages, k, sink, window;
+    uint64_t* keys;                              // [n_slots, T, Hkv, max_pages]
+    int32_t *sel, *list;                         // [n_slots, T, Hkv, k], [n_slots, T, Hkv, k + 1]
+    int32_t* status;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kScorePages)
+page_score_kernel(const __grid_constant__ SelectArgs a) {
+    __shared__ double s_q[4][D];
+    const int slot = blockIdx.z, kvh = blockIdx.y, b = blockIdx.x * kScorePages + threadIdx.x;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int len = checked_len(a.len[slot], static_cast<int64_t>(a.max_pages) << a.page_shift, false, nullptr);
+    const int full = len >> a.page_shift;
+    if (full <= a.k || static_cast<int>(blockIdx.x) * kScorePages >= full) return;      // (all pages are taken as they are)
+    const int n = a.n_draft != nullptr ? min(max(a.n_draft[slot], 0), a.T) : a.T, g = 1 << a.g_shift;
+    const bool forced = b < a.sink || b >= full - a.window;
+    int page = -1;
+    if (b < full) {
+        page = a.table[static_cast<int64_t>(slot) * a.max_pages + b];
+        if (page < 0 || page >= a.n_pages) {
+            report(a.status, PULSAR_DEV_BAD_PAGE);
+            page = -1;
+        }
+    }
+    const uint4* low = reinterpret_cast<const uint4*>(a.summary + (static_cast<int64_t>(max(page, 0)) * a.Hkv + kvh) * 2 * D);
+    const uint4* high = low + D / 8;
+    double best = -INFINITY;
+    for (int r0 = 0; r0 < n * g; r0 += 4) {                             // four query rows (token, head of the group) at a time
+        __syncthreads();
+        for (int i = threadIdx.x; i < 4 * D; i += kScorePages) {
+            const int r = r0 + i / D, j = i % D;
+            double x = 0.0;
+            if (r < n * g)
+                x = static_cast<double>(__uint_as_float(static_cast<uint32_t>(
+                        a.Q[(static_cast<int64_t>(slot * a.T + (r >> a.g_shift)) * a.Hq + (kvh << a.g_shift) + (r & (g - 1))) * D + j]) << 16));
+            s_q[i / D][j] = x;
+        }
+        __syncthreads();
+        double acc[4] = {0.0, 0.0, 0.0, 0.0};
+        if (page >= 0 && !forced) {
+#pragma unroll 2
+            for (int v = 0; v < D / 8; ++v) {
+                const uint4 x = low[v], y = high[v];
+                const uint32_t lo[4] = {x.x, x.y, x.z, x.w}, hi[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const double l = static_cast<double>(__uint_as_float(j & 1 ? lo[j >> 1] & 0xffff0000u : lo[j >> 1] << 16));
+                    const double h = static_cast<double>(__uint_as_float(j & 1 ? hi[j >> 1] & 0xffff0000u : hi[j >> 1] << 16));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const double q = s_q[i][v * 8 + j];
+                        acc[i] = fma(q, q > 0.0 ? h : l, acc[i]);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = r0 + i;
+            if (r >= n * g) break;
+            const double x = acc[i] == acc[i] ? acc[i] : -INFINITY;
+            best = (r & (g - 1)) == 0 ? x : fmax(best, x);
+            if ((r & (g - 1)) == g - 1 && b < full)
+                a.keys[(static_cast<int64_t>(slot * a.T + (r >> a.g_shift)) * a.Hkv + kvh) * a.max_pages + b] =
+                    forced ? kForced : order_key(page >= 0 ? best : -INFINITY);
+        }
+    }
+}
+
+constexpr int kTopThreads = 512, kTopWarps = kTopThreads / 32;
+__global__ void __launch_bounds__(kTopThreads)
+page_select_kernel(const __grid_constant__ SelectArgs a) {
+    __shared__ int s_hist[256], s_gt[kTopWarps], s_eq[kTopWarps];
+    __shared__ int s_bin, s_left;
+    const int row = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const int token0 = row / a.Hkv, slot = token0 / a.T, u = token0 - slot * a.T;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int len = checked_len(a.len[slot], static_cast<int64_t>(a.max_pages) << a.page_shift, false, nullptr);
+    const int full = len >> a.page_shift, k = min(a.k, full);
+    if (a.n_draft != nullptr && u >= a.n_draft[slot]) return;
+    const uint64_t* keys = a.keys + static_cast<int64_t>(row) * a.max_pages;
+    int32_t* sel = a.sel + static_cast<int64_t>(row) * a.k;
+    int32_t* list = a.list + static_cast<int64_t>(row) * (a.k + 1);
+    const int32_t* table = a.table + static_cast<int64_t>(slot) * a.max_pages;
+
+    // ---- the k-th largest key, a byte at a time; `left`: how many of those equal to it are taken ----
+    uint64_t kth = 0, known = 0;                 // known: the bits of kth that are settled
+    int left = k;
+    if (full > a.k) {
+        for (int shift = 56; shift >= 0; shift -= 8) {
+            for (int i = t; i < 256; i += kTopThreads) s_hist[i] = 0;
+            __syncthreads();
+            for (int b = t; b < full; b += kTopThreads) {
+                const uint64_t x = keys[b];
+                if ((x & known) == kth) atomicAdd(&s_hist[(x >> shift) & 255], 1);
+            }
+            __syncthreads();
+            if (warp == 0) {                     // lane i: bins 255 - 8 i .. 248 - 8 i, from the largest down
+                int mine[8], sum = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    mine[i] = s_hist[255 - 8 * lane - i];
+                    sum += mine[i];
+                }
+                int before = sum;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int z = __shfl_up_sync(0xffffffffu, before, d);
+                    if (lane >= d) before += z;
+                }
+                before -= sum;
+                if (before < left && before + sum >= left) {
+                    int i = 0;
+                    while (before + mine[i] < left) before += mine[i++];
+                    s_bin = 255 - 8 * lane - i;
+                    s_left = left - before;
+                }
+            }
+            __syncthreads();
+            kth |= static_cast<uint64_t>(s_bin) << shift;
+            known |= 255ull << shift;
+            left = s_left;
+        }
+    }
+    // ---- pages in ascending order: larger keys, and the first `left` equal ones ----
+    int done = 0, done_eq = 0;
+    for (int b0 = 0; b0 < full; b0 += kTopThreads) {
+        const int b = b0 + t;
+        const uint64_t x = b < full && full > a.k ? keys[b] : 0;
+        const bool gt = b < full && (full <= a.k || x > kth), eq = b < full && full > a.k && x == kth;
+        const uint32_t gts = __ballot_sync(0xffffffffu, gt), eqs = __ballot_sync(0xffffffffu, eq);
+        __syncthreads();
+        if (lane == 0) {
+            s_gt[warp] = __popc(gts);
+            s_eq[warp] = __popc(eqs);
+        }
+        __syncthreads();
+        int n_gt = 0, n_eq = 0, all_gt = 0, all_eq = 0;
+        for (int w = 0; w < kTopWarps; ++w) {
+            if (w < warp) {
+                n_gt += s_gt[w];
+                n_eq += s_eq[w];
+            }
+            all_gt += s_gt[w];
+            all_eq += s_eq[w];
+        }
+        const uint32_t lower = (1u << lane) - 1u;
+        n_gt += __popc(gts & lower);
+        n_eq += __popc(eqs & lower);
+        if (gt || (eq && done_eq + n_eq < left)) {
+            const int at = done + n_gt + min(done_eq + n_eq, left) - min(done_eq, left);
+            sel[at] = b;
+            list[at] = table[b];
+        }
+        done += all_gt + min(done_eq + all_eq, left) - min(done_eq, left);
+        done_eq += all_eq;
+    }
+    for (int i = k + t; i < a.k; i += kTopThreads) sel[i] = -1;
+    if (t == 0 && len > full << a.page_shift) list[k] = table[full];      // the page of the rows after the last full one
+}
+
+// ---------------------------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------------------------
+constexpr int kSmemBytes = kRingBytes + kRows * kWarps * 8 + kMaxTree * 8 + (kMaxSlots + 1) * 8 + kWarps * 8 + kMaxTree * 4;
+
+bool heads_ok(int32_t Hq, int32_t Hkv) {
+    if (Hkv < 1 || Hq < Hkv || Hq % Hkv != 0) return false;
+    const int g = Hq / Hkv;
+    return g == 1 || g == 2 || g == 4 || g == 8 || g == 16;
+}
+
+// Scratch of an attention launch: what its CTAs leave for the merge.
+struct Scratch {
+    size_t meta, part_O, part_LSE, total;
+    Scratch(int d, size_t at) {
+        const size_t ctas = 2 * static_cast<size_t>(sm_count());
+        meta = at;
+        part_LSE = round_up(meta + ctas * sizeof(Meta), 256);
+        part_O = round_up(part_LSE + 2 * ctas * kRows * 4, 256);
+        total = round_up(part_O + 2 * ctas * kRows * d * 4, 256);
+    }
+};
+
+template <typename Kernel>
+int32_t launch_rows(Kernel kernel, const PagedArgs& a, int d, cudaStream_t st) {
+    const unsigned ctas = 2 * static_cast<unsigned>(sm_count());
+    PULSAR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes));
+    PULSAR_CUDA_OK(launch_kernel(kernel, dim3(ctas), dim3(kThreads), kSmemBytes, st, true, a));
+    count_launch();
+    const auto merge = d == 128 ? paged_merge_kernel<128> : paged_merge_kernel<64>;
+    PULSAR_CUDA_OK(launch_kernel(merge, dim3(ctas, kRows), dim3(kThreads), 0, st, true, a.meta, a.part_O, a.part_LSE, a.g_shift, a.Hq, a.O,
+                                 a.out_f32, a.LSE));
+    count_launch();
+    return PULSAR_OK;
+}
+
+float scale_log2(float softmax_scale, int32_t d) {
+    return (softmax_scale > 0.f ? softmax_scale : 1.f / sqrtf(static_cast<float>(d))) * 1.4426950408889634f;
+}
+
+}  // namespace
+}  // namespace pulsar
+
+using namespace pulsar;
+
+extern "C" size_t pulsar_tree_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t Hq, int32_t Hkv, int32_t d) {
+    if (n_slots < 1 || n_slots > kMaxSlots || T < 1 || T > kMaxTree || !heads_ok(Hq, Hkv) || (d != 64 && d != 128)) return 0;
+    return Scratch(d, 0).total;
+}
+
+extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, const uint16_t* Vnew, int32_t T, uint16_t* K_pages,
+                                    uint16_t* V_pages, int32_t n_pages, int32_t page_size, const int32_t* page_table,
+                                    const int32_t* cache_len, int32_t n_slots, int32_t max_pages, const int32_t* parent,
+                                    const int32_t* n_draft, int32_t Hq, int32_t Hkv, int32_t d, float softmax_scale, void* O,
+                                    int32_t out_is_f32, float* LSE, void* workspace, size_t workspace_bytes, int32_t* device_status,
+                                    void* stream) {
+    if (!pool_ok(1, n_pages, page_size, Hkv, d, n_slots, max_pages) || !heads_ok(Hq, Hkv) || T < 1 || T > kMaxTree) return PULSAR_ERR_SHAPE;
+    if (Q == nullptr || Knew == nullptr || Vnew == nullptr || K_pages == nullptr || V_pages == nullptr || page_table == nullptr ||
+        cache_len == nullptr || O == nullptr || workspace == nullptr)
+        return PULSAR_ERR_INVALID_ARG;
+    for (const void* p : {static_cast<const void*>(Q), static_cast<const void*>(Knew), static_cast<const void*>(Vnew),
+                          static_cast<const void*>(K_pages), static_cast<const void*>(V_pages), static_cast<const void*>(O)})
+        if (!aligned(p, 16)) return PULSAR_ERR_ALIGNMENT;
+    if (!aligned(page_table, 4) || !aligned(cache_len, 4) || !aligned(parent, 4) || !aligned(n_draft, 4) || !aligned(LSE, 4) ||
+        !aligned(workspace, 256))
+        return PULSAR_ERR_ALIGNMENT;
+    const Scratch z(d, 0);
+    if (workspace_bytes < z.total) return PULSAR_ERR_WORKSPACE;
+    if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
+    auto* ws = static_cast<uint8_t*>(workspace);
+    PagedArgs a{};
+    a.Q = Q;
+    a.Knew = Knew;
+    a.Vnew = Vnew;
+    a.K = K_pages;
+    a.V = V_pages;
+    a.table = page_table;
+    a.len = cache_len;
+    a.n_draft = n_draft;
+    a.parent = parent;
+    a.n_slots = n_slots;
+    a.T = T;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.g_shift = log2_exact(Hq / Hkv);
+    a.page_shift = log2_exact(page_size);
+    a.n_pages = n_pages;
+    a.max_pages = max_pages;
+    a.scale_log2 = scale_log2(softmax_scale, d);
+    a.O = O;
+    a.out_f32 = out_is_f32;
+    a.LSE = LSE;
+    a.meta = reinterpret_cast<Meta*>(ws + z.meta);
+    a.part_O = reinterpret_cast<float*>(ws + z.part_O);
+    a.part_LSE = reinterpret_cast<float*>(ws + z.part_LSE);
+    a.status = device_status;
+    return launch_rows(d == 128 ? paged_rows_kernel<128, false> : paged_rows_kernel<64, false>, a, d, static_cast<cudaStream_t>(stream));
+}
+
+namespace {
+struct SparseScratch {
+    size_t keys, list, total;
+    SparseScratch(int64_t rows, int64_t max_pages, int64_t k, int d) {
+        keys = Scratch(d, 0).total;
+        list = round_up(keys + static_cast<size_t>(rows * max_pages) * 8, 256);
+        total = round_up(list + static_cast<size_t>(rows * (k + 1)) * 4, 256);
+    }
+};
+bool sparse_ok(int32_t n_slots, int32_t T, int32_t k, int32_t Hq, int32_t Hkv, int32_t d) {
+    return n_slots >= 1 && n_slots <= kMaxSlots && T >= 1 && T <= kMaxTree && heads_ok(Hq, Hkv) && Hkv <= 1024 && (d == 64 || d == 128) &&
+           k >= 1 && k <= 65536 && static_cast<int64_t>(n_slots) * T * Hkv <= (1 << 20);
+}
+}  // namespace
+
+extern "C" size_t pulsar_sparse_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t max_pages, int32_t k, int32_t Hq, int32_t Hkv,
+                                                     int32_t d) {
+    if (!sparse_ok(n_slots, T, k, Hq, Hkv, d) || max_pages < 1) return 0;
+    return SparseScratch(static_cast<int64_t>(n_slots) * T * Hkv, max_pages, k, d).total;
+}
+
+extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, const uint16_t* Vnew, int32_t T, uint16_t* K_pages,
+                                      uint16_t* V_pages, const uint16_t* summary, int32_t n_pages, int32_t page_size,
+                                      const int32_t* page_table, const int32_t* cache_len, int32_t n_slots, int32_t max_pages,
+                                      const int32_t* n_draft, int32_t k, int32_t sink, int32_t window, int32_t Hq, int32_t Hkv, int32_t d,
+                                      float softmax_scale, uint16_t* O, float* LSE, int32_t* sel, void* workspace,
+                                      size_t workspace_bytes, int32_t* device_status, void* stream) {
+    if (!pool_ok(1, n_pages, page_size, Hkv, d, n_slots, max_pages) || !sparse_ok(n_slots, T, k, Hq, Hkv, d) || sink < 0 || window < 0 ||
+        static_cast<int64_t>(sink) + window > k)
+        return PULSAR_ERR_SHAPE;
+    if (Q == nullptr || Knew == nullptr || Vnew == nullptr || K_pages == nullptr || V_pages == nullptr || summary == nullptr ||
+        page_table == nullptr || cache_len == nullptr || O == nullptr || sel == nullptr || workspace == nullptr)
+        return PULSAR_ERR_INVALID_ARG;
+    for (const void* p : {static_cast<const void*>(Q), static_cast<const void*>(Knew), static_cast<const void*>(Vnew), static_cast<const void*>(summary),
+                          static_cast<const void*>(K_pages), static_cast<const void*>(V_pages), static_cast<const void*>(O)})
+        if (!aligned(p, 16)) return PULSAR_ERR_ALIGNMENT;
+    if (!aligned(page_table, 4) || !aligned(cache_len, 4) || !aligned(n_draft, 4) || !aligned(LSE, 4) || !aligned(sel, 4) || !aligned(workspace, 256))
+        return PULSAR_ERR_ALIGNMENT;
+    const int64_t rows = static_cast<int64_t>(n_slots) * T * Hkv;
+    const Scratch z(d, 0);
+    const SparseScratch y(rows, max_pages, k, d);
+    if (workspace_bytes < y.total) return PULSAR_ERR_WORKSPACE;
+    if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
+    auto* ws = static_cast<uint8_t*>(workspace);
+    auto st = static_cast<cudaStream_t>(stream);
+
+    SelectArgs b{};
+    b.Q = Q;
+    b.summary = summary;
+    b.table = page_table;
+    b.len = cache_len;
+    b.n_draft = n_draft;
+    b.T = T;
+    b.Hq = Hq;
+    b.Hkv = Hkv;
+    b.g_shift = log2_exact(Hq / Hkv);
+    b.page_shift = log2_exact(page_size);
+    b.n_pages = n_pages;
+    b.max_pages = max_pages;
+    b.k = k;
+    b.sink = sink;
+    b.window = window;
+    b.keys = reinterpret_cast<uint64_t*>(ws + y.keys);
+    b.sel = sel;
+    b.list = reinterpret_cast<int32_t*>(ws + y.list);
+    b.status = device_status;
+    PULSAR_CUDA_OK(launch_kernel(d == 128 ? page_score_kernel<128> : page_score_kernel<64>,
+                                 dim3((max_pages + kScorePages - 1) / kScorePages, Hkv, n_slots), dim3(kScorePages), 0, st, true, b));
+    count_launch();
+    PULSAR_CUDA_OK(launch_kernel(page_select_kernel, dim3(static_cast<unsigned>(rows)), dim3(kTopThreads), 0, st, true, b));
+    count_launch();
+
+    PagedArgs a{};
+    a.Q = Q;
+    a.Knew = Knew;
+    a.Vnew = Vnew;
+    a.K = K_pages;
+    a.V = V_pages;
+    a.table = page_table;
+    a.len = cache_len;
+    a.n_draft = n_draft;
+    a.list = b.list;
+    a.n_slots = n_slots;
+    a.T = T;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.g_shift = b.g_shift;
+    a.page_shift = b.page_shift;
+    a.n_pages = n_pages;
+    a.max_pages = max_pages;
+    a.k = k;
+    a.scale_log2 = scale_log2(softmax_scale, d);
+    a.O = O;
+    a.LSE = LSE;
+    a.meta = reinterpret_cast<Meta*>(ws + z.meta);
+    a.part_O = reinterpret_cast<float*>(ws + z.part_O);
+    a.part_LSE = reinterpret_cast<float*>(ws + z.part_LSE);
+    a.status = device_status;
+    return launch_rows(d == 128 ? paged_rows_kernel<128, true> : paged_rows_kernel<64, true>, a, d, st);
+}

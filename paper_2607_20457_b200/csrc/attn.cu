@@ -21,10 +21,9 @@
 #include <functional>
 #include <type_traits>
 
-#include <cuda.h>
-
 #include "common.cuh"
 #include "decode.cuh"
+#include "tensor_map.cuh"
 
 namespace pulsar {
 
@@ -1282,7 +1281,9 @@ EncodeTiledFn encode_fn() {
     return fn;
 }
 
-// [rows, heads, d] bf16 viewed as (d, heads, rows); box = (64, box_heads, box_rows), 128-byte swizzle.
+}  // namespace
+
+// (declared in tensor_map.cuh)
 bool make_map_3d(CUtensorMap* m, const void* base, int64_t rows, int heads, int d, int box_heads, int box_rows) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
@@ -1294,6 +1295,8 @@ bool make_map_3d(CUtensorMap* m, const void* base, int64_t rows, int heads, int 
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+namespace {
 
 // [rows, width] bf16; box = (64, 128), 128-byte swizzle.
 bool make_map_2d(CUtensorMap* m, const void* base, int64_t rows, int64_t width) {

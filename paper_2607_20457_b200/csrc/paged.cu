@@ -20,54 +20,7 @@ constexpr int kRows = 8;                        // query rows of an item: the co
 constexpr int kUnitBytes = 4096;
 constexpr int kUnits = 3;                       // of a warp's ring: one in use, two on their way
 constexpr int kRingBytes = kWarps * kUnits * kUnitBytes;
-constexpr int kMaxSlots = 1024, kMaxTree = 64;
 constexpr int kLeastPieces = 3 * kWarps;        // of a CTA: three per warp, unless all CTAs have fewer
-
-struct Meta {                                   // the item that begins in a CTA and goes on in the next ones
-    int first, parts;                           // first partial (those of the CTAs after it are their first ones); 0: there is none
-    int token0, head0, row0, rows;              // of its rows: see row_of
-};
-
-struct PagedArgs {
-    const uint16_t *Q, *Knew, *Vnew;             // [n_slots, T, Hq | Hkv, D]
-    uint16_t *K, *V;                             // [n_pages, page_size, Hkv, D]
-    const int32_t *table, *len, *n_draft, *parent;
-    const int32_t* list;                         // selected pages: [n_slots, T, Hkv, k + 1] page ids, the last row's page among them
-    int n_slots, T, Hq, Hkv, g_shift, page_shift, n_pages, max_pages, k;
-    float scale_log2;
-    void* O;
-    int out_f32;
-    float* LSE;
-    float *part_O, *part_LSE;                    // [2 * CTAs, kRows, D], [2 * CTAs, kRows]
-    Meta* meta;                                  // [CTAs]
-    int32_t* status;
-};
-
-// Bookkeeping of a slot, the same in every CTA.
-struct SlotWork {
-    int len, n;                                  // rows in the cache; new tokens
-    int keys;                                    // cached rows an item reads
-    int cache_pieces, pieces, items;
-};
-template <bool kSparse, int kKeys>
-__device__ __forceinline__ SlotWork slot_work(const PagedArgs& a, int slot, bool tell) {
-    SlotWork w;
-    w.len = checked_len(a.len[slot], static_cast<int64_t>(a.max_pages) << a.page_shift, tell, a.status);
-    w.n = a.n_draft != nullptr ? min(max(a.n_draft[slot], 0), a.T) : a.T;
-    const int full = w.len >> a.page_shift;
-    w.keys = kSparse ? (min(a.k, full) << a.page_shift) + (w.len - (full << a.page_shift)) : w.len;
-    w.cache_pieces = (w.keys + kKeys - 1) / kKeys;
-    w.pieces = w.cache_pieces + (w.n + kKeys - 1) / kKeys;
-    const int g = 1 << a.g_shift;
-    w.items = kSparse ? w.n * a.Hkv * ((g + kRows - 1) / kRows) : a.Hkv * ((w.n * g + kRows - 1) / kRows);
-    return w;
-}
-
-// Row r of an item: token token0 + r' / g and head head0 + r' % g, with r' = row0 + r.
-__device__ __forceinline__ int64_t row_of(int token0, int head0, int row0, int r, int g_shift, int Hq) {
-    const int x = row0 + r;
-    return static_cast<int64_t>(token0 + (x >> g_shift)) * Hq + head0 + (x & ((1 << g_shift) - 1));
-}
 
 // Two CTAs per SM: while the keys of one are on their way, the other computes.
 template <int D, bool kSparse>
@@ -93,55 +46,19 @@ paged_rows_kernel(const __grid_constant__ PagedArgs a) {
     grid_dependency_wait();
     grid_launch_dependents();
 
-    // ---- all pieces of all slots, and this CTA's share ----
-    int64_t total = 0;
-    for (int s0 = 0; s0 < a.n_slots; s0 += kThreads) {
-        const int s = s0 + threadIdx.x;
-        int64_t x = 0;
-        if (s < a.n_slots) {
-            const SlotWork w = slot_work<kSparse, kKeys>(a, s, blockIdx.x == 0);
-            x = static_cast<int64_t>(w.pieces) * w.items;
-        }
-        int64_t y = x;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int64_t z = __shfl_up_sync(0xffffffffu, y, d);
-            if (lane >= d) y += z;
-        }
-        if (lane == 31) s_warp[warp] = y;
-        __syncthreads();
-        int64_t before = total;
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) before += s_warp[w];
-            total += s_warp[w];
-        }
-        if (s < a.n_slots) s_pieces[s] = before + y - x;
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) s_pieces[a.n_slots] = total;
-    __syncthreads();
-    const int64_t n_ctas = max(static_cast<int64_t>(1), min(static_cast<int64_t>(gridDim.x), total / kLeastPieces));
-    const int64_t begin = blockIdx.x < n_ctas ? total * blockIdx.x / n_ctas : total;
-    const int64_t end = blockIdx.x < n_ctas ? total * (blockIdx.x + 1) / n_ctas : total;
+    // ---- this CTA's share of all pieces of all slots ----
+    const Share share = share_of(all_pieces<kSparse, kKeys, kRows, kThreads>(a, s_pieces, s_warp), kLeastPieces);
+    const int64_t begin = share.begin, end = share.end;
     if (begin >= end) {
         if (threadIdx.x == 0) a.meta[blockIdx.x].parts = 0;
         return;
     }
-    int slot = 0;
-    {
-        int hi = a.n_slots - 1;                                // the last slot that begins at or before this CTA's first piece
-        while (slot < hi) {
-            const int mid = (slot + hi + 1) >> 1;
-            if (s_pieces[mid] <= begin) slot = mid;
-            else hi = mid - 1;
-        }
-    }
+    int slot_now = slot_at(s_pieces, a.n_slots, begin);
 
     const uint32_t ring = smem_u32(smem) + warp * (kUnits * kUnitBytes);
     const int copy_row = lane / kVecs, copy_vec = lane % kVecs;
     const int64_t pitch = static_cast<int64_t>(a.Hkv) * D;     // elements between the rows of a head
     const int page_mask = (1 << a.page_shift) - 1;
-    const int g = 1 << a.g_shift;
     const int mi = lane >> 3, l8 = lane & 7;
     const uint32_t k_lane = ring + ((mi & 1) * 8 + l8) * (D * 2), k_x = ((mi >> 1) ^ l8) << 4;     // K: rows are keys
     const uint32_t v_lane = ring + ((mi >> 1) * 8 + l8) * (D * 2), v_x = ((mi & 1) ^ l8) << 4;     // V: read transposed
@@ -149,16 +66,10 @@ paged_rows_kernel(const __grid_constant__ PagedArgs a) {
 
     for (int64_t at = begin; at < end;) {
         // ---- the next item and this CTA's pieces of it ----
-        while (s_pieces[slot + 1] <= at) ++slot;
-        const SlotWork w = slot_work<kSparse, kKeys>(a, slot, false);
-        const int item = static_cast<int>((at - s_pieces[slot]) / w.pieces);
-        const int64_t item_at = s_pieces[slot] + static_cast<int64_t>(item) * w.pieces;
-        const int p_begin = static_cast<int>(at - item_at), p_end = static_cast<int>(min(end - item_at, static_cast<int64_t>(w.pieces)));
-        const int row_blocks = kSparse ? (g + kRows - 1) / kRows : (w.n * g + kRows - 1) / kRows;
-        const int row0 = (item % row_blocks) * kRows, unit = item / row_blocks;      // unit: KV head, or token and KV head
-        const int kvh = kSparse ? unit % a.Hkv : unit, token = kSparse ? unit / a.Hkv : 0;
-        const int n_rows = min(kRows, (kSparse ? g : w.n * g) - row0);
-        const int token0 = slot * a.T + token, head0 = kvh << a.g_shift;
+        const Segment seg = segment_at<kSparse, kKeys, kRows>(a, s_pieces, at, end, slot_now);
+        const SlotWork& w = seg.w;
+        const int slot = seg.slot, p_begin = seg.p_begin, p_end = seg.p_end, row0 = seg.row0, n_rows = seg.n_rows, kvh = seg.kvh;
+        const int token = seg.token, token0 = seg.token0, head0 = seg.head0;
         const bool appends = row0 == 0 && token == 0;
         const int head_at = kvh * D + copy_vec * 8;
         const int32_t* list = kSparse ? a.list + (static_cast<int64_t>(token0) * a.Hkv + kvh) * (a.k + 1)
@@ -220,35 +131,10 @@ paged_rows_kernel(const __grid_constant__ PagedArgs a) {
         load(a.K, fresh_k, now_ids, now_ok, p_first, 0);
         load(a.V, fresh_v, now_ids, now_ok, p_first, 1);
 
-        // ---- which nodes a node sees: pointers to ancestors are doubled ----
+        // ---- which nodes a node sees ----
         const bool has_new = p_end > w.cache_pieces;
-        if (!kSparse && has_new && a.parent != nullptr) {
-            const int t = threadIdx.x;
-            int up = -1;
-            if (t < w.n) {
-                up = a.parent[static_cast<int64_t>(slot) * a.T + t];
-                if (up < -1 || up >= t) {
-                    report(a.status, PULSAR_DEV_BAD_TREE);
-                    up = -1;
-                }
-            }
-            uint64_t sees = t < kMaxTree ? 1ull << t : 0ull;
-#pragma unroll 1
-            for (int step = 1; step < kMaxTree; step <<= 1) {
-                if (t < kMaxTree) {
-                    s_sees[t] = sees;
-                    s_up[t] = up;
-                }
-                __syncthreads();
-                if (t < kMaxTree && up >= 0) {
-                    sees |= s_sees[up];
-                    up = s_up[up];
-                }
-                __syncthreads();
-            }
-            if (t < kMaxTree) s_sees[t] = sees;
-            __syncthreads();
-        }
+        if (!kSparse && has_new && a.parent != nullptr)
+            ancestors(a, slot, w.n, threadIdx.x, s_sees, s_up, [] { __syncthreads(); });
         uint64_t sees[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -410,17 +296,9 @@ paged_rows_kernel(const __grid_constant__ PagedArgs a) {
                 for (int i = 0; i < kCopies; ++i) {
                     const int row = (p - w.cache_pieces) * kKeys + i * kRowsPerCopy + copy_row;
                     if (row >= w.n) continue;
-                    const int64_t to_row = static_cast<int64_t>(w.len) + row;
-                    if ((to_row >> a.page_shift) >= a.max_pages) {
-                        report(a.status, PULSAR_DEV_BAD_LENGTH);
-                        continue;
-                    }
-                    const int page = a.table[static_cast<int64_t>(slot) * a.max_pages + (to_row >> a.page_shift)];
-                    if (page < 0 || page >= a.n_pages) {
-                        report(a.status, PULSAR_DEV_BAD_PAGE);
-                        continue;
-                    }
-                    const int64_t to = ((static_cast<int64_t>(page) << a.page_shift) + (to_row & page_mask)) * pitch + head_at;
+                    int64_t to = new_row_at(a, slot, static_cast<int64_t>(w.len) + row, pitch);
+                    if (to < 0) continue;
+                    to += head_at;
                     *reinterpret_cast<uint4*>(a.K + to) = *reinterpret_cast<const uint4*>(fresh_k + row * pitch);
                     *reinterpret_cast<uint4*>(a.V + to) = *reinterpret_cast<const uint4*>(fresh_v + row * pitch);
                 }
@@ -490,12 +368,12 @@ paged_rows_kernel(const __grid_constant__ PagedArgs a) {
         // An item that begins here and goes on elsewhere is this CTA's last; the CTAs up to the one with its last piece have a part each.
         if (p_begin == 0 && p_end < w.pieces) {
             if (threadIdx.x == 0) {
-                const int64_t last = ((item_at + w.pieces) * n_ctas - 1) / total;         // the last CTA that begins before the item's end
+                const int64_t last = ((seg.item_at + w.pieces) * share.n_ctas - 1) / share.total;         // the last CTA that begins before the item's end
                 a.meta[blockIdx.x] = {static_cast<int>(part), static_cast<int>(last - blockIdx.x) + 1, token0, head0, row0, n_rows};
             }
             meta_written = true;
         }
-        at = item_at + p_end;
+        at = seg.item_at + p_end;
         __syncthreads();                         // the ring is loaded into again
     }
     if (!meta_written && threadIdx.x == 0) a.meta[blockIdx.x].parts = 0;
@@ -743,17 +621,7 @@ bool heads_ok(int32_t Hq, int32_t Hkv) {
     return g == 1 || g == 2 || g == 4 || g == 8 || g == 16;
 }
 
-// Scratch of an attention launch: what its CTAs leave for the merge.
-struct Scratch {
-    size_t meta, part_O, part_LSE, total;
-    Scratch(int d, size_t at) {
-        const size_t ctas = 2 * static_cast<size_t>(sm_count());
-        meta = at;
-        part_LSE = round_up(meta + ctas * sizeof(Meta), 256);
-        part_O = round_up(part_LSE + 2 * ctas * kRows * 4, 256);
-        total = round_up(part_O + 2 * ctas * kRows * d * 4, 256);
-    }
-};
+PartScratch rows_scratch(int d) { return PartScratch(2 * static_cast<size_t>(sm_count()), kRows, d); }
 
 template <typename Kernel>
 int32_t launch_rows(Kernel kernel, const PagedArgs& a, int d, cudaStream_t st) {
@@ -779,7 +647,8 @@ using namespace pulsar;
 
 extern "C" size_t pulsar_tree_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t Hq, int32_t Hkv, int32_t d) {
     if (n_slots < 1 || n_slots > kMaxSlots || T < 1 || T > kMaxTree || !heads_ok(Hq, Hkv) || (d != 64 && d != 128)) return 0;
-    return Scratch(d, 0).total;
+    const int rows = T * (Hq / Hkv);
+    return rows > kRows ? tree_tiles_workspace_bytes(rows, d) : rows_scratch(d).total;
 }
 
 extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, const uint16_t* Vnew, int32_t T, uint16_t* K_pages,
@@ -798,10 +667,8 @@ extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, con
     if (!aligned(page_table, 4) || !aligned(cache_len, 4) || !aligned(parent, 4) || !aligned(n_draft, 4) || !aligned(LSE, 4) ||
         !aligned(workspace, 256))
         return PULSAR_ERR_ALIGNMENT;
-    const Scratch z(d, 0);
-    if (workspace_bytes < z.total) return PULSAR_ERR_WORKSPACE;
+    if (workspace_bytes < pulsar_tree_attn_workspace_bytes(n_slots, T, Hq, Hkv, d)) return PULSAR_ERR_WORKSPACE;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
-    auto* ws = static_cast<uint8_t*>(workspace);
     PagedArgs a{};
     a.Q = Q;
     a.Knew = Knew;
@@ -824,10 +691,10 @@ extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, con
     a.O = O;
     a.out_f32 = out_is_f32;
     a.LSE = LSE;
-    a.meta = reinterpret_cast<Meta*>(ws + z.meta);
-    a.part_O = reinterpret_cast<float*>(ws + z.part_O);
-    a.part_LSE = reinterpret_cast<float*>(ws + z.part_LSE);
     a.status = device_status;
+    const int rows = T * (Hq / Hkv);
+    if (rows > kRows) return launch_tree_tiles(a, rows, d, workspace, static_cast<cudaStream_t>(stream));
+    rows_scratch(d).place(a, workspace);
     return launch_rows(d == 128 ? paged_rows_kernel<128, false> : paged_rows_kernel<64, false>, a, d, static_cast<cudaStream_t>(stream));
 }
 
@@ -835,7 +702,7 @@ namespace {
 struct SparseScratch {
     size_t keys, list, total;
     SparseScratch(int64_t rows, int64_t max_pages, int64_t k, int d) {
-        keys = Scratch(d, 0).total;
+        keys = rows_scratch(d).total;
         list = round_up(keys + static_cast<size_t>(rows * max_pages) * 8, 256);
         total = round_up(list + static_cast<size_t>(rows * (k + 1)) * 4, 256);
     }
@@ -870,7 +737,6 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
     if (!aligned(page_table, 4) || !aligned(cache_len, 4) || !aligned(n_draft, 4) || !aligned(LSE, 4) || !aligned(sel, 4) || !aligned(workspace, 256))
         return PULSAR_ERR_ALIGNMENT;
     const int64_t rows = static_cast<int64_t>(n_slots) * T * Hkv;
-    const Scratch z(d, 0);
     const SparseScratch y(rows, max_pages, k, d);
     if (workspace_bytes < y.total) return PULSAR_ERR_WORKSPACE;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
@@ -925,9 +791,7 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
     a.scale_log2 = scale_log2(softmax_scale, d);
     a.O = O;
     a.LSE = LSE;
-    a.meta = reinterpret_cast<Meta*>(ws + z.meta);
-    a.part_O = reinterpret_cast<float*>(ws + z.part_O);
-    a.part_LSE = reinterpret_cast<float*>(ws + z.part_LSE);
     a.status = device_status;
+    rows_scratch(d).place(a, ws);
     return launch_rows(d == 128 ? paged_rows_kernel<128, true> : paged_rows_kernel<64, true>, a, d, st);
 }

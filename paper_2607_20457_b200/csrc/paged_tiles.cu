@@ -1,0 +1,686 @@
+// Attention of drafted trees with more than eight query rows per KV head, on the tensor cores (tcgen05).
+//
+// S^T = K Q^T: the 128 keys of a tile stand in the rows (TMEM lanes) and the query rows -- nodes x heads of the group, 16 to 128 --
+// in the columns, so that the products cost what the rows need and every softmax thread has one key.  O^T += V^T P^T takes the V
+// tile as it lies in memory (d contiguous) as its first operand and P^T from shared memory.
+//
+//   warp 0      loader: pages of K and V by TMA into a ring of tiles, the nodes' own rows as the last tile of an item
+//   warp 1      issues the matrix instructions: S of the next tile before PV of this one
+//   warps 2-3   query rows into shared memory, ancestors of the nodes, the nodes' rows to their pages
+//   warps 4-..  softmax: a thread per key and 64 columns (or all, if fewer); epilogue: a thread per output component
+//
+// A column's maximum lies across lanes, so it is not formed for every tile: P is formed with the largest logit seen when it was
+// last moved, and moved (and O^T and the sums rescaled) when a logit exceeds it by more than 2^8.  P, O^T and the sums use the same
+// stale maximum, so the result is unchanged.  The sums stay with their keys' threads until an item ends.
+#include <algorithm>
+
+#include "mma.cuh"
+#include "paged.cuh"
+#include "tensor_map.cuh"
+
+namespace pulsar {
+
+namespace {
+
+constexpr int kTile = 128;                       // keys
+constexpr int kPanelBytes = kTile * 128;         // 64 columns of a tile: 128-byte lines, swizzled
+constexpr int kFreshRows = 64;                   // rows of the nodes' own tile that are loaded
+constexpr float kRescale = 8.f;                  // in log2 units
+constexpr float kUnset = 1e30f;                  // stands for minus a maximum that no logit has set: every logit exceeds it
+constexpr int kLeastTiles = 2;                   // of a CTA, unless all CTAs have fewer
+constexpr int kSeesBuffers = 4;                  // see the loader of query rows
+
+template <int D, int N>
+struct Cfg {
+    static constexpr int kPanels = D / 64;
+    static constexpr int kTileBytes = kPanels * kPanelBytes;
+    static constexpr int kCols = N < 64 ? N : 64;                // columns of a softmax thread
+    static constexpr int kGroups = N / kCols;                    // softmax warpgroups
+    static constexpr int kSoftWarps = 4 * kGroups;
+    static constexpr int kThreads = 128 + 128 * kGroups;
+    static constexpr int kPBytes = (N + 63) / 64 * kPanelBytes;
+    static constexpr int kQBytes = kPanels * N * 128;
+    static constexpr int kMisc = (kMaxSlots + 2) * 8 + kThreads / 32 * 8 + kSeesBuffers * (kMaxTree * 8 + 8) + 64 * 8 + 7 * N * 4 + kMaxTree * 4 + 8;
+    static constexpr int kFit = (232448 - kPBytes - kQBytes - kMisc) / kTileBytes;
+    static constexpr int kStages = kFit < 10 ? kFit : 10;
+    // The product with V reads 128 components; with d = 64 the second half is whatever follows the tile (and is not used), so
+    // something has to follow the last tile of the ring: P does.
+    static constexpr int kP = kStages * kTileBytes;
+    static constexpr int kQ = kP + kPBytes;
+    static constexpr int kRest = kQ + kQBytes;
+    static constexpr int kSmem = kRest + kMisc;
+    static constexpr int kTmemCols = 3 * N <= 32 ? 32 : 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 3 * N <= 256 ? 256 : 512;
+    // barriers
+    static constexpr int bKvFull = 0, bKvEmpty = kStages, bQFull = 2 * kStages, bQEmpty = bQFull + 1, bSFull = bQEmpty + 1, bSEmpty = bSFull + 2,
+                         bPFull = bSEmpty + 2, bPEmpty = bPFull + 1, bOFull = bPEmpty + 1, bOEmpty = bOFull + 1, kBars = bOEmpty + 1;
+    static_assert(kBars <= 64 && kStages >= 3, "");
+};
+
+// Barriers of some warps (whole ones: their lanes come together first).
+__device__ __forceinline__ void named_sync(int id, int threads) {
+    __syncwarp();
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+// Whether any of the barrier's threads says so; the threads wait for each other.
+__device__ __forceinline__ bool named_any(int id, int threads, bool x) {
+    uint32_t y;
+    __syncwarp();
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 q, %1, 0;\n\t"
+        "bar.red.or.pred p, %2, %3, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(y) : "r"(x ? 1u : 0u), "r"(id), "r"(threads) : "memory");
+    return y != 0;
+}
+__device__ __forceinline__ void arrive_a(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+// Columns [0, C) of TMEM, 32 lanes per warp.
+template <int C>
+__device__ __forceinline__ void load_columns(uint32_t taddr, float (&x)[C]) {
+    if constexpr (C == 16) {
+        uint32_t r[16];
+        tmem_ld16(taddr, r);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r[i]);
+    } else {
+        uint32_t r[C];
+        PULSAR_TMEM_LD32_AT(taddr, r, 0);
+        if constexpr (C == 64) PULSAR_TMEM_LD32_AT(taddr + 32, r, 32);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[i] = __uint_as_float(r[i]);
+    }
+}
+
+// Column sums over a warp's lanes: lane l ends with those of columns [l * C / 32, ...) (C = 16: lanes 2 c and 2 c + 1 with column c).
+// Every step hands half of the columns to the other half of the lanes.
+template <int C>
+__device__ __forceinline__ void column_sums(float (&x)[C], int lane) {
+    int n = C;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        if (n > 1) {
+            n >>= 1;
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i)
+                if (i < n) {
+                    const bool upper = (lane & off) != 0;
+                    const float keep = upper ? x[i + n] : x[i], give = upper ? x[i] : x[i + n];
+                    x[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
+                }
+        } else {
+            x[0] += __shfl_xor_sync(0xffffffffu, x[0], off);
+        }
+    }
+}
+
+template <int D, int N>
+__global__ void __launch_bounds__(Cfg<D, N>::kThreads, 1)
+tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                  const __grid_constant__ CUtensorMap tmKn, const __grid_constant__ CUtensorMap tmVn) {
+    using C = Cfg<D, N>;
+    constexpr int kCols = C::kCols;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint8_t* rest = smem + C::kRest;
+    int64_t* s_pieces = reinterpret_cast<int64_t*>(rest);                              // [n_slots + 1]
+    int64_t* s_warp = s_pieces + kMaxSlots + 2;                                        // (what float4 reads stays on 16 bytes)
+    uint64_t* s_sees = reinterpret_cast<uint64_t*>(s_warp + C::kThreads / 32);         // [kSeesBuffers][kMaxTree]
+    uint64_t* bars = s_sees + kSeesBuffers * kMaxTree;                                 // [64]
+    float* s_col = reinterpret_cast<float*>(bars + 64);                                // [4][N] of each warp's keys: largest logits, sums
+    float* s_neg = s_col + 4 * N;                                                      // [N] minus the maximum in use
+    float* s_alpha = s_neg + N;                                                        // [N] rescaling factors
+    float* s_inv = s_alpha + N;                                                        // [N] 1 / sum
+    int* s_up = reinterpret_cast<int*>(s_inv + N);                                     // [kMaxTree]
+    uint32_t* s_odd = reinterpret_cast<uint32_t*>(s_up + kMaxTree);                    // [kSeesBuffers][2] nodes whose value is not finite
+    uint32_t* tmem_ptr = s_odd + 2 * kSeesBuffers;
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_ptr + 1);
+
+    const int lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
+    const uint32_t bar0 = smem_u32(bars);
+    const auto bar = [&](int i) { return bar0 + 8 * static_cast<uint32_t>(i); };
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(bars + C::bKvFull + i, 1);
+            mbar_init(bars + C::bKvEmpty + i, 1);
+        }
+        mbar_init(bars + C::bQFull, 1);
+        mbar_init(bars + C::bQEmpty, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bars + C::bSFull + i, 1);
+            mbar_init(bars + C::bSEmpty + i, C::kSoftWarps);
+        }
+        mbar_init(bars + C::bPFull, C::kSoftWarps);
+        mbar_init(bars + C::bPEmpty, 1);
+        mbar_init(bars + C::bOFull, 1);
+        mbar_init(bars + C::bOEmpty, C::kSoftWarps);
+        mbar_fence_init();
+        tma_prefetch_desc(&tmK);
+        tma_prefetch_desc(&tmV);
+        tma_prefetch_desc(&tmKn);
+        tma_prefetch_desc(&tmVn);
+    }
+    if (warp == 1) {
+        tmem_alloc(tmem_ptr, C::kTmemCols);
+        tmem_relinquish();
+    }
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const Share share = share_of(all_pieces<false, kTile, N, C::kThreads>(a, s_pieces, s_warp), kLeastTiles);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_ptr, tO = tmem + 2 * N;
+    const int64_t pitch = static_cast<int64_t>(a.Hkv) * D;
+    int slot_now = share.begin < share.end ? slot_at(s_pieces, a.n_slots, share.begin) : 0;
+    if (share.begin >= share.end && threadIdx.x == 0) a.meta[blockIdx.x].parts = 0;
+    // Every role walks the CTA's segments by itself: at, slot_now.
+    const auto segment = [&](int64_t at) { return segment_at<false, kTile, N>(a, s_pieces, at, share.end, slot_now); };
+    int64_t at = share.begin;
+
+    if (warp == 0) {
+        // ---- loader: every lane copies a page ----
+        uint32_t stage = 0, phase = 0;
+        bool ok = true;
+        const int per_tile = kTile >> a.page_shift;
+        const uint32_t page_bytes = static_cast<uint32_t>(C::kPanels) << (a.page_shift + 7);
+        while (at < share.end && ok) {
+            const Segment s = segment(at);
+            const int32_t* list = a.table + static_cast<int64_t>(s.slot) * a.max_pages;
+            const auto page_of = [&](int t) {                          // this lane's page of tile t, -1: none to load
+                const int o = t * per_tile + lane;
+                if (lane >= per_tile || t >= min(s.p_end, s.w.cache_pieces) || static_cast<int64_t>(o) << a.page_shift >= s.w.keys) return -1;
+                const int page = list[o];
+                if (page >= 0 && page < a.n_pages) return page;
+                report(a.status, PULSAR_DEV_BAD_PAGE);                 // (some page is loaded; its rows count as absent)
+                return 0;
+            };
+            int page = page_of(s.p_begin);
+            for (int t = s.p_begin; t < s.p_end && ok; ++t) {
+                const int next = page_of(t + 1);
+                const bool fresh = t >= s.w.cache_pieces;
+                const uint32_t pages = __ballot_sync(0xffffffffu, page >= 0);
+                const uint32_t bytes = fresh ? static_cast<uint32_t>(C::kPanels) * kFreshRows * 128 : __popc(pages) * page_bytes;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    __syncwarp();
+                    ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bKvEmpty + stage), phase ^ 1, abort_flag, a.status));
+                    if (!ok) break;
+                    const uint32_t full = bar(C::bKvFull + stage), dst = smem_u32(smem) + stage * C::kTileBytes;
+                    if (lane == 0) mbar_expect_tx_a(full, bytes);
+                    __syncwarp();
+#pragma unroll
+                    for (int p = 0; p < C::kPanels; ++p) {
+                        if (fresh) {
+                            if (lane == 0) tma_load_3d_a(dst + p * kPanelBytes, kv ? &tmVn : &tmKn, full, p * 64, s.kvh, s.slot * a.T);
+                        } else if (page >= 0) {
+                            tma_load_3d_a(dst + p * kPanelBytes + (lane << (a.page_shift + 7)), kv ? &tmV : &tmK, full, p * 64, s.kvh,
+                                          page << a.page_shift);
+                        }
+                    }
+                    if (++stage == C::kStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+                page = next;
+            }
+            at = s.item_at + s.p_end;
+        }
+    } else if (warp == 1) {
+        // ---- matrix instructions: S of a tile, then PV of the tile before it ----
+        const bool leader = elect_one();
+        constexpr uint32_t kIdescS = umma_idesc_bf16(kTile, N, false, false), kIdescO = umma_idesc_bf16(kTile, N, true, true);
+        const uint64_t desc_k = umma_smem_desc_sw128(smem_u32(smem), 16, 1024);
+        const uint64_t desc_v = umma_smem_desc_sw128(smem_u32(smem), kPanelBytes, 1024);
+        const uint64_t desc_q = umma_smem_desc_sw128(smem_u32(smem + C::kQ), 16, 1024);
+        const uint64_t desc_p = umma_smem_desc_sw128(smem_u32(smem + C::kP), kPanelBytes, 1024);
+        uint32_t tile = 0, n_seg = 0, n_done = 0;          // tiles issued, segments begun, segments finished
+        uint32_t stage = 0, phase = 0;                     // of the next K or V
+        bool ok = true, first = false, last = false;       // of the tile whose PV is due
+        const auto wait = [&](int b, uint32_t parity) {
+            __syncwarp();
+            ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(b), parity, abort_flag, a.status));
+        };
+        uint32_t v_stage = 0, v_phase = 0;
+        const auto issue_pv = [&](uint32_t t) {
+            wait(C::bKvFull + static_cast<int>(v_stage), v_phase);
+            if (first) wait(C::bOEmpty, (n_done & 1) ^ 1);
+            wait(C::bPFull, t & 1);
+            if (!ok) return;
+            tc_fence_after();
+            if (leader) {
+#pragma unroll
+                for (int kk = 0; kk < kTile / 16; ++kk)
+                    umma_ss(tO, desc_v + static_cast<uint64_t>(v_stage * (C::kTileBytes >> 4) + kk * 128), desc_p + static_cast<uint64_t>(kk * 128),
+                            kIdescO, first && kk == 0 ? 0u : 1u);
+                umma_commit_a(bar(C::bKvEmpty + static_cast<int>(v_stage)));
+                umma_commit_a(bar(C::bPEmpty));
+                if (last) umma_commit_a(bar(C::bOFull));
+            }
+            if (last) ++n_done;
+        };
+        while (at < share.end && ok) {
+            const Segment s = segment(at);
+            for (int t = s.p_begin; t < s.p_end && ok; ++t, ++tile) {
+                wait(C::bKvFull + static_cast<int>(stage), phase);
+                if (t == s.p_begin) wait(C::bQFull, n_seg & 1);
+                wait(C::bSEmpty + static_cast<int>(tile & 1), ((tile >> 1) & 1) ^ 1);
+                if (!ok) break;
+                tc_fence_after();
+                if (leader) {
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint64_t off_k = static_cast<uint64_t>(stage * (C::kTileBytes >> 4) + (((kk >> 2) * kPanelBytes + (kk & 3) * 32) >> 4));
+                        const uint64_t off_q = static_cast<uint64_t>(((kk >> 2) * (N * 128) + (kk & 3) * 32) >> 4);
+                        umma_ss(tmem + (tile & 1) * N, desc_k + off_k, desc_q + off_q, kIdescS, kk > 0 ? 1u : 0u);
+                    }
+                    umma_commit_a(bar(C::bSFull + static_cast<int>(tile & 1)));
+                    umma_commit_a(bar(C::bKvEmpty + static_cast<int>(stage)));
+                    if (t + 1 == s.p_end) umma_commit_a(bar(C::bQEmpty));
+                }
+                if (++stage == C::kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+                if (tile > 0) issue_pv(tile - 1);
+                v_stage = stage;
+                v_phase = phase;
+                if (++stage == C::kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+                first = t == s.p_begin;
+                last = t + 1 == s.p_end;
+            }
+            ++n_seg;
+            at = s.item_at + s.p_end;
+        }
+        if (ok && tile > 0) issue_pv(tile - 1);
+    } else if (warp < 4) {
+        // ---- query rows, ancestors, the nodes' rows to their pages ----
+        const int t = threadIdx.x - 64;
+        bool ok = true;
+        for (uint32_t seg = 0; at < share.end; ++seg) {
+            const Segment s = segment(at);
+            ok = ok && mbar_wait_a(bar(C::bQEmpty), (seg & 1) ^ 1, abort_flag, a.status);
+            if (named_any(3, 64, !ok)) break;
+            for (int i = t; i < N * (D / 8); i += 64) {
+                const int r = i / (D / 8), v = i % (D / 8);
+                uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                if (r < s.n_rows)
+                    x = reinterpret_cast<const uint4*>(a.Q + row_of(s.token0, s.head0, s.row0, r, a.g_shift, a.Hq) * D)[v];
+                *reinterpret_cast<uint4*>(smem + C::kQ + (v >> 3) * (N * 128) + r * 128 + (((v & 7) ^ (r & 7)) << 4)) = x;
+            }
+            fence_proxy_async_smem();
+            // The softmax of an item is at most two tiles behind the products that have freed its query rows, and four buffers
+            // hold at least three items after it.
+            const bool has_new = s.p_end > s.w.cache_pieces;
+            if (has_new) ancestors(a, s.slot, s.w.n, t, s_sees + (seg % kSeesBuffers) * kMaxTree, s_up, [] { named_sync(3, 64); });
+            else named_sync(3, 64);
+            if (t == 0) {
+                s_odd[2 * (seg % kSeesBuffers)] = s_odd[2 * (seg % kSeesBuffers) + 1] = 0u;
+                arrive_a(bar(C::bQFull));
+            }
+            if (has_new && s.row0 == 0) {
+                constexpr int kVecs = D / 8;
+                const int head_at = s.kvh * D;
+                for (int i = t; i < s.w.n * kVecs; i += 64) {
+                    const int row = i / kVecs, v = i % kVecs;
+                    const int64_t to = new_row_at(a, s.slot, static_cast<int64_t>(s.w.len) + row, pitch);
+                    if (to < 0) continue;
+                    const int64_t from = (static_cast<int64_t>(s.slot) * a.T + row) * pitch + head_at;
+                    reinterpret_cast<uint4*>(a.K + to + head_at)[v] = reinterpret_cast<const uint4*>(a.Knew + from)[v];
+                    reinterpret_cast<uint4*>(a.V + to + head_at)[v] = reinterpret_cast<const uint4*>(a.Vnew + from)[v];
+                }
+            }
+            at = s.item_at + s.p_end;
+        }
+    } else {
+        // ---- softmax and epilogue ----
+        const int quarter = warp & 3, group = (warp - 4) >> 2;
+        const int key = quarter * 32 + lane, col0 = group * kCols;
+        const int id = 1 + group;                          // barrier of the warpgroup
+        const uint32_t my_lanes = static_cast<uint32_t>(quarter * 32) << 16;
+        const int tg = threadIdx.x - 128 - group * 128;    // thread of the warpgroup
+        uint32_t tile = 0;
+        uint32_t v_stage = 1, v_phase = 0;                 // ring place of the tile's V
+        bool ok = true, meta_written = false;
+        for (uint32_t seg = 0; at < share.end; ++seg) {
+            const Segment s = segment(at);
+            const int32_t* list = a.table + static_cast<int64_t>(s.slot) * a.max_pages;
+            float sum[kCols];
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) sum[c] = 0.f;
+            if (tg < kCols) s_neg[col0 + tg] = kUnset;
+            if (named_any(id, 128, !ok)) break;
+            const auto page_ok = [&](int t) {              // this thread's key of tile t exists
+                const int64_t row = static_cast<int64_t>(t) * kTile + key;
+                if (t >= min(s.p_end, s.w.cache_pieces) || row >= s.w.keys) return false;
+                const int page = list[row >> a.page_shift];
+                return page >= 0 && page < a.n_pages;
+            };
+            bool here = page_ok(s.p_begin);
+            bool failed = false;
+            for (int t = s.p_begin; t < s.p_end; ++t, ++tile) {
+                const bool next = page_ok(t + 1);
+                const bool fresh = t >= s.w.cache_pieces;
+                if (fresh) here = key < s.w.n;
+                const uint32_t tS = tmem + (tile & 1) * N + col0 + my_lanes;
+                __syncwarp();
+                ok = ok && mbar_wait_a(bar(C::bSFull + static_cast<int>(tile & 1)), (tile >> 1) & 1, abort_flag, a.status);
+                tc_fence_after();
+                uint64_t visible = ~0ull;                  // columns that see this key
+                if (fresh) {
+                    visible = 0ull;
+                    if (here) {
+                        const uint64_t* sees = s_sees + (seg % kSeesBuffers) * kMaxTree;
+#pragma unroll 4
+                        for (int c = 0; c < kCols; ++c)
+                            if (col0 + c < s.n_rows) visible |= ((sees[(s.row0 + col0 + c) >> a.g_shift] >> key) & 1ull) << c;
+                    }
+                } else if (!here) {
+                    visible = 0ull;
+                }
+                const bool masked = fresh || __any_sync(0xffffffffu, visible != ~0ull);
+                float x[kCols];
+                // x = logits (log2 units) minus the maximum in use
+                const auto logits = [&]() {
+                    __syncwarp();
+                    load_columns<kCols>(tS, x);
+                    if (masked) {
+#pragma unroll
+                        for (int c = 0; c < kCols; ++c)
+                            if (((visible >> c) & 1ull) == 0ull) x[c] = -INFINITY;
+                    }
+                };
+                const auto below = [&]() {
+                    float most = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < kCols; c += 4) {
+                        const float4 neg = *reinterpret_cast<const float4*>(s_neg + col0 + c);
+                        x[c] = fmaf(x[c], a.scale_log2, neg.x);
+                        x[c + 1] = fmaf(x[c + 1], a.scale_log2, neg.y);
+                        x[c + 2] = fmaf(x[c + 2], a.scale_log2, neg.z);
+                        x[c + 3] = fmaf(x[c + 3], a.scale_log2, neg.w);
+                        most = max3(most, fmaxf(x[c], x[c + 1]), fmaxf(x[c + 2], x[c + 3]));
+                    }
+                    return most;
+                };
+                logits();
+                if (named_any(id, 128, below() > kRescale || !ok)) {
+                    // ---- the maximum moves ----
+                    __syncwarp();
+                    ok = ok && mbar_wait_a(bar(C::bPEmpty), (tile & 1) ^ 1, abort_flag, a.status);       // PV of the tile before is done
+                    if (named_any(id, 128, !ok)) {
+                        failed = true;
+                        break;
+                    }
+                    tc_fence_after();
+                    logits();
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) {
+                        const float most = warp_max(x[c]);
+                        if (lane == 0) s_col[quarter * N + col0 + c] = most;
+                    }
+                    named_sync(id, 128);
+                    if (tg < kCols) {
+                        const int c = col0 + tg;
+                        const float most = fmaxf(fmaxf(s_col[c], s_col[N + c]), fmaxf(s_col[2 * N + c], s_col[3 * N + c])) * a.scale_log2;
+                        const float old = s_neg[c];
+                        const bool moves = most > -INFINITY && (old == kUnset || most > -old);
+                        s_alpha[c] = !moves ? 1.f : old == kUnset ? 0.f : ex2(-old - most);
+                        if (moves) s_neg[c] = -most;
+                    }
+                    named_sync(id, 128);
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) sum[c] *= s_alpha[col0 + c];
+                    if (t > s.p_begin) {
+#pragma unroll 1
+                        for (int c0 = 0; c0 < kCols; c0 += 16) {
+                            uint32_t o[16];
+                            __syncwarp();
+                            tmem_ld16(tO + col0 + c0 + my_lanes, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * s_alpha[col0 + c0 + c]);
+                            tmem_st16(tO + col0 + c0 + my_lanes, o);
+                        }
+                        tmem_wait_st();
+                    }
+                    (void)below();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_a(bar(C::bSEmpty + static_cast<int>(tile & 1)));
+                uint32_t p[kCols / 2];
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2) {
+                    const float p0 = ex2(x[c]), p1 = ex2(x[c + 1]);
+                    sum[c] += p0;
+                    sum[c + 1] += p1;
+                    p[c / 2] = pack_bf16x2(p0, p1);
+                }
+                // P^T: a line of 64 rows per key, where the product before has been read
+                __syncwarp();
+                ok = ok && mbar_wait_a(bar(C::bPEmpty), (tile & 1) ^ 1, abort_flag, a.status);
+                uint8_t* line = smem + C::kP + group * kPanelBytes + key * 128;
+#pragma unroll
+                for (int v = 0; v < kCols / 8; ++v)
+                    *reinterpret_cast<uint4*>(line + ((v ^ (key & 7)) << 4)) = make_uint4(p[4 * v], p[4 * v + 1], p[4 * v + 2], p[4 * v + 3]);
+                if (masked && group == 0) {
+                    // Rows of V that do not exist may hold anything, and 0 * NaN is NaN: they become zeros.  So does a node's value
+                    // that is not finite: nodes that do not see it have weight 0.  The epilogue adds it where it is seen.
+                    __syncwarp();
+                    ok = ok && mbar_wait_a(bar(C::bKvFull + static_cast<int>(v_stage)), v_phase, abort_flag, a.status);
+                    uint8_t* value = smem + v_stage * C::kTileBytes + key * 128;
+                    bool clear = !here;
+                    if (fresh && here) {
+                        uint32_t odd = 0;
+#pragma unroll
+                        for (int v = 0; v < D / 8; ++v) {
+                            const uint4 y = *reinterpret_cast<const uint4*>(value + (v >> 3) * kPanelBytes + ((v & 7) << 4));
+                            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                odd |= (w[k] & 0x7f80u) == 0x7f80u || (w[k] & 0x7f800000u) == 0x7f800000u ? 1u : 0u;
+                        }
+                        if (odd != 0u) {
+                            clear = true;
+                            atomicOr(&s_odd[2 * (seg % kSeesBuffers) + (key >> 5)], 1u << (key & 31));
+                        }
+                    }
+                    if (clear) {
+#pragma unroll
+                        for (int v = 0; v < D / 8; ++v)
+                            *reinterpret_cast<uint4*>(value + (v >> 3) * kPanelBytes + ((v & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                }
+                fence_proxy_async_smem();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_a(bar(C::bPFull));
+                v_stage += 2;
+                if (v_stage >= C::kStages) {
+                    v_stage -= C::kStages;
+                    v_phase ^= 1;
+                }
+                here = next;
+            }
+            if (failed) break;
+
+            // ---- sums over the keys, and the item's outputs: a thread per component ----
+            column_sums<kCols>(sum, lane);
+            if constexpr (kCols == 64) {
+                s_col[quarter * N + col0 + 2 * lane] = sum[0];
+                s_col[quarter * N + col0 + 2 * lane + 1] = sum[1];
+            } else if constexpr (kCols == 32) {
+                s_col[quarter * N + col0 + lane] = sum[0];
+            } else {
+                if ((lane & 1) == 0) s_col[quarter * N + col0 + (lane >> 1)] = sum[0];
+            }
+            named_sync(id, 128);
+            const bool whole = s.p_begin == 0 && s.p_end == s.w.pieces;
+            const int64_t part = 2 * static_cast<int64_t>(blockIdx.x) + (at == share.begin ? 0 : 1);
+            if (tg < kCols) {
+                const int c = col0 + tg;
+                const float total = (s_col[c] + s_col[N + c]) + (s_col[2 * N + c] + s_col[3 * N + c]);
+                s_inv[c] = total == 0.f ? 0.f : 1.f / total;
+                const float lse = total == 0.f ? -INFINITY : (log2f(total) - s_neg[c]) * 0.6931471805599453f;
+                if (c < s.n_rows) {
+                    if (!whole) a.part_LSE[part * N + c] = lse;
+                    else if (a.LSE != nullptr) a.LSE[row_of(s.token0, s.head0, s.row0, c, a.g_shift, a.Hq)] = lse;
+                }
+            }
+            __syncwarp();
+            ok = ok && mbar_wait_a(bar(C::bOFull), seg & 1, abort_flag, a.status);
+            if (named_any(id, 128, !ok)) break;
+            tc_fence_after();
+            const uint64_t odd = s_odd[2 * (seg % kSeesBuffers)] | static_cast<uint64_t>(s_odd[2 * (seg % kSeesBuffers) + 1]) << 32;
+#pragma unroll 1
+            for (int c0 = 0; c0 < kCols; c0 += 16) {
+                uint32_t r[16];
+                __syncwarp();
+                tmem_ld16(tO + col0 + c0 + my_lanes, r);
+                tmem_wait_ld();
+                if (key >= D) continue;                    // (d = 64: the lower half of the lanes)
+                float o[16];
+#pragma unroll
+                for (int c = 0; c < 16; ++c) o[c] = __uint_as_float(r[c]);
+                for (uint64_t left = odd; left != 0ull; left &= left - 1ull) {
+                    const int node = __ffsll(static_cast<long long>(left)) - 1;
+                    const uint64_t* sees = s_sees + (seg % kSeesBuffers) * kMaxTree;
+                    const float v = __uint_as_float(static_cast<uint32_t>(a.Vnew[(static_cast<int64_t>(s.slot) * a.T + node) * pitch + s.kvh * D + key]) << 16);
+                    const uint8_t* line = smem + C::kP + group * kPanelBytes + node * 128;
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        const int col = c0 + c;
+                        if (col0 + col >= s.n_rows || ((sees[(s.row0 + col0 + col) >> a.g_shift] >> node) & 1ull) == 0ull) continue;
+                        const uint32_t p = *reinterpret_cast<const uint16_t*>(line + (((col >> 3) ^ (node & 7)) << 4) + (col & 7) * 2);
+                        o[c] = fmaf(__uint_as_float(p << 16), v, o[c]);
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    const int col = col0 + c0 + c;
+                    if (col >= s.n_rows) break;
+                    const float y = o[c] * s_inv[col];
+                    if (!whole) {
+                        a.part_O[(part * N + col) * D + key] = y;
+                        continue;
+                    }
+                    const int64_t row = row_of(s.token0, s.head0, s.row0, col, a.g_shift, a.Hq);
+                    if (a.out_f32) static_cast<float*>(a.O)[row * D + key] = y;
+                    else static_cast<__nv_bfloat16*>(a.O)[row * D + key] = __float2bfloat16_rn(y);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_a(bar(C::bOEmpty));
+            if (s.p_begin == 0 && s.p_end < s.w.pieces) {
+                if (threadIdx.x == 128) {
+                    const int64_t end = ((s.item_at + s.w.pieces) * share.n_ctas - 1) / share.total;
+                    a.meta[blockIdx.x] = {static_cast<int>(part), static_cast<int>(end - blockIdx.x) + 1, s.token0, s.head0, s.row0, s.n_rows};
+                }
+                meta_written = true;
+            }
+            at = s.item_at + s.p_end;
+        }
+        if (share.begin < share.end && !meta_written && threadIdx.x == 128) a.meta[blockIdx.x].parts = 0;
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag != 0) {                                // copies that are still under way land before the memory is given back
+        const uint64_t t0 = globaltimer_ns();
+        while (globaltimer_ns() - t0 < 5000000ull) {
+        }
+        __syncthreads();
+    }
+    if (warp == 1) tmem_dealloc(tmem, C::kTmemCols);
+}
+
+// Joins the parts of the items that several CTAs share, a warp per row (see paged.cu for the form with few rows and many parts).
+template <int D>
+__global__ void __launch_bounds__(256)
+tiles_merge_kernel(const Meta* __restrict__ meta, const float* __restrict__ part_O, const float* __restrict__ part_LSE, int n, int g_shift, int Hq,
+                   void* O, int out_f32, float* LSE) {
+    constexpr int kPer = D / 32;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const Meta x = meta[blockIdx.x];
+    const int r = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (x.parts < 2 || r >= x.rows) return;
+    const auto slot_of = [&](int j) { return j == 0 ? x.first : 2 * (static_cast<int>(blockIdx.x) + j); };
+    float m = -INFINITY;
+    for (int j = lane; j < x.parts; j += 32) m = fmaxf(m, part_LSE[static_cast<int64_t>(slot_of(j)) * n + r]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    float acc[kPer] = {}, total = 0.f;
+    if (m > -INFINITY) {
+#pragma unroll 8
+        for (int j = 0; j < x.parts; ++j) {
+            const int64_t at = static_cast<int64_t>(slot_of(j)) * n + r;
+            const float w = ex2((part_LSE[at] - m) * 1.4426950408889634f);
+            total += w;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) acc[i] = fmaf(w, part_O[at * D + i * 32 + lane], acc[i]);
+        }
+    }
+    const float inv = total > 0.f ? 1.f / total : 0.f;
+    const int64_t row = row_of(x.token0, x.head0, x.row0, r, g_shift, Hq);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        if (out_f32) static_cast<float*>(O)[row * D + i * 32 + lane] = acc[i] * inv;
+        else static_cast<__nv_bfloat16*>(O)[row * D + i * 32 + lane] = __float2bfloat16_rn(acc[i] * inv);
+    }
+    if (lane == 0 && LSE != nullptr) LSE[row] = total > 0.f ? m + logf(total) : -INFINITY;
+}
+
+int item_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+
+template <int D, int N>
+int32_t launch(const PagedArgs& a, const CUtensorMap (&map)[4], cudaStream_t stream) {
+    using C = Cfg<D, N>;
+    const unsigned ctas = static_cast<unsigned>(sm_count());
+    PULSAR_CUDA_OK(cudaFuncSetAttribute(tree_tiles_kernel<D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    PULSAR_CUDA_OK(launch_kernel(tree_tiles_kernel<D, N>, dim3(ctas), dim3(C::kThreads), C::kSmem, stream, true, a, map[0], map[1], map[2], map[3]));
+    count_launch();
+    PULSAR_CUDA_OK(launch_kernel(tiles_merge_kernel<D>, dim3(ctas, N / 8), dim3(256), 0, stream, true, a.meta, a.part_O, a.part_LSE, N, a.g_shift, a.Hq,
+                                 a.O, a.out_f32, a.LSE));
+    count_launch();
+    return PULSAR_OK;
+}
+
+}  // namespace
+
+size_t tree_tiles_workspace_bytes(int rows, int d) { return PartScratch(sm_count(), item_rows(rows), d).total; }
+
+int32_t launch_tree_tiles(PagedArgs a, int rows, int d, void* workspace, cudaStream_t stream) {
+    const int n = item_rows(rows);
+    PartScratch(sm_count(), n, d).place(a, workspace);
+    CUtensorMap map[4];
+    const int64_t pool_rows = static_cast<int64_t>(a.n_pages) << a.page_shift, fresh_rows = static_cast<int64_t>(a.n_slots) * a.T;
+    if (!make_map_3d(&map[0], a.K, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) || !make_map_3d(&map[1], a.V, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) ||
+        !make_map_3d(&map[2], a.Knew, fresh_rows, a.Hkv, d, 1, kFreshRows) || !make_map_3d(&map[3], a.Vnew, fresh_rows, a.Hkv, d, 1, kFreshRows))
+        return PULSAR_ERR_CUDA;
+    if (d == 128) {
+        switch (n) {
+            case 16: return launch<128, 16>(a, map, stream);
+            case 32: return launch<128, 32>(a, map, stream);
+            case 64: return launch<128, 64>(a, map, stream);
+            default: return launch<128, 128>(a, map, stream);
+        }
+    }
+    switch (n) {
+        case 16: return launch<64, 16>(a, map, stream);
+        case 32: return launch<64, 32>(a, map, stream);
+        case 64: return launch<64, 64>(a, map, stream);
+        default: return launch<64, 128>(a, map, stream);
+    }
+}
+
+}  // namespace pulsar

@@ -17,7 +17,6 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 constexpr int kForkThreads = 1024;               // one per slot, at least
 constexpr int kForkCtas = 8;
-constexpr int kMaxSlots = 1024;
 
 struct Copy {                                    // rows of page src that page dst receives
     int src, dst, rows, pad_;
@@ -249,7 +248,7 @@ fork_copy_kernel(const int32_t* __restrict__ n_copies, const Copy* __restrict__ 
 // Compact: rows len + accept[j] move to rows len + j.  A row may be the target of one move and the source of another, so a CTA
 // holds its columns of all the slot's moving rows in registers before it writes any of them.
 // ---------------------------------------------------------------------------------------------
-constexpr int kCompactThreads = 256, kCompactUnroll = 4, kMaxTree = 64;
+constexpr int kCompactThreads = 256, kCompactUnroll = 4;
 
 struct PoolArgs {
     uint4 *K, *V;

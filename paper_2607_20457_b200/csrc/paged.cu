@@ -4,7 +4,7 @@
 // head (tree: nodes x heads of the group; selected pages: the group's heads of one token) against a list of keys, cut into pieces
 // of 16 keys (d = 128; 32 with d = 64).  Every CTA adds up the pieces of all slots, takes an equal share of them, whichever items they
 // belong to, and leaves a partial (normalised output and l = ln sum exp) where it holds an item only in part; a second
-// launch joins those.
+// launch joins those (paged_merge.cu).
 #include <algorithm>
 
 #include "mma.cuh"
@@ -20,6 +20,7 @@ constexpr int kRows = 8;                        // query rows of an item: the co
 constexpr int kUnitBytes = 4096;
 constexpr int kUnits = 3;                       // of a warp's ring: one in use, two on their way
 constexpr int kRingBytes = kWarps * kUnits * kUnitBytes;
+constexpr int kLeastKeys = 16;                  // of a piece
 constexpr int kLeastPieces = 3 * kWarps;        // of a CTA: three per warp, unless all CTAs have fewer
 
 // Two CTAs per SM: while the keys of one are on their way, the other computes.
@@ -36,9 +37,8 @@ paged_rows_kernel(const __grid_constant__ PagedArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
     float2* w_ml = reinterpret_cast<float2*>(smem + kRingBytes);               // [kRows][kWarps]
     uint64_t* s_sees = reinterpret_cast<uint64_t*>(w_ml + kRows * kWarps);     // [kMaxTree] a node's ancestors and itself
-    int64_t* s_pieces = reinterpret_cast<int64_t*>(s_sees + kMaxTree);         // [n_slots + 1] pieces of the slots before
-    int64_t* s_warp = s_pieces + kMaxSlots + 1;                                // [kWarps]
-    int* s_up = reinterpret_cast<int*>(s_warp + kWarps);                       // [kMaxTree]
+    int* s_up = reinterpret_cast<int*>(s_sees + kMaxTree);                     // [kMaxTree]
+    Slots& slots = *reinterpret_cast<Slots*>(s_up + kMaxTree);
     float* w_o = reinterpret_cast<float*>(smem);                               // [kWarps][kRows][kPitch], where the rings were
 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -47,13 +47,15 @@ paged_rows_kernel(const __grid_constant__ PagedArgs a) {
     grid_launch_dependents();
 
     // ---- this CTA's share of all pieces of all slots ----
-    const Share share = share_of(all_pieces<kSparse, kKeys, kRows, kThreads>(a, s_pieces, s_warp), kLeastPieces);
-    const int64_t begin = share.begin, end = share.end;
+    if (warp == 0) (void)all_pieces<kSparse, kKeys, kRows>(a, slots);
+    __syncthreads();
+    const Shares shares(slots.before[a.n_slots], kLeastPieces, gridDim.x);
+    const int begin = shares.begin(blockIdx.x), end = shares.begin(blockIdx.x + 1);
     if (begin >= end) {
         if (threadIdx.x == 0) a.meta[blockIdx.x].parts = 0;
         return;
     }
-    int slot_now = slot_at(s_pieces, a.n_slots, begin);
+    int slot_now = slot_at(slots, a.n_slots, begin);
 
     const uint32_t ring = smem_u32(smem) + warp * (kUnits * kUnitBytes);
     const int copy_row = lane / kVecs, copy_vec = lane % kVecs;
@@ -64,9 +66,9 @@ paged_rows_kernel(const __grid_constant__ PagedArgs a) {
     const uint32_t v_lane = ring + ((mi >> 1) * 8 + l8) * (D * 2), v_x = ((mi & 1) ^ l8) << 4;     // V: read transposed
     bool meta_written = false;
 
-    for (int64_t at = begin; at < end;) {
+    for (int at = begin; at < end;) {
         // ---- the next item and this CTA's pieces of it ----
-        const Segment seg = segment_at<kSparse, kKeys, kRows>(a, s_pieces, at, end, slot_now);
+        const Segment seg = segment_at<kSparse, kKeys, kRows>(a, slots, at, end, slot_now);
         const SlotWork& w = seg.w;
         const int slot = seg.slot, p_begin = seg.p_begin, p_end = seg.p_end, row0 = seg.row0, n_rows = seg.n_rows, kvh = seg.kvh;
         const int token = seg.token, token0 = seg.token0, head0 = seg.head0;
@@ -368,8 +370,7 @@ paged_rows_kernel(const __grid_constant__ PagedArgs a) {
         // An item that begins here and goes on elsewhere is this CTA's last; the CTAs up to the one with its last piece have a part each.
         if (p_begin == 0 && p_end < w.pieces) {
             if (threadIdx.x == 0) {
-                const int64_t last = ((seg.item_at + w.pieces) * share.n_ctas - 1) / share.total;         // the last CTA that begins before the item's end
-                a.meta[blockIdx.x] = {static_cast<int>(part), static_cast<int>(last - blockIdx.x) + 1, token0, head0, row0, n_rows};
+                a.meta[blockIdx.x] = {static_cast<int>(part), shares.owner(seg.item_at + w.pieces - 1) - static_cast<int>(blockIdx.x) + 1, 1, token0, head0, row0, n_rows};
             }
             meta_written = true;
         }
@@ -377,59 +378,6 @@ paged_rows_kernel(const __grid_constant__ PagedArgs a) {
         __syncthreads();                         // the ring is loaded into again
     }
     if (!meta_written && threadIdx.x == 0) a.meta[blockIdx.x].parts = 0;
-}
-
-// The parts of an item that several CTAs share: O = sum_j e^{l_j - l} A_j (Appendix H's closed form).  One CTA per item and row; its
-// warps share the parts.
-template <int D>
-__global__ void __launch_bounds__(kThreads)
-paged_merge_kernel(const Meta* __restrict__ meta, const float* __restrict__ part_O, const float* __restrict__ part_LSE, int g_shift, int Hq,
-                   void* O, int out_f32, float* LSE) {
-    constexpr int kPer = D / 32;
-    __shared__ float s_o[kWarps][D];
-    __shared__ float s_m[kWarps], s_l[kWarps];
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const Meta x = meta[blockIdx.x];
-    const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (x.parts < 2 || r >= x.rows) return;
-    const auto slot_of = [&](int j) { return j == 0 ? x.first : 2 * (static_cast<int>(blockIdx.x) + j); };
-    float m = -INFINITY;
-    for (int j = threadIdx.x; j < x.parts; j += kThreads) m = fmaxf(m, part_LSE[slot_of(j) * kRows + r]);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    if (lane == 0) s_m[warp] = m;
-    __syncthreads();
-    m = s_m[0];
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s_m[w]);
-    float acc[kPer] = {}, sum = 0.f;
-    if (m > -INFINITY) {
-#pragma unroll 4
-        for (int j = warp; j < x.parts; j += kWarps) {
-            const int64_t at = static_cast<int64_t>(slot_of(j)) * kRows + r;
-            const float w = ex2((part_LSE[at] - m) * 1.4426950408889634f);
-            sum += w;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) acc[i] = fmaf(w, part_O[at * D + i * 32 + lane], acc[i]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) s_o[warp][i * 32 + lane] = acc[i];
-    if (lane == 0) s_l[warp] = sum;
-    __syncthreads();
-    if (threadIdx.x >= D) return;
-    float y = 0.f, total = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        y += s_o[w][threadIdx.x];
-        total += s_l[w];
-    }
-    y = total > 0.f ? y / total : 0.f;
-    const int64_t row = row_of(x.token0, x.head0, x.row0, r, g_shift, Hq);
-    if (out_f32) static_cast<float*>(O)[row * D + threadIdx.x] = y;
-    else reinterpret_cast<__nv_bfloat16*>(O)[row * D + threadIdx.x] = __float2bfloat16_rn(y);
-    if (threadIdx.x == 0 && LSE != nullptr) LSE[row] = total > 0.f ? m + logf(total) : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -613,7 +561,7 @@ page_select_kernel(const __grid_constant__ SelectArgs a) {
 // ---------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------
-constexpr int kSmemBytes = kRingBytes + kRows * kWarps * 8 + kMaxTree * 8 + (kMaxSlots + 1) * 8 + kWarps * 8 + kMaxTree * 4;
+constexpr int kSmemBytes = kRingBytes + kRows * kWarps * 8 + kMaxTree * 8 + kMaxTree * 4 + static_cast<int>(sizeof(Slots));
 
 bool heads_ok(int32_t Hq, int32_t Hkv) {
     if (Hkv < 1 || Hq < Hkv || Hq % Hkv != 0) return false;
@@ -629,11 +577,7 @@ int32_t launch_rows(Kernel kernel, const PagedArgs& a, int d, cudaStream_t st) {
     PULSAR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes));
     PULSAR_CUDA_OK(launch_kernel(kernel, dim3(ctas), dim3(kThreads), kSmemBytes, st, true, a));
     count_launch();
-    const auto merge = d == 128 ? paged_merge_kernel<128> : paged_merge_kernel<64>;
-    PULSAR_CUDA_OK(launch_kernel(merge, dim3(ctas, kRows), dim3(kThreads), 0, st, true, a.meta, a.part_O, a.part_LSE, a.g_shift, a.Hq, a.O,
-                                 a.out_f32, a.LSE));
-    count_launch();
-    return PULSAR_OK;
+    return launch_parts_merge(a, ctas, kRows, d, st);
 }
 
 float scale_log2(float softmax_scale, int32_t d) {
@@ -667,6 +611,9 @@ extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, con
     if (!aligned(page_table, 4) || !aligned(cache_len, 4) || !aligned(parent, 4) || !aligned(n_draft, 4) || !aligned(LSE, 4) ||
         !aligned(workspace, 256))
         return PULSAR_ERR_ALIGNMENT;
+    if (!(T * (Hq / Hkv) > kRows ? tree_tiles_ok(n_slots, Hkv, static_cast<int64_t>(max_pages) * page_size, T)
+                                 : pieces_ok(n_slots, Hkv, static_cast<int64_t>(max_pages) * page_size, T, kLeastKeys)))
+        return PULSAR_ERR_SHAPE;
     if (workspace_bytes < pulsar_tree_attn_workspace_bytes(n_slots, T, Hq, Hkv, d)) return PULSAR_ERR_WORKSPACE;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
     PagedArgs a{};
@@ -726,7 +673,8 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
                                       float softmax_scale, uint16_t* O, float* LSE, int32_t* sel, void* workspace,
                                       size_t workspace_bytes, int32_t* device_status, void* stream) {
     if (!pool_ok(1, n_pages, page_size, Hkv, d, n_slots, max_pages) || !sparse_ok(n_slots, T, k, Hq, Hkv, d) || sink < 0 || window < 0 ||
-        static_cast<int64_t>(sink) + window > k)
+        static_cast<int64_t>(sink) + window > k ||
+        !pieces_ok(n_slots, static_cast<int64_t>(T) * Hkv * 2, std::min<int64_t>(k + 1, max_pages) * page_size, T, kLeastKeys))
         return PULSAR_ERR_SHAPE;
     if (Q == nullptr || Knew == nullptr || Vnew == nullptr || K_pages == nullptr || V_pages == nullptr || summary == nullptr ||
         page_table == nullptr || cache_len == nullptr || O == nullptr || sel == nullptr || workspace == nullptr)

@@ -12,6 +12,10 @@ inline bool pool_ok(int64_t n_layers, int32_t n_pages, int32_t page_size, int32_
            n_slots >= 1 && n_slots <= 1024 && max_pages >= 1 && static_cast<int64_t>(max_pages) * page_size <= (int64_t{1} << 30) &&
            static_cast<int64_t>(n_slots) * max_pages < (int64_t{1} << 31);
 }
+// Whether the pieces of an attention call can be counted in 32 bits, whatever the lengths on the device are.
+inline bool pieces_ok(int64_t n_slots, int64_t max_items, int64_t keys, int64_t T, int piece) {
+    return n_slots * max_items * ((keys + piece - 1) / piece + (T + piece - 1) / piece) < (int64_t{1} << 31);
+}
 inline int log2_exact(int x) {
     int s = 0;
     while ((1 << s) < x) ++s;
@@ -30,7 +34,8 @@ constexpr int kMaxTree = 64;                    // nodes of a drafted tree
 // CTA takes an equal share of all pieces of all slots and leaves a partial (normalised output and l = ln sum exp) where it holds an
 // item only in part.
 struct Meta {                                   // the item that begins in a CTA and goes on in the next ones
-    int first, parts;                           // first partial (those of the CTAs after it are their first ones); 0: there is none
+    int first, parts;                           // first partial, and how many (0: there is no such item); those after it are the first
+    int step;                                   // ones of every step-th CTA
     int token0, head0, row0, rows;              // of its rows: see row_of
 };
 
@@ -49,7 +54,11 @@ struct PagedArgs {
     int32_t* status;
 };
 
+// Joins the partials that `ctas` CTAs have left of items of `rows` rows (paged_merge.cu).
+int32_t launch_parts_merge(const PagedArgs& a, unsigned ctas, int rows, int d, cudaStream_t stream);
+
 // Trees with more than eight query rows per KV head (paged_tiles.cu).
+bool tree_tiles_ok(int64_t n_slots, int64_t Hkv, int64_t keys, int64_t T);
 size_t tree_tiles_workspace_bytes(int rows, int d);
 int32_t launch_tree_tiles(PagedArgs a, int rows, int d, void* workspace, cudaStream_t stream);
 
@@ -78,23 +87,23 @@ __device__ __forceinline__ int checked_len(int len, int64_t capacity, bool tell,
     return len < 0 ? 0 : static_cast<int>(capacity);
 }
 
-// Bookkeeping of a slot, the same in every CTA.
+// Bookkeeping of a slot, the same in every CTA.  Pieces of all slots together are fewer than 2^31 (checked on the host: pieces_ok).
 struct SlotWork {
     int len, n;                                  // rows in the cache; new tokens
     int keys;                                    // cached rows an item reads
     int cache_pieces, pieces, items;
 };
 template <bool kSparse, int kKeys, int kRows>
-__device__ __forceinline__ SlotWork slot_work(const PagedArgs& a, int slot, bool tell) {
+__device__ __forceinline__ SlotWork slot_work(const PagedArgs& a, int len, int n) {
     SlotWork w;
-    w.len = checked_len(a.len[slot], static_cast<int64_t>(a.max_pages) << a.page_shift, tell, a.status);
-    w.n = a.n_draft != nullptr ? min(max(a.n_draft[slot], 0), a.T) : a.T;
-    const int full = w.len >> a.page_shift;
-    w.keys = kSparse ? (min(a.k, full) << a.page_shift) + (w.len - (full << a.page_shift)) : w.len;
+    w.len = len;
+    w.n = n;
+    const int full = len >> a.page_shift;
+    w.keys = kSparse ? (min(a.k, full) << a.page_shift) + (len - (full << a.page_shift)) : len;
     w.cache_pieces = (w.keys + kKeys - 1) / kKeys;
-    w.pieces = w.cache_pieces + (w.n + kKeys - 1) / kKeys;
+    w.pieces = w.cache_pieces + (n + kKeys - 1) / kKeys;
     const int g = 1 << a.g_shift;
-    w.items = kSparse ? w.n * a.Hkv * ((g + kRows - 1) / kRows) : a.Hkv * ((w.n * g + kRows - 1) / kRows);
+    w.items = kSparse ? n * a.Hkv * ((g + kRows - 1) / kRows) : a.Hkv * ((n * g + kRows - 1) / kRows);
     return w;
 }
 
@@ -104,57 +113,65 @@ __device__ __forceinline__ int64_t row_of(int token0, int head0, int row0, int r
     return static_cast<int64_t>(token0 + (x >> g_shift)) * Hq + head0 + (x & ((1 << g_shift) - 1));
 }
 
-// Pieces of the slots before each slot, in s_pieces [n_slots + 1]; returns those of all.  s_warp: [warps of the CTA].
-template <bool kSparse, int kKeys, int kRows, int kThreads>
-__device__ __forceinline__ int64_t all_pieces(const PagedArgs& a, int64_t* s_pieces, int64_t* s_warp) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t total = 0;
-    for (int s0 = 0; s0 < a.n_slots; s0 += kThreads) {
-        const int s = s0 + threadIdx.x;
-        int64_t x = 0;
+// What a CTA knows of the slots, in shared memory.
+struct Slots {
+    int before[kMaxSlots + 1];                   // pieces of the slots before
+    int len[kMaxSlots];
+    unsigned char n[kMaxSlots];
+};
+// One warp fills it in; returns the pieces of all slots.
+template <bool kSparse, int kKeys, int kRows>
+__device__ __forceinline__ int all_pieces(const PagedArgs& a, Slots& slots) {
+    const int lane = threadIdx.x & 31;
+    int total = 0;
+    for (int s0 = 0; s0 < a.n_slots; s0 += 32) {
+        const int s = s0 + lane;
+        int x = 0;
         if (s < a.n_slots) {
-            const SlotWork w = slot_work<kSparse, kKeys, kRows>(a, s, blockIdx.x == 0);
-            x = static_cast<int64_t>(w.pieces) * w.items;
+            const int len = checked_len(a.len[s], static_cast<int64_t>(a.max_pages) << a.page_shift, blockIdx.x == 0, a.status);
+            const int n = a.n_draft != nullptr ? min(max(a.n_draft[s], 0), a.T) : a.T;
+            const SlotWork w = slot_work<kSparse, kKeys, kRows>(a, len, n);
+            x = w.pieces * w.items;
+            slots.len[s] = len;
+            slots.n[s] = static_cast<unsigned char>(n);
         }
-        int64_t y = x;
+        int y = x;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int64_t z = __shfl_up_sync(0xffffffffu, y, d);
+            const int z = __shfl_up_sync(0xffffffffu, y, d);
             if (lane >= d) y += z;
         }
-        if (lane == 31) s_warp[warp] = y;
-        __syncthreads();
-        int64_t before = total;
-        for (int w = 0; w < kThreads / 32; ++w) {
-            if (w < warp) before += s_warp[w];
-            total += s_warp[w];
-        }
-        if (s < a.n_slots) s_pieces[s] = before + y - x;
-        __syncthreads();
+        if (s < a.n_slots) slots.before[s] = total + y - x;
+        total += __shfl_sync(0xffffffffu, y, 31);
     }
-    if (threadIdx.x == 0) s_pieces[a.n_slots] = total;
-    __syncthreads();
+    if (lane == 0) slots.before[a.n_slots] = total;
+    __syncwarp();
     return total;
 }
 
-// This CTA's share of them.
-struct Share {
-    int64_t total, n_ctas, begin, end;
+// Equal shares of `total` pieces: the first `more` of n have one more than the others.
+struct Shares {
+    uint32_t n, each, more;
+    __device__ __forceinline__ Shares(int total, int least, int ctas) {
+        n = static_cast<uint32_t>(max(1, min(ctas, total / least)));
+        each = static_cast<uint32_t>(total) / n;
+        more = static_cast<uint32_t>(total) - each * n;
+    }
+    __device__ __forceinline__ int begin(int i) const {        // n and beyond: all of them
+        const uint32_t c = min(static_cast<uint32_t>(i), n);
+        return static_cast<int>(c * each + min(c, more));
+    }
+    __device__ __forceinline__ int owner(int piece) const {
+        const uint32_t p = static_cast<uint32_t>(piece), low = more * (each + 1);
+        return static_cast<int>(p < low ? p / (each + 1) : more + (p - low) / each);
+    }
 };
-__device__ __forceinline__ Share share_of(int64_t total, int least) {
-    Share s;
-    s.total = total;
-    s.n_ctas = max(static_cast<int64_t>(1), min(static_cast<int64_t>(gridDim.x), total / least));
-    s.begin = blockIdx.x < s.n_ctas ? total * blockIdx.x / s.n_ctas : total;
-    s.end = blockIdx.x < s.n_ctas ? total * (blockIdx.x + 1) / s.n_ctas : total;
-    return s;
-}
 // The last slot that begins at or before piece `at`.
-__device__ __forceinline__ int slot_at(const int64_t* s_pieces, int n_slots, int64_t at) {
+__device__ __forceinline__ int slot_at(const Slots& slots, int n_slots, int at) {
     int lo = 0, hi = n_slots - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (s_pieces[mid] <= at) lo = mid;
+        if (slots.before[mid] <= at) lo = mid;
         else hi = mid - 1;
     }
     return lo;
@@ -165,21 +182,22 @@ struct Segment {
     SlotWork w;
     int slot, p_begin, p_end;
     int row0, n_rows, kvh, token, token0, head0;
-    int64_t item_at;                             // the item's first piece among all
+    int item_at;                                 // the item's first piece among all
 };
 template <bool kSparse, int kKeys, int kRows>
-__device__ __forceinline__ Segment segment_at(const PagedArgs& a, const int64_t* s_pieces, int64_t at, int64_t end, int& slot) {
+__device__ __forceinline__ Segment segment_at(const PagedArgs& a, const Slots& slots, int at, int end, int& slot) {
     Segment s;
-    while (s_pieces[slot + 1] <= at) ++slot;
+    while (slots.before[slot + 1] <= at) ++slot;
     s.slot = slot;
-    s.w = slot_work<kSparse, kKeys, kRows>(a, slot, false);
-    const int item = static_cast<int>((at - s_pieces[slot]) / s.w.pieces), g = 1 << a.g_shift;
-    s.item_at = s_pieces[slot] + static_cast<int64_t>(item) * s.w.pieces;
-    s.p_begin = static_cast<int>(at - s.item_at);
-    s.p_end = static_cast<int>(min(end - s.item_at, static_cast<int64_t>(s.w.pieces)));
+    s.w = slot_work<kSparse, kKeys, kRows>(a, slots.len[slot], slots.n[slot]);
+    const int first = slots.before[slot], g = 1 << a.g_shift;
+    const int item = static_cast<int>(static_cast<uint32_t>(at - first) / static_cast<uint32_t>(s.w.pieces));
+    s.item_at = first + item * s.w.pieces;
+    s.p_begin = at - s.item_at;
+    s.p_end = min(end - s.item_at, s.w.pieces);
     const int rows = kSparse ? g : s.w.n * g, row_blocks = (rows + kRows - 1) / kRows;
-    const int unit = item / row_blocks;          // KV head, or token and KV head
-    s.row0 = (item % row_blocks) * kRows;
+    const int unit = row_blocks == 1 ? item : item / row_blocks;         // KV head, or token and KV head
+    s.row0 = (item - unit * row_blocks) * kRows;
     s.kvh = kSparse ? unit % a.Hkv : unit;
     s.token = kSparse ? unit / a.Hkv : 0;
     s.n_rows = min(kRows, rows - s.row0);

@@ -6,8 +6,8 @@
 //
 //   warp 0      loader: pages of K and V by TMA into a ring of tiles, the nodes' own rows as the last tile of an item
 //   warp 1      issues the matrix instructions: S of the next tile before PV of this one
-//   warps 2-3   query rows into shared memory, ancestors of the nodes, the nodes' rows to their pages
-//   warps 4-..  softmax: a thread per key and 64 columns (or all, if fewer); epilogue: a thread per output component
+//   warps 2-3   query rows (TMA), which nodes see which, the nodes' rows to their pages
+//   warps 4-..  softmax: a thread per key and 32 columns (or all, if fewer); epilogue: a thread per output component and 32 rows
 //
 // A column's maximum lies across lanes, so it is not formed for every tile: P is formed with the largest logit seen when it was
 // last moved, and moved (and O^T and the sums rescaled) when a logit exceeds it by more than 2^8.  P, O^T and the sums use the same
@@ -28,19 +28,32 @@ constexpr int kFreshRows = 64;                   // rows of the nodes' own tile 
 constexpr float kRescale = 8.f;                  // in log2 units
 constexpr float kUnset = 1e30f;                  // stands for minus a maximum that no logit has set: every logit exceeds it
 constexpr int kLeastTiles = 2;                   // of a CTA, unless all CTAs have fewer
-constexpr int kSeesBuffers = 4;                  // see the loader of query rows
+constexpr int kRowsBarrier = 5;                  // named barriers: 1 .. 4 of the softmax warpgroups, this one of warps 2 and 3
+constexpr int kAllRows = 1 << 20;                // (the rows of an item are cut up between CTAs, not between items)
+constexpr int kQueue = 4;                        // segments that the loader may publish ahead of the slowest consumer
+
+// A CTA's pieces of one item, as the loader publishes them.
+struct __align__(16) Work {
+    int valid;                                   // 0: no more
+    int slot, p_begin, p_end, cache_pieces;
+    int keys, n, row0, n_rows, kvh, token0, head0;
+    int part;                                    // place of the partial, -1: all of the item, its outputs are final
+    int pad_[3];
+};
+static_assert(sizeof(Work) == 64, "");
 
 template <int D, int N>
 struct Cfg {
     static constexpr int kPanels = D / 64;
     static constexpr int kTileBytes = kPanels * kPanelBytes;
-    static constexpr int kCols = N < 64 ? N : 64;                // columns of a softmax thread
+    static constexpr int kCols = N < 32 ? N : 32;                // columns of a softmax thread
     static constexpr int kGroups = N / kCols;                    // softmax warpgroups
     static constexpr int kSoftWarps = 4 * kGroups;
     static constexpr int kThreads = 128 + 128 * kGroups;
     static constexpr int kPBytes = (N + 63) / 64 * kPanelBytes;
     static constexpr int kQBytes = kPanels * N * 128;
-    static constexpr int kMisc = (kMaxSlots + 2) * 8 + kThreads / 32 * 8 + kSeesBuffers * (kMaxTree * 8 + 8) + 64 * 8 + 7 * N * 4 + kMaxTree * 4 + 8;
+    static constexpr int kMisc = static_cast<int>(sizeof(Slots)) + 12 + (kQueue + 1) * kMaxTree * 8 + kQueue * (8 + 64) + 64 * 8 + 7 * N * 4 + N * 8 +
+                                 kMaxTree * 4 + 8;
     static constexpr int kFit = (232448 - kPBytes - kQBytes - kMisc) / kTileBytes;
     static constexpr int kStages = kFit < 10 ? kFit : 10;
     // The product with V reads 128 components; with d = 64 the second half is whatever follows the tile (and is not used), so
@@ -52,7 +65,8 @@ struct Cfg {
     static constexpr int kTmemCols = 3 * N <= 32 ? 32 : 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 3 * N <= 256 ? 256 : 512;
     // barriers
     static constexpr int bKvFull = 0, bKvEmpty = kStages, bQFull = 2 * kStages, bQEmpty = bQFull + 1, bSFull = bQEmpty + 1, bSEmpty = bSFull + 2,
-                         bPFull = bSEmpty + 2, bPEmpty = bPFull + 1, bOFull = bPEmpty + 1, bOEmpty = bOFull + 1, kBars = bOEmpty + 1;
+                         bPFull = bSEmpty + 2, bPEmpty = bPFull + 1, bOFull = bPEmpty + 1, bOEmpty = bOFull + 1, bSees = bOEmpty + 1, bWorkFull = bSees + kQueue, bWorkEmpty = bWorkFull + kQueue,
+                         kBars = bWorkEmpty + kQueue;
     static_assert(kBars <= 64 && kStages >= 3, "");
 };
 
@@ -75,6 +89,22 @@ __device__ __forceinline__ bool named_any(int id, int threads, bool x) {
 }
 __device__ __forceinline__ void arrive_a(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
+// Two fused multiply-adds (x * s + y), two sums, with one instruction each.
+__device__ __forceinline__ void fma2(float& x0, float& x1, float s, float y0, float y1) {
+    asm("{\n\t.reg .b64 a, b, c;\n\t"
+        "mov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %2};\n\tmov.b64 c, {%3, %4};\n\t"
+        "fma.rn.f32x2 a, a, b, c;\n\t"
+        "mov.b64 {%0, %1}, a;\n\t}"
+        : "+f"(x0), "+f"(x1) : "f"(s), "f"(y0), "f"(y1));
+}
+__device__ __forceinline__ void add2(float& x0, float& x1, float y0, float y1) {
+    asm("{\n\t.reg .b64 a, b;\n\t"
+        "mov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %3};\n\t"
+        "add.rn.f32x2 a, a, b;\n\t"
+        "mov.b64 {%0, %1}, a;\n\t}"
+        : "+f"(x0), "+f"(x1) : "f"(y0), "f"(y1));
+}
+
 // Columns [0, C) of TMEM, 32 lanes per warp.
 template <int C>
 __device__ __forceinline__ void load_columns(uint32_t taddr, float (&x)[C]) {
@@ -85,12 +115,12 @@ __device__ __forceinline__ void load_columns(uint32_t taddr, float (&x)[C]) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r[i]);
     } else {
-        uint32_t r[C];
-        PULSAR_TMEM_LD32_AT(taddr, r, 0);
-        if constexpr (C == 64) PULSAR_TMEM_LD32_AT(taddr + 32, r, 32);
+        static_assert(C == 32, "");
+        uint32_t r[32];
+        tmem_ld32(taddr, r);
         tmem_wait_ld();
 #pragma unroll
-        for (int i = 0; i < C; ++i) x[i] = __uint_as_float(r[i]);
+        for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
     }
 }
 
@@ -119,23 +149,26 @@ __device__ __forceinline__ void column_sums(float (&x)[C], int lane) {
 template <int D, int N>
 __global__ void __launch_bounds__(Cfg<D, N>::kThreads, 1)
 tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                  const __grid_constant__ CUtensorMap tmKn, const __grid_constant__ CUtensorMap tmVn) {
+                  const __grid_constant__ CUtensorMap tmKn, const __grid_constant__ CUtensorMap tmVn, const __grid_constant__ CUtensorMap tmQ,
+                  int row_blocks) {
     using C = Cfg<D, N>;
     constexpr int kCols = C::kCols;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* rest = smem + C::kRest;
-    int64_t* s_pieces = reinterpret_cast<int64_t*>(rest);                              // [n_slots + 1]
-    int64_t* s_warp = s_pieces + kMaxSlots + 2;                                        // (what float4 reads stays on 16 bytes)
-    uint64_t* s_sees = reinterpret_cast<uint64_t*>(s_warp + C::kThreads / 32);         // [kSeesBuffers][kMaxTree]
-    uint64_t* bars = s_sees + kSeesBuffers * kMaxTree;                                 // [64]
+    uint64_t* s_seen = reinterpret_cast<uint64_t*>(rest);                              // [kQueue][kMaxTree] the nodes that see a node
+    uint64_t* s_sees = s_seen + kQueue * kMaxTree;                                     // [kMaxTree] a node's ancestors and itself
+    Work* s_work = reinterpret_cast<Work*>(s_sees + kMaxTree);                         // [kQueue]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(s_work + kQueue);                     // [64]
     float* s_col = reinterpret_cast<float*>(bars + 64);                                // [4][N] of each warp's keys: largest logits, sums
     float* s_neg = s_col + 4 * N;                                                      // [N] minus the maximum in use
     float* s_alpha = s_neg + N;                                                        // [N] rescaling factors
     float* s_inv = s_alpha + N;                                                        // [N] 1 / sum
-    int* s_up = reinterpret_cast<int*>(s_inv + N);                                     // [kMaxTree]
-    uint32_t* s_odd = reinterpret_cast<uint32_t*>(s_up + kMaxTree);                    // [kSeesBuffers][2] nodes whose value is not finite
-    uint32_t* tmem_ptr = s_odd + 2 * kSeesBuffers;
+    int64_t* s_to = reinterpret_cast<int64_t*>(s_inv + N);                             // [N] where a row's outputs go
+    int* s_up = reinterpret_cast<int*>(s_to + N);                                      // [kMaxTree]
+    uint32_t* s_odd = reinterpret_cast<uint32_t*>(s_up + kMaxTree);                    // [kQueue][2] nodes whose value is not finite
+    uint32_t* tmem_ptr = s_odd + 2 * kQueue;
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_ptr + 1);
+    Slots& slots = *reinterpret_cast<Slots*>(tmem_ptr + 2);
 
     const int lane = threadIdx.x & 31;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
@@ -157,11 +190,17 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
         mbar_init(bars + C::bPEmpty, 1);
         mbar_init(bars + C::bOFull, 1);
         mbar_init(bars + C::bOEmpty, C::kSoftWarps);
+        for (int i = 0; i < kQueue; ++i) {
+            mbar_init(bars + C::bSees + i, 1);
+            mbar_init(bars + C::bWorkFull + i, 1);
+            mbar_init(bars + C::bWorkEmpty + i, C::kSoftWarps + 2);                    // and the issuer, and warps 2 and 3
+        }
         mbar_fence_init();
         tma_prefetch_desc(&tmK);
         tma_prefetch_desc(&tmV);
         tma_prefetch_desc(&tmKn);
         tma_prefetch_desc(&tmVn);
+        tma_prefetch_desc(&tmQ);
     }
     if (warp == 1) {
         tmem_alloc(tmem_ptr, C::kTmemCols);
@@ -169,17 +208,17 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
     }
     grid_dependency_wait();
     grid_launch_dependents();
-    const Share share = share_of(all_pieces<false, kTile, N, C::kThreads>(a, s_pieces, s_warp), kLeastTiles);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_ptr, tO = tmem + 2 * N;
     const int64_t pitch = static_cast<int64_t>(a.Hkv) * D;
-    int slot_now = share.begin < share.end ? slot_at(s_pieces, a.n_slots, share.begin) : 0;
-    if (share.begin >= share.end && threadIdx.x == 0) a.meta[blockIdx.x].parts = 0;
-    // Every role walks the CTA's segments by itself: at, slot_now.
-    const auto segment = [&](int64_t at) { return segment_at<false, kTile, N>(a, s_pieces, at, share.end, slot_now); };
-    int64_t at = share.begin;
+    // The next published segment (a warp's lanes together); false at the end.
+    const auto next_work = [&](uint32_t seq, bool& ok) -> const Work* {
+        __syncwarp();
+        ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bWorkFull + static_cast<int>(seq % kQueue)), (seq / kQueue) & 1, abort_flag, a.status));
+        return s_work + seq % kQueue;
+    };
 
     if (warp == 0) {
         // ---- loader: every lane copies a page ----
@@ -187,21 +226,55 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
         bool ok = true;
         const int per_tile = kTile >> a.page_shift;
         const uint32_t page_bytes = static_cast<uint32_t>(C::kPanels) << (a.page_shift + 7);
-        while (at < share.end && ok) {
-            const Segment s = segment(at);
+        // More than N rows: neighbouring CTAs have the same keys at the same time, and N of the rows each.
+        const int cta = static_cast<int>(blockIdx.x) / row_blocks, n_ctas = static_cast<int>(gridDim.x) / row_blocks;
+        const Shares shares(all_pieces<false, kTile, kAllRows>(a, slots), kLeastTiles, n_ctas);
+        const int begin = shares.begin(cta), end = shares.begin(cta + 1);
+        int slot_now = begin < end ? slot_at(slots, a.n_slots, begin) : 0, at = begin;
+        bool joined = false;                     // an item that begins here goes on elsewhere
+        for (uint32_t seq = 0;; ++seq) {
+            const uint32_t place = seq % kQueue;
+            __syncwarp();
+            ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bWorkEmpty + static_cast<int>(place)), ((seq / kQueue) & 1) ^ 1, abort_flag, a.status));
+            if (!ok) break;
+            if (at >= end) {
+                if (lane == 0) {
+                    s_work[place].valid = 0;
+                    arrive_a(bar(C::bWorkFull + static_cast<int>(place)));
+                }
+                break;
+            }
+            const Segment s = segment_at<false, kTile, kAllRows>(a, slots, at, end, slot_now);
+            const int row0 = static_cast<int>(blockIdx.x) % row_blocks * N, n_rows = min(s.n_rows - row0, N);
+            const int part = 2 * static_cast<int>(blockIdx.x) + (at == begin ? 0 : 1);
+            at = s.item_at + s.p_end;
+            if (n_rows <= 0) {                   // (this slot has fewer rows)
+                --seq;
+                continue;
+            }
+            if (lane == 0) {
+                s_work[place] = Work{1, s.slot, s.p_begin, s.p_end, s.w.cache_pieces, s.w.keys, s.w.n, row0, n_rows, s.kvh, s.token0, s.head0,
+                                     s.p_begin == 0 && s.p_end == s.w.pieces ? -1 : part, {}};
+                arrive_a(bar(C::bWorkFull + static_cast<int>(place)));
+                if (s.p_begin == 0 && s.p_end < s.w.pieces) {
+                    a.meta[blockIdx.x] = {part, shares.owner(s.item_at + s.w.pieces - 1) - cta + 1, row_blocks, s.token0, s.head0, row0, n_rows};
+                    joined = true;
+                }
+            }
             const int32_t* list = a.table + static_cast<int64_t>(s.slot) * a.max_pages;
-            const auto page_of = [&](int t) {                          // this lane's page of tile t, -1: none to load
-                const int o = t * per_tile + lane;
-                if (lane >= per_tile || t >= min(s.p_end, s.w.cache_pieces) || static_cast<int64_t>(o) << a.page_shift >= s.w.keys) return -1;
-                const int page = list[o];
-                if (page >= 0 && page < a.n_pages) return page;
-                report(a.status, PULSAR_DEV_BAD_PAGE);                 // (some page is loaded; its rows count as absent)
-                return 0;
+            const auto has_page = [&](int t) {                         // this lane has a page of tile t to load
+                return lane < per_tile && t < min(s.p_end, s.w.cache_pieces) && ((t * per_tile + lane) << a.page_shift) < s.w.keys;
             };
-            int page = page_of(s.p_begin);
+            const auto page_of = [&](int t) { return has_page(t) ? list[t * per_tile + lane] : 0; };
+            int id = page_of(s.p_begin);
             for (int t = s.p_begin; t < s.p_end && ok; ++t) {
-                const int next = page_of(t + 1);
+                const int next = page_of(t + 1);                       // (looked at a tile later)
                 const bool fresh = t >= s.w.cache_pieces;
+                int page = has_page(t) ? id : -1;
+                if (has_page(t) && (id < 0 || id >= a.n_pages)) {
+                    report(a.status, PULSAR_DEV_BAD_PAGE);             // (some page is loaded; its rows count as absent)
+                    page = 0;
+                }
                 const uint32_t pages = __ballot_sync(0xffffffffu, page >= 0);
                 const uint32_t bytes = fresh ? static_cast<uint32_t>(C::kPanels) * kFreshRows * 128 : __popc(pages) * page_bytes;
 #pragma unroll
@@ -226,10 +299,10 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
                         phase ^= 1;
                     }
                 }
-                page = next;
+                id = next;
             }
-            at = s.item_at + s.p_end;
         }
+        if (lane == 0 && !joined) a.meta[blockIdx.x].parts = 0;
     } else if (warp == 1) {
         // ---- matrix instructions: S of a tile, then PV of the tile before it ----
         const bool leader = elect_one();
@@ -238,7 +311,7 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
         const uint64_t desc_v = umma_smem_desc_sw128(smem_u32(smem), kPanelBytes, 1024);
         const uint64_t desc_q = umma_smem_desc_sw128(smem_u32(smem + C::kQ), 16, 1024);
         const uint64_t desc_p = umma_smem_desc_sw128(smem_u32(smem + C::kP), kPanelBytes, 1024);
-        uint32_t tile = 0, n_seg = 0, n_done = 0;          // tiles issued, segments begun, segments finished
+        uint32_t tile = 0, n_done = 0;                     // tiles issued, segments finished
         uint32_t stage = 0, phase = 0;                     // of the next K or V
         bool ok = true, first = false, last = false;       // of the tile whose PV is due
         const auto wait = [&](int b, uint32_t parity) {
@@ -263,11 +336,15 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
             }
             if (last) ++n_done;
         };
-        while (at < share.end && ok) {
-            const Segment s = segment(at);
-            for (int t = s.p_begin; t < s.p_end && ok; ++t, ++tile) {
+        for (uint32_t seq = 0;; ++seq) {
+            const Work* s = next_work(seq, ok);
+            if (!ok || s->valid == 0) break;
+            const int p_begin = s->p_begin, p_end = s->p_end;
+            __syncwarp();
+            if (lane == 0) arrive_a(bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));
+            for (int t = p_begin; t < p_end && ok; ++t, ++tile) {
                 wait(C::bKvFull + static_cast<int>(stage), phase);
-                if (t == s.p_begin) wait(C::bQFull, n_seg & 1);
+                if (t == p_begin) wait(C::bQFull, seq & 1);
                 wait(C::bSEmpty + static_cast<int>(tile & 1), ((tile >> 1) & 1) ^ 1);
                 if (!ok) break;
                 tc_fence_after();
@@ -280,7 +357,7 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
                     }
                     umma_commit_a(bar(C::bSFull + static_cast<int>(tile & 1)));
                     umma_commit_a(bar(C::bKvEmpty + static_cast<int>(stage)));
-                    if (t + 1 == s.p_end) umma_commit_a(bar(C::bQEmpty));
+                    if (t + 1 == p_end) umma_commit_a(bar(C::bQEmpty));
                 }
                 if (++stage == C::kStages) {
                     stage = 0;
@@ -293,51 +370,57 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
                     stage = 0;
                     phase ^= 1;
                 }
-                first = t == s.p_begin;
-                last = t + 1 == s.p_end;
+                first = t == p_begin;
+                last = t + 1 == p_end;
             }
-            ++n_seg;
-            at = s.item_at + s.p_end;
         }
         if (ok && tile > 0) issue_pv(tile - 1);
     } else if (warp < 4) {
         // ---- query rows, ancestors, the nodes' rows to their pages ----
         const int t = threadIdx.x - 64;
         bool ok = true;
-        for (uint32_t seg = 0; at < share.end; ++seg) {
-            const Segment s = segment(at);
-            ok = ok && mbar_wait_a(bar(C::bQEmpty), (seg & 1) ^ 1, abort_flag, a.status);
-            if (named_any(3, 64, !ok)) break;
-            for (int i = t; i < N * (D / 8); i += 64) {
-                const int r = i / (D / 8), v = i % (D / 8);
-                uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                if (r < s.n_rows)
-                    x = reinterpret_cast<const uint4*>(a.Q + row_of(s.token0, s.head0, s.row0, r, a.g_shift, a.Hq) * D)[v];
-                *reinterpret_cast<uint4*>(smem + C::kQ + (v >> 3) * (N * 128) + r * 128 + (((v & 7) ^ (r & 7)) << 4)) = x;
+        for (uint32_t seq = 0;; ++seq) {
+            const Work* work = next_work(seq, ok);
+            ok = ok && mbar_wait_a(bar(C::bQEmpty), (seq & 1) ^ 1, abort_flag, a.status);
+            if (named_any(kRowsBarrier, 64, !ok) || work->valid == 0) break;
+            const Work s = *work;
+            if (t == 0) {                                  // (rows past the item's are other slots', or zeros: nobody reads their outputs)
+                mbar_expect_tx_a(bar(C::bQFull), C::kQBytes);
+#pragma unroll
+                for (int p = 0; p < C::kPanels; ++p)
+                    tma_load_3d_a(smem_u32(smem) + C::kQ + p * (N * 128), &tmQ, bar(C::bQFull), p * 64, s.head0, s.token0 + (s.row0 >> a.g_shift));
             }
-            fence_proxy_async_smem();
-            // The softmax of an item is at most two tiles behind the products that have freed its query rows, and four buffers
-            // hold at least three items after it.
-            const bool has_new = s.p_end > s.w.cache_pieces;
-            if (has_new) ancestors(a, s.slot, s.w.n, t, s_sees + (seg % kSeesBuffers) * kMaxTree, s_up, [] { named_sync(3, 64); });
-            else named_sync(3, 64);
+            // (the place in the queue, and with it these buffers, is free when the softmax has left the segment kQueue before)
+            const bool has_new = s.p_end > s.cache_pieces;
+            if (has_new) {
+                ancestors(a, s.slot, s.n, t, s_sees, s_up, [] { named_sync(kRowsBarrier, 64); });
+                const uint64_t mine = s_sees[t];
+                uint32_t* seen = reinterpret_cast<uint32_t*>(s_seen + (seq % kQueue) * kMaxTree);
+#pragma unroll 8
+                for (int node = 0; node < kMaxTree; ++node) {          // this warp's 32 nodes that see `node`
+                    const uint32_t by = __ballot_sync(0xffffffffu, ((mine >> node) & 1ull) != 0ull);
+                    if (lane == (node & 31)) seen[2 * node + (t >> 5)] = by;
+                }
+            }
+            if (t < 2) s_odd[2 * (seq % kQueue) + t] = 0u;
+            named_sync(kRowsBarrier, 64);
             if (t == 0) {
-                s_odd[2 * (seg % kSeesBuffers)] = s_odd[2 * (seg % kSeesBuffers) + 1] = 0u;
-                arrive_a(bar(C::bQFull));
+                arrive_a(bar(C::bSees + static_cast<int>(seq % kQueue)));
+                arrive_a(bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));         // (both warps have their copy)
             }
             if (has_new && s.row0 == 0) {
                 constexpr int kVecs = D / 8;
                 const int head_at = s.kvh * D;
-                for (int i = t; i < s.w.n * kVecs; i += 64) {
+                const int len = s.keys;
+                for (int i = t; i < s.n * kVecs; i += 64) {
                     const int row = i / kVecs, v = i % kVecs;
-                    const int64_t to = new_row_at(a, s.slot, static_cast<int64_t>(s.w.len) + row, pitch);
+                    const int64_t to = new_row_at(a, s.slot, static_cast<int64_t>(len) + row, pitch);
                     if (to < 0) continue;
                     const int64_t from = (static_cast<int64_t>(s.slot) * a.T + row) * pitch + head_at;
                     reinterpret_cast<uint4*>(a.K + to + head_at)[v] = reinterpret_cast<const uint4*>(a.Knew + from)[v];
                     reinterpret_cast<uint4*>(a.V + to + head_at)[v] = reinterpret_cast<const uint4*>(a.Vnew + from)[v];
                 }
             }
-            at = s.item_at + s.p_end;
         }
     } else {
         // ---- softmax and epilogue ----
@@ -348,44 +431,42 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
         const int tg = threadIdx.x - 128 - group * 128;    // thread of the warpgroup
         uint32_t tile = 0;
         uint32_t v_stage = 1, v_phase = 0;                 // ring place of the tile's V
-        bool ok = true, meta_written = false;
-        for (uint32_t seg = 0; at < share.end; ++seg) {
-            const Segment s = segment(at);
+        bool ok = true;
+        for (uint32_t seg = 0;; ++seg) {
+            const Work& s = *next_work(seg, ok);
+            if (named_any(id, 128, !ok) || s.valid == 0) break;
             const int32_t* list = a.table + static_cast<int64_t>(s.slot) * a.max_pages;
+            const int p_begin = s.p_begin, p_end = s.p_end, cache_pieces = s.cache_pieces, n_rows = s.n_rows;
             float sum[kCols];
 #pragma unroll
             for (int c = 0; c < kCols; ++c) sum[c] = 0.f;
-            if (tg < kCols) s_neg[col0 + tg] = kUnset;
-            if (named_any(id, 128, !ok)) break;
-            const auto page_ok = [&](int t) {              // this thread's key of tile t exists
-                const int64_t row = static_cast<int64_t>(t) * kTile + key;
-                if (t >= min(s.p_end, s.w.cache_pieces) || row >= s.w.keys) return false;
-                const int page = list[row >> a.page_shift];
-                return page >= 0 && page < a.n_pages;
+            const auto page_of = [&](int t) {              // the page of this thread's key of tile t, -1: there is no such key
+                const int row = t * kTile + key;
+                return t < min(p_end, cache_pieces) && row < s.keys ? list[row >> a.page_shift] : -1;
             };
-            bool here = page_ok(s.p_begin);
+            int page = page_of(p_begin);
             bool failed = false;
-            for (int t = s.p_begin; t < s.p_end; ++t, ++tile) {
-                const bool next = page_ok(t + 1);
-                const bool fresh = t >= s.w.cache_pieces;
-                if (fresh) here = key < s.w.n;
+            for (int t = p_begin; t < p_end; ++t, ++tile) {
+                const int next = page_of(t + 1);           // (looked at a tile later)
+                const bool fresh = t >= cache_pieces;
+                const bool here = fresh ? key < s.n : page >= 0 && page < a.n_pages;
                 const uint32_t tS = tmem + (tile & 1) * N + col0 + my_lanes;
                 __syncwarp();
                 ok = ok && mbar_wait_a(bar(C::bSFull + static_cast<int>(tile & 1)), (tile >> 1) & 1, abort_flag, a.status);
                 tc_fence_after();
-                uint64_t visible = ~0ull;                  // columns that see this key
+                uint32_t visible = ~0u;                    // columns that see this key
                 if (fresh) {
-                    visible = 0ull;
-                    if (here) {
-                        const uint64_t* sees = s_sees + (seg % kSeesBuffers) * kMaxTree;
-#pragma unroll 4
-                        for (int c = 0; c < kCols; ++c)
-                            if (col0 + c < s.n_rows) visible |= ((sees[(s.row0 + col0 + c) >> a.g_shift] >> key) & 1ull) << c;
-                    }
+                    __syncwarp();
+                    ok = ok && mbar_wait_a(bar(C::bSees + static_cast<int>(seg % kQueue)), (seg / kQueue) & 1, abort_flag, a.status);
+                    const int gs = a.g_shift, per = 1 << gs;
+                    const uint64_t seen = here ? s_seen[(seg % kQueue) * kMaxTree + key] >> ((s.row0 + col0) >> gs) : 0ull;
+                    visible = 0u;                          // every node's bit becomes the bits of its rows
+                    for (int c = 0; c < kCols; c += per)
+                        if (((seen >> (c >> gs)) & 1ull) != 0ull) visible |= (per == 32 ? ~0u : (1u << per) - 1u) << c;
                 } else if (!here) {
-                    visible = 0ull;
+                    visible = 0u;
                 }
-                const bool masked = fresh || __any_sync(0xffffffffu, visible != ~0ull);
+                const bool masked = fresh || __any_sync(0xffffffffu, visible != ~0u);
                 float x[kCols];
                 // x = logits (log2 units) minus the maximum in use
                 const auto logits = [&]() {
@@ -394,7 +475,7 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
                     if (masked) {
 #pragma unroll
                         for (int c = 0; c < kCols; ++c)
-                            if (((visible >> c) & 1ull) == 0ull) x[c] = -INFINITY;
+                            if (((visible >> c) & 1u) == 0u) x[c] = -INFINITY;
                     }
                 };
                 const auto below = [&]() {
@@ -402,15 +483,21 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
 #pragma unroll
                     for (int c = 0; c < kCols; c += 4) {
                         const float4 neg = *reinterpret_cast<const float4*>(s_neg + col0 + c);
-                        x[c] = fmaf(x[c], a.scale_log2, neg.x);
-                        x[c + 1] = fmaf(x[c + 1], a.scale_log2, neg.y);
-                        x[c + 2] = fmaf(x[c + 2], a.scale_log2, neg.z);
-                        x[c + 3] = fmaf(x[c + 3], a.scale_log2, neg.w);
-                        most = max3(most, fmaxf(x[c], x[c + 1]), fmaxf(x[c + 2], x[c + 3]));
+                        fma2(x[c], x[c + 1], a.scale_log2, neg.x, neg.y);
+                        fma2(x[c + 2], x[c + 3], a.scale_log2, neg.z, neg.w);
+                        most = max3(max3(most, x[c], x[c + 1]), x[c + 2], x[c + 3]);
                     }
                     return most;
                 };
                 logits();
+                if (t == p_begin) {
+                    // To begin with, a column's maximum is its logit at the tile's first key, if it sees that key.
+                    if (tg == 0) {
+#pragma unroll
+                        for (int c = 0; c < kCols; ++c) s_neg[col0 + c] = x[c] > -INFINITY ? x[c] * -a.scale_log2 : kUnset;
+                    }
+                    named_sync(id, 128);
+                }
                 if (named_any(id, 128, below() > kRescale || !ok)) {
                     // ---- the maximum moves ----
                     __syncwarp();
@@ -438,7 +525,7 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
                     named_sync(id, 128);
 #pragma unroll
                     for (int c = 0; c < kCols; ++c) sum[c] *= s_alpha[col0 + c];
-                    if (t > s.p_begin) {
+                    if (t > p_begin) {
 #pragma unroll 1
                         for (int c0 = 0; c0 < kCols; c0 += 16) {
                             uint32_t o[16];
@@ -460,17 +547,16 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
 #pragma unroll
                 for (int c = 0; c < kCols; c += 2) {
                     const float p0 = ex2(x[c]), p1 = ex2(x[c + 1]);
-                    sum[c] += p0;
-                    sum[c + 1] += p1;
+                    add2(sum[c], sum[c + 1], p0, p1);
                     p[c / 2] = pack_bf16x2(p0, p1);
                 }
                 // P^T: a line of 64 rows per key, where the product before has been read
                 __syncwarp();
                 ok = ok && mbar_wait_a(bar(C::bPEmpty), (tile & 1) ^ 1, abort_flag, a.status);
-                uint8_t* line = smem + C::kP + group * kPanelBytes + key * 128;
+                uint8_t* line = smem + C::kP + (group >> 1) * kPanelBytes + key * 128;
 #pragma unroll
                 for (int v = 0; v < kCols / 8; ++v)
-                    *reinterpret_cast<uint4*>(line + ((v ^ (key & 7)) << 4)) = make_uint4(p[4 * v], p[4 * v + 1], p[4 * v + 2], p[4 * v + 3]);
+                    *reinterpret_cast<uint4*>(line + (((v + (group & 1) * 4) ^ (key & 7)) << 4)) = make_uint4(p[4 * v], p[4 * v + 1], p[4 * v + 2], p[4 * v + 3]);
                 if (masked && group == 0) {
                     // Rows of V that do not exist may hold anything, and 0 * NaN is NaN: they become zeros.  So does a node's value
                     // that is not finite: nodes that do not see it have weight 0.  The epilogue adds it where it is seen.
@@ -482,7 +568,7 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
                         uint32_t odd = 0;
 #pragma unroll
                         for (int v = 0; v < D / 8; ++v) {
-                            const uint4 y = *reinterpret_cast<const uint4*>(value + (v >> 3) * kPanelBytes + ((v & 7) << 4));
+                            const uint4 y = *reinterpret_cast<const uint4*>(value + (v >> 3) * kPanelBytes + (((v ^ key) & 7) << 4));
                             const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
@@ -490,13 +576,13 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
                         }
                         if (odd != 0u) {
                             clear = true;
-                            atomicOr(&s_odd[2 * (seg % kSeesBuffers) + (key >> 5)], 1u << (key & 31));
+                            atomicOr(&s_odd[2 * (seg % kQueue) + (key >> 5)], 1u << (key & 31));
                         }
                     }
                     if (clear) {
 #pragma unroll
                         for (int v = 0; v < D / 8; ++v)
-                            *reinterpret_cast<uint4*>(value + (v >> 3) * kPanelBytes + ((v & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                            *reinterpret_cast<uint4*>(value + (v >> 3) * kPanelBytes + (((v ^ key) & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
                     }
                 }
                 fence_proxy_async_smem();
@@ -508,38 +594,34 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
                     v_stage -= C::kStages;
                     v_phase ^= 1;
                 }
-                here = next;
+                page = next;
             }
             if (failed) break;
 
             // ---- sums over the keys, and the item's outputs: a thread per component ----
             column_sums<kCols>(sum, lane);
-            if constexpr (kCols == 64) {
-                s_col[quarter * N + col0 + 2 * lane] = sum[0];
-                s_col[quarter * N + col0 + 2 * lane + 1] = sum[1];
-            } else if constexpr (kCols == 32) {
+            if constexpr (kCols == 32) {
                 s_col[quarter * N + col0 + lane] = sum[0];
             } else {
                 if ((lane & 1) == 0) s_col[quarter * N + col0 + (lane >> 1)] = sum[0];
             }
             named_sync(id, 128);
-            const bool whole = s.p_begin == 0 && s.p_end == s.w.pieces;
-            const int64_t part = 2 * static_cast<int64_t>(blockIdx.x) + (at == share.begin ? 0 : 1);
+            const bool whole = s.part < 0;
             if (tg < kCols) {
                 const int c = col0 + tg;
                 const float total = (s_col[c] + s_col[N + c]) + (s_col[2 * N + c] + s_col[3 * N + c]);
                 s_inv[c] = total == 0.f ? 0.f : 1.f / total;
                 const float lse = total == 0.f ? -INFINITY : (log2f(total) - s_neg[c]) * 0.6931471805599453f;
-                if (c < s.n_rows) {
-                    if (!whole) a.part_LSE[part * N + c] = lse;
-                    else if (a.LSE != nullptr) a.LSE[row_of(s.token0, s.head0, s.row0, c, a.g_shift, a.Hq)] = lse;
-                }
+                const int64_t row = whole ? row_of(s.token0, s.head0, s.row0, c, a.g_shift, a.Hq) : static_cast<int64_t>(s.part) * N + c;
+                s_to[c] = row * D;
+                float* to_lse = whole ? a.LSE : a.part_LSE;
+                if (c < n_rows && to_lse != nullptr) to_lse[row] = lse;
             }
             __syncwarp();
             ok = ok && mbar_wait_a(bar(C::bOFull), seg & 1, abort_flag, a.status);
             if (named_any(id, 128, !ok)) break;
             tc_fence_after();
-            const uint64_t odd = s_odd[2 * (seg % kSeesBuffers)] | static_cast<uint64_t>(s_odd[2 * (seg % kSeesBuffers) + 1]) << 32;
+            const uint64_t odd = p_end <= cache_pieces ? 0ull : s_odd[2 * (seg % kQueue)] | static_cast<uint64_t>(s_odd[2 * (seg % kQueue) + 1]) << 32;
 #pragma unroll 1
             for (int c0 = 0; c0 < kCols; c0 += 16) {
                 uint32_t r[16];
@@ -552,44 +634,35 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
                 for (int c = 0; c < 16; ++c) o[c] = __uint_as_float(r[c]);
                 for (uint64_t left = odd; left != 0ull; left &= left - 1ull) {
                     const int node = __ffsll(static_cast<long long>(left)) - 1;
-                    const uint64_t* sees = s_sees + (seg % kSeesBuffers) * kMaxTree;
+                    const uint64_t seen = s_seen[(seg % kQueue) * kMaxTree + node];
                     const float v = __uint_as_float(static_cast<uint32_t>(a.Vnew[(static_cast<int64_t>(s.slot) * a.T + node) * pitch + s.kvh * D + key]) << 16);
-                    const uint8_t* line = smem + C::kP + group * kPanelBytes + node * 128;
+                    const uint8_t* line = smem + C::kP + (group >> 1) * kPanelBytes + node * 128;
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
                         const int col = c0 + c;
-                        if (col0 + col >= s.n_rows || ((sees[(s.row0 + col0 + col) >> a.g_shift] >> node) & 1ull) == 0ull) continue;
-                        const uint32_t p = *reinterpret_cast<const uint16_t*>(line + (((col >> 3) ^ (node & 7)) << 4) + (col & 7) * 2);
+                        if (((seen >> ((s.row0 + col0 + col) >> a.g_shift)) & 1ull) == 0ull) continue;
+                        const uint32_t p = *reinterpret_cast<const uint16_t*>(line + ((((col >> 3) + (group & 1) * 4) ^ (node & 7)) << 4) + (col & 7) * 2);
                         o[c] = fmaf(__uint_as_float(p << 16), v, o[c]);
                     }
                 }
+                const int n = min(16, n_rows - (col0 + c0));
+                float* to_f = whole ? static_cast<float*>(a.O) : a.part_O;
+                if (!whole || a.out_f32) {
 #pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    const int col = col0 + c0 + c;
-                    if (col >= s.n_rows) break;
-                    const float y = o[c] * s_inv[col];
-                    if (!whole) {
-                        a.part_O[(part * N + col) * D + key] = y;
-                        continue;
-                    }
-                    const int64_t row = row_of(s.token0, s.head0, s.row0, col, a.g_shift, a.Hq);
-                    if (a.out_f32) static_cast<float*>(a.O)[row * D + key] = y;
-                    else static_cast<__nv_bfloat16*>(a.O)[row * D + key] = __float2bfloat16_rn(y);
+                    for (int c = 0; c < 16; ++c)
+                        if (c < n) to_f[s_to[col0 + c0 + c] + key] = o[c] * s_inv[col0 + c0 + c];
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 16; ++c)
+                        if (c < n) static_cast<__nv_bfloat16*>(a.O)[s_to[col0 + c0 + c] + key] = __float2bfloat16_rn(o[c] * s_inv[col0 + c0 + c]);
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_a(bar(C::bOEmpty));
-            if (s.p_begin == 0 && s.p_end < s.w.pieces) {
-                if (threadIdx.x == 128) {
-                    const int64_t end = ((s.item_at + s.w.pieces) * share.n_ctas - 1) / share.total;
-                    a.meta[blockIdx.x] = {static_cast<int>(part), static_cast<int>(end - blockIdx.x) + 1, s.token0, s.head0, s.row0, s.n_rows};
-                }
-                meta_written = true;
-            }
-            at = s.item_at + s.p_end;
+            __syncwarp();
+            if (lane == 0) arrive_a(bar(C::bWorkEmpty + static_cast<int>(seg % kQueue)));
         }
-        if (share.begin < share.end && !meta_written && threadIdx.x == 128) a.meta[blockIdx.x].parts = 0;
     }
 
     tc_fence_before();
@@ -603,83 +676,49 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
     if (warp == 1) tmem_dealloc(tmem, C::kTmemCols);
 }
 
-// Joins the parts of the items that several CTAs share, a warp per row (see paged.cu for the form with few rows and many parts).
-template <int D>
-__global__ void __launch_bounds__(256)
-tiles_merge_kernel(const Meta* __restrict__ meta, const float* __restrict__ part_O, const float* __restrict__ part_LSE, int n, int g_shift, int Hq,
-                   void* O, int out_f32, float* LSE) {
-    constexpr int kPer = D / 32;
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const Meta x = meta[blockIdx.x];
-    const int r = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (x.parts < 2 || r >= x.rows) return;
-    const auto slot_of = [&](int j) { return j == 0 ? x.first : 2 * (static_cast<int>(blockIdx.x) + j); };
-    float m = -INFINITY;
-    for (int j = lane; j < x.parts; j += 32) m = fmaxf(m, part_LSE[static_cast<int64_t>(slot_of(j)) * n + r]);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    float acc[kPer] = {}, total = 0.f;
-    if (m > -INFINITY) {
-#pragma unroll 8
-        for (int j = 0; j < x.parts; ++j) {
-            const int64_t at = static_cast<int64_t>(slot_of(j)) * n + r;
-            const float w = ex2((part_LSE[at] - m) * 1.4426950408889634f);
-            total += w;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) acc[i] = fmaf(w, part_O[at * D + i * 32 + lane], acc[i]);
-        }
-    }
-    const float inv = total > 0.f ? 1.f / total : 0.f;
-    const int64_t row = row_of(x.token0, x.head0, x.row0, r, g_shift, Hq);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        if (out_f32) static_cast<float*>(O)[row * D + i * 32 + lane] = acc[i] * inv;
-        else static_cast<__nv_bfloat16*>(O)[row * D + i * 32 + lane] = __float2bfloat16_rn(acc[i] * inv);
-    }
-    if (lane == 0 && LSE != nullptr) LSE[row] = total > 0.f ? m + logf(total) : -INFINITY;
-}
-
-int item_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+int item_rows(int rows) { return rows <= 16 ? 16 : std::min((rows + 31) / 32 * 32, 128); }
 
 template <int D, int N>
-int32_t launch(const PagedArgs& a, const CUtensorMap (&map)[4], cudaStream_t stream) {
+int32_t launch(const PagedArgs& a, const CUtensorMap (&map)[5], int rows, cudaStream_t stream) {
     using C = Cfg<D, N>;
     const unsigned ctas = static_cast<unsigned>(sm_count());
     PULSAR_CUDA_OK(cudaFuncSetAttribute(tree_tiles_kernel<D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
-    PULSAR_CUDA_OK(launch_kernel(tree_tiles_kernel<D, N>, dim3(ctas), dim3(C::kThreads), C::kSmem, stream, true, a, map[0], map[1], map[2], map[3]));
+    PULSAR_CUDA_OK(launch_kernel(tree_tiles_kernel<D, N>, dim3(ctas), dim3(C::kThreads), C::kSmem, stream, true, a, map[0], map[1], map[2], map[3],
+                                 map[4], (rows + N - 1) / N));
     count_launch();
-    PULSAR_CUDA_OK(launch_kernel(tiles_merge_kernel<D>, dim3(ctas, N / 8), dim3(256), 0, stream, true, a.meta, a.part_O, a.part_LSE, N, a.g_shift, a.Hq,
-                                 a.O, a.out_f32, a.LSE));
-    count_launch();
-    return PULSAR_OK;
+    return launch_parts_merge(a, ctas, N, D, stream);
 }
 
 }  // namespace
+
+bool tree_tiles_ok(int64_t n_slots, int64_t Hkv, int64_t keys, int64_t T) { return pieces_ok(n_slots, Hkv, keys, T, kTile); }
 
 size_t tree_tiles_workspace_bytes(int rows, int d) { return PartScratch(sm_count(), item_rows(rows), d).total; }
 
 int32_t launch_tree_tiles(PagedArgs a, int rows, int d, void* workspace, cudaStream_t stream) {
     const int n = item_rows(rows);
     PartScratch(sm_count(), n, d).place(a, workspace);
-    CUtensorMap map[4];
+    CUtensorMap map[5];
     const int64_t pool_rows = static_cast<int64_t>(a.n_pages) << a.page_shift, fresh_rows = static_cast<int64_t>(a.n_slots) * a.T;
     if (!make_map_3d(&map[0], a.K, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) || !make_map_3d(&map[1], a.V, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) ||
-        !make_map_3d(&map[2], a.Knew, fresh_rows, a.Hkv, d, 1, kFreshRows) || !make_map_3d(&map[3], a.Vnew, fresh_rows, a.Hkv, d, 1, kFreshRows))
+        !make_map_3d(&map[2], a.Knew, fresh_rows, a.Hkv, d, 1, kFreshRows) || !make_map_3d(&map[3], a.Vnew, fresh_rows, a.Hkv, d, 1, kFreshRows) ||
+        !make_map_3d(&map[4], a.Q, fresh_rows, a.Hq, d, 1 << a.g_shift, n >> a.g_shift))
         return PULSAR_ERR_CUDA;
     if (d == 128) {
         switch (n) {
-            case 16: return launch<128, 16>(a, map, stream);
-            case 32: return launch<128, 32>(a, map, stream);
-            case 64: return launch<128, 64>(a, map, stream);
-            default: return launch<128, 128>(a, map, stream);
+            case 16: return launch<128, 16>(a, map, rows, stream);
+            case 32: return launch<128, 32>(a, map, rows, stream);
+            case 64: return launch<128, 64>(a, map, rows, stream);
+            case 96: return launch<128, 96>(a, map, rows, stream);
+            default: return launch<128, 128>(a, map, rows, stream);
         }
     }
     switch (n) {
-        case 16: return launch<64, 16>(a, map, stream);
-        case 32: return launch<64, 32>(a, map, stream);
-        case 64: return launch<64, 64>(a, map, stream);
-        default: return launch<64, 128>(a, map, stream);
+        case 16: return launch<64, 16>(a, map, rows, stream);
+        case 32: return launch<64, 32>(a, map, rows, stream);
+        case 64: return launch<64, 64>(a, map, rows, stream);
+        case 96: return launch<64, 96>(a, map, rows, stream);
+        default: return launch<64, 128>(a, map, rows, stream);
     }
 }
 

@@ -381,178 +381,445 @@ paged_rows_kernel(const __grid_constant__ PagedArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// Scores of the full pages and the k best.  Keys are the scores' bit patterns in an order that compares like the numbers.
+// Scores of the full pages and the k best.
+//
+// sum_j (q_j > 0 ? q_j max_j : q_j min_j) is one product of length 2 d: the negative parts of the query with the smallest components, the
+// positive ones with the largest.  The tensor cores form it for all pages and rows in fp32, which is what the memory's rate leaves
+// time for (in float64 on the FMA pipe 16 slots of 45,000 rows took 70 us); the ranking is that of the float64 scores all the
+// same: a page whose fp32 score lies further from the k-th than both can be off is in or out, and the few others are formed again in
+// float64.
 // ---------------------------------------------------------------------------------------------
-constexpr uint64_t kForced = ~0ull;
-constexpr int kScorePages = 128;                // pages of a CTA, a thread each
-__device__ __forceinline__ uint64_t order_key(double x) {
-    if (x != x) x = -INFINITY;
-    const uint64_t b = static_cast<uint64_t>(__double_as_longlong(x + 0.0));      // (-0 counts as 0)
-    return b >> 63 ? ~b : b | (1ull << 63);
-}
+constexpr int kScoreThreads = 128, kScorePages = 64;     // of a CTA: 16 pages per warp
+constexpr int kScoreRows = 32;                           // query rows in shared memory at a time
 
 struct SelectArgs {
     const uint16_t *Q, *summary;
     const int32_t *table, *len, *n_draft;
     int T, Hq, Hkv, g_shift, page_shift, n_pages, max_pages, k, sink, window;
-    uint64_t* keys;                              // [n_slots, T, Hkv, max_pages]
+    float* score;                                // [n_slots, T, Hkv, max_pages] in fp32
+    uint64_t* exact;                             // [n_slots, T, Hkv, max_pages] of the pages that are ranked in float64
+    float* most;                                 // [n_slots, Hkv, blocks of kScorePages pages] largest magnitude of a bound
     int32_t *sel, *list;                         // [n_slots, T, Hkv, k], [n_slots, T, Hkv, k + 1]
     int32_t* status;
 };
 
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float c;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(a), "f"(b));
+    return c;
+}
+__device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {     // of two bf16 each; NaN counts as nothing
+    uint32_t c;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(c) : "r"(a), "r"(b & 0x7fff7fffu));
+    return c;
+}
+
 template <int D>
-__global__ void __launch_bounds__(kScorePages)
+__global__ void __launch_bounds__(kScoreThreads)
 page_score_kernel(const __grid_constant__ SelectArgs a) {
-    __shared__ double s_q[4][D];
-    const int slot = blockIdx.z, kvh = blockIdx.y, b = blockIdx.x * kScorePages + threadIdx.x;
+    constexpr int kChunks = 2 * D / 32;          // of 32 products: a lane has 8 consecutive ones, 16 bytes, of two pages
+    constexpr int kPitch = 2 * D + 32;           // of a query row in shared memory: two rows' vectors fill the banks
+    __shared__ __align__(16) uint16_t s_q[kScoreRows * kPitch];
+    __shared__ float s_most[kScoreThreads / 32];
+    const int slot = blockIdx.z, kvh = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
     grid_dependency_wait();
     grid_launch_dependents();
     const int len = checked_len(a.len[slot], static_cast<int64_t>(a.max_pages) << a.page_shift, false, nullptr);
-    const int full = len >> a.page_shift;
-    if (full <= a.k || static_cast<int>(blockIdx.x) * kScorePages >= full) return;      // (all pages are taken as they are)
-    const int n = a.n_draft != nullptr ? min(max(a.n_draft[slot], 0), a.T) : a.T, g = 1 << a.g_shift;
-    const bool forced = b < a.sink || b >= full - a.window;
-    int page = -1;
-    if (b < full) {
-        page = a.table[static_cast<int64_t>(slot) * a.max_pages + b];
-        if (page < 0 || page >= a.n_pages) {
-            report(a.status, PULSAR_DEV_BAD_PAGE);
-            page = -1;
-        }
+    const int full = len >> a.page_shift, b0 = blockIdx.x * kScorePages;
+    if (full <= a.k || b0 >= full) return;       // (all pages are taken as they are)
+    const int n = a.n_draft != nullptr ? min(max(a.n_draft[slot], 0), a.T) : a.T, g = 1 << a.g_shift, rows = n * g;
+    if (rows == 0) return;
+
+    // ---- the bounds of pages gid and gid + 8 of the warp's 16, as A fragments: products are summed in the order of these vectors ----
+    uint4 f[2][kChunks];
+    bool known[2];
+    const int page0 = b0 + warp * 16 + gid;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int b = page0 + 8 * h;
+        const int page = b < full ? a.table[static_cast<int64_t>(slot) * a.max_pages + b] : -1;
+        known[h] = page >= 0 && page < a.n_pages;
+        if (b < full && !known[h] && tig == 0) report(a.status, PULSAR_DEV_BAD_PAGE);
+        const uint4* src = reinterpret_cast<const uint4*>(a.summary + (static_cast<int64_t>(known[h] ? page : 0) * a.Hkv + kvh) * 2 * D) + tig;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) f[h][c] = known[h] ? src[4 * c] : make_uint4(0u, 0u, 0u, 0u);
     }
-    const uint4* low = reinterpret_cast<const uint4*>(a.summary + (static_cast<int64_t>(max(page, 0)) * a.Hkv + kvh) * 2 * D);
-    const uint4* high = low + D / 8;
-    double best = -INFINITY;
-    for (int r0 = 0; r0 < n * g; r0 += 4) {                             // four query rows (token, head of the group) at a time
-        __syncthreads();
-        for (int i = threadIdx.x; i < 4 * D; i += kScorePages) {
-            const int r = r0 + i / D, j = i % D;
-            double x = 0.0;
-            if (r < n * g)
-                x = static_cast<double>(__uint_as_float(static_cast<uint32_t>(
-                        a.Q[(static_cast<int64_t>(slot * a.T + (r >> a.g_shift)) * a.Hq + (kvh << a.g_shift) + (r & (g - 1))) * D + j]) << 16));
-            s_q[i / D][j] = x;
-        }
-        __syncthreads();
-        double acc[4] = {0.0, 0.0, 0.0, 0.0};
-        if (page >= 0 && !forced) {
-#pragma unroll 2
-            for (int v = 0; v < D / 8; ++v) {
-                const uint4 x = low[v], y = high[v];
-                const uint32_t lo[4] = {x.x, x.y, x.z, x.w}, hi[4] = {y.x, y.y, y.z, y.w};
+    {
+        uint32_t m = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const double l = static_cast<double>(__uint_as_float(j & 1 ? lo[j >> 1] & 0xffff0000u : lo[j >> 1] << 16));
-                    const double h = static_cast<double>(__uint_as_float(j & 1 ? hi[j >> 1] & 0xffff0000u : hi[j >> 1] << 16));
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const double q = s_q[i][v * 8 + j];
-                        acc[i] = fma(q, q > 0.0 ? h : l, acc[i]);
-                    }
-                }
+            for (int c = 0; c < kChunks; ++c)
+                m = max_abs2(max_abs2(max_abs2(max_abs2(m, f[h][c].x), f[h][c].y), f[h][c].z), f[h][c].w);
+        float most = fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        if (lane == 0) s_most[warp] = most;
+    }
+    float best[2];                               // g = 16: of the row tile before
+    for (int r0 = 0; r0 < rows; r0 += kScoreRows) {
+        __syncthreads();
+        if (r0 == 0 && threadIdx.x == 0)
+            a.most[(static_cast<int64_t>(slot) * a.Hkv + kvh) * gridDim.x + blockIdx.x] = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
+        for (int i = threadIdx.x; i < kScoreRows * (D / 2); i += kScoreThreads) {
+            const int r = i / (D / 2), j = i % (D / 2);
+            uint32_t x = 0, up = 0;
+            if (r0 + r < rows) {
+                x = reinterpret_cast<const uint32_t*>(a.Q + row_of(slot * a.T, kvh << a.g_shift, r0, r, a.g_shift, a.Hq) * D)[j];
+                up = (__uint_as_float(x << 16) > 0.f ? 0xffffu : 0u) | (__uint_as_float(x & 0xffff0000u) > 0.f ? 0xffff0000u : 0u);
             }
+            uint32_t* to = reinterpret_cast<uint32_t*>(s_q + r * kPitch);
+            to[j] = x & ~up;
+            to[D / 2 + j] = x & up;
         }
+        __syncthreads();
+        for (int t = 0; t < min(kScoreRows, rows - r0); t += 8) {
+            float c[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};       // two chains of products
+            const uint4* src = reinterpret_cast<const uint4*>(s_q + (t + gid) * kPitch) + tig;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = r0 + i;
-            if (r >= n * g) break;
-            const double x = acc[i] == acc[i] ? acc[i] : -INFINITY;
-            best = (r & (g - 1)) == 0 ? x : fmax(best, x);
-            if ((r & (g - 1)) == g - 1 && b < full)
-                a.keys[(static_cast<int64_t>(slot * a.T + (r >> a.g_shift)) * a.Hkv + kvh) * a.max_pages + b] =
-                    forced ? kForced : order_key(page >= 0 ? best : -INFINITY);
+            for (int i = 0; i < kChunks; ++i) {
+                const uint4 q = src[4 * i];
+                const uint32_t lo[4] = {f[0][i].x, f[1][i].x, f[0][i].y, f[1][i].y}, hi[4] = {f[0][i].z, f[1][i].z, f[0][i].w, f[1][i].w};
+                mma_bf16(c, lo, q.x, q.y);
+                mma_bf16(c2, hi, q.z, q.w);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float x = c[2 * h] + c2[2 * h], y = c[2 * h + 1] + c2[2 * h + 1];  // rows r0 + t + 2 tig and the next
+                const int b = page0 + 8 * h, r = r0 + t + 2 * tig;
+                const auto put = [&](int row, float z) {
+                    if (b < full && row < rows)
+                        a.score[(static_cast<int64_t>(slot * a.T + (row >> a.g_shift)) * a.Hkv + kvh) * a.max_pages + b] = known[h] ? z : -INFINITY;
+                };
+                if (g == 1) {
+                    put(r, x);
+                    put(r + 1, y);
+                    continue;
+                }
+                x = max_nan(x, y);
+                if (g >= 4) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, 1));
+                if (g >= 8) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, 2));
+                if (g == 16) {
+                    if ((t & 8) == 0) {
+                        best[h] = x;
+                        continue;
+                    }
+                    x = max_nan(x, best[h]);
+                }
+                if ((2 * tig & (min(g, 8) - 1)) == 0) put(r, x);
+            }
         }
     }
 }
 
+// The score of a page for one KV head's queries in float64, as a number whose order is the scores'.  A warp together; s_q: [g][D].
+__device__ __forceinline__ uint64_t order_key(double x) {
+    if (x != x) x = -INFINITY;
+    const uint64_t b = static_cast<uint64_t>(__double_as_longlong(x + 0.0));      // (-0 counts as 0)
+    return b >> 63 ? ~b : b | (1ull << 63);
+}
+template <int D>
+__device__ __forceinline__ uint64_t exact_score(const SelectArgs& a, const float* s_q, int g, int page, int kvh) {
+    if (page < 0 || page >= a.n_pages) return order_key(-INFINITY);
+    constexpr int kPer = D / 32;
+    const int lane = threadIdx.x & 31;
+    const uint16_t* src = a.summary + (static_cast<int64_t>(page) * a.Hkv + kvh) * 2 * D;
+    double low[kPer], high[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        low[i] = static_cast<double>(__uint_as_float(static_cast<uint32_t>(src[i * 32 + lane]) << 16));
+        high[i] = static_cast<double>(__uint_as_float(static_cast<uint32_t>(src[D + i * 32 + lane]) << 16));
+    }
+    double best = -INFINITY;
+    for (int h = 0; h < g; ++h) {
+        double x = 0.0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const double q = static_cast<double>(s_q[h * D + i * 32 + lane]);
+            x = fma(q, q > 0.0 ? high[i] : low[i], x);
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        best = x > best ? x : best;              // (a NaN never is)
+    }
+    return order_key(best);
+}
+
 constexpr int kTopThreads = 512, kTopWarps = kTopThreads / 32;
+constexpr int kBins = 2 * kTopThreads;
+constexpr int kTopHeld = 8;                      // scores that a thread holds; more are read again
+constexpr int kNear = 256;                       // pages that are ranked in float64 within shared memory
+// How far an fp32 score can be off, as a share of the sum of the products' magnitudes: 2 d / 16 = 16 matrix instructions (d = 128), each
+// of which rounds a sum of 17 terms that are no larger than that; 2^-20 for each is several times what fp32 sums lose.
+constexpr float kScoreError = 1.f / 65536.f;
+
+struct TopScratch {
+    int bins[kBins];
+    float q[16 * 128];
+    float value[kTopWarps];
+    int count[2][kTopWarps];
+    uint64_t near_key[kNear], cut_key;
+    int near_at[kNear], n_near, cut_at, bin, above;
+    int odd;                                     // a score that is not finite
+};
+
+// Largest (or smallest: of the negated values) over the CTA.
+__device__ __forceinline__ float block_max(float x, float* s) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = s[threadIdx.x & (kTopWarps - 1)];
+#pragma unroll
+    for (int d = kTopWarps / 2; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+    return x;
+}
+// Of two flags: how many threads before this one have them, and how many in all.
+__device__ __forceinline__ void block_counts(const bool (&flag)[2], int (&before)[2], int (&all)[2], int (&s)[2][kTopWarps]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t m[2] = {__ballot_sync(0xffffffffu, flag[0]), __ballot_sync(0xffffffffu, flag[1])};
+    __syncthreads();
+    if (lane < 2) s[lane][warp] = __popc(m[lane]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = s[i][lane & (kTopWarps - 1)];
+        int x = lane < warp ? c : 0, y = lane < kTopWarps ? c : 0;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            x += __shfl_xor_sync(0xffffffffu, x, d);
+            y += __shfl_xor_sync(0xffffffffu, y, d);
+        }
+        before[i] = x + __popc(m[i] & ((1u << lane) - 1u));
+        all[i] = y;
+    }
+}
+
+template <int D>
 __global__ void __launch_bounds__(kTopThreads)
-page_select_kernel(const __grid_constant__ SelectArgs a) {
-    __shared__ int s_hist[256], s_gt[kTopWarps], s_eq[kTopWarps];
-    __shared__ int s_bin, s_left;
+page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
+    __shared__ TopScratch s;
     const int row = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    const int token0 = row / a.Hkv, slot = token0 / a.T, u = token0 - slot * a.T;
+    const int token0 = row / a.Hkv, kvh = row - token0 * a.Hkv, slot = token0 / a.T, u = token0 - slot * a.T, g = 1 << a.g_shift;
     grid_dependency_wait();
     grid_launch_dependents();
     const int len = checked_len(a.len[slot], static_cast<int64_t>(a.max_pages) << a.page_shift, false, nullptr);
     const int full = len >> a.page_shift, k = min(a.k, full);
     if (a.n_draft != nullptr && u >= a.n_draft[slot]) return;
-    const uint64_t* keys = a.keys + static_cast<int64_t>(row) * a.max_pages;
+    const float* score = a.score + static_cast<int64_t>(row) * a.max_pages;
+    uint64_t* exact = a.exact + static_cast<int64_t>(row) * a.max_pages;
     int32_t* sel = a.sel + static_cast<int64_t>(row) * a.k;
     int32_t* list = a.list + static_cast<int64_t>(row) * (a.k + 1);
     const int32_t* table = a.table + static_cast<int64_t>(slot) * a.max_pages;
 
-    // ---- the k-th largest key, a byte at a time; `left`: how many of those equal to it are taken ----
-    uint64_t kth = 0, known = 0;                 // known: the bits of kth that are settled
-    int left = k;
-    if (full > a.k) {
-        for (int shift = 56; shift >= 0; shift -= 8) {
-            for (int i = t; i < 256; i += kTopThreads) s_hist[i] = 0;
-            __syncthreads();
-            for (int b = t; b < full; b += kTopThreads) {
-                const uint64_t x = keys[b];
-                if ((x & known) == kth) atomicAdd(&s_hist[(x >> shift) & 255], 1);
+    // Pages [first, last) are ranked, `want` of them taken; those before and after are taken anyway.
+    const bool all = full <= a.k;
+    const int first = min(a.sink, full), last = max(first, full - a.window), want = all ? 0 : k - first - (full - last);
+    const bool ranked = !all && want > 0;
+    float held[kTopHeld], above = INFINITY, below = INFINITY;      // scores over `above` are taken, under `below` not, the others ranked
+    const auto at = [&](int i) { return first + t + i * kTopThreads; };
+    const int rounds = (last - first + kTopThreads - 1) / kTopThreads;
+    const auto value = [&](int i) { return at(i) < last ? score[at(i)] : -INFINITY; };
+    if (ranked) {
+        float lo = INFINITY, hi = -INFINITY;
+        bool odd = false;
+        if (t == 0) {
+            s.odd = 0;
+            s.n_near = 0;
+        }
+        for (int i = t; i < kBins; i += kTopThreads) s.bins[i] = 0;
+        const auto look = [&](float x) {
+            odd |= !(x < INFINITY);
+            if (x > -INFINITY) {
+                lo = fminf(lo, x);
+                hi = fmaxf(hi, x);
             }
-            __syncthreads();
-            if (warp == 0) {                     // lane i: bins 255 - 8 i .. 248 - 8 i, from the largest down
-                int mine[8], sum = 0;
+        };
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    mine[i] = s_hist[255 - 8 * lane - i];
-                    sum += mine[i];
-                }
-                int before = sum;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const int z = __shfl_up_sync(0xffffffffu, before, d);
-                    if (lane >= d) before += z;
-                }
-                before -= sum;
-                if (before < left && before + sum >= left) {
-                    int i = 0;
-                    while (before + mine[i] < left) before += mine[i++];
-                    s_bin = 255 - 8 * lane - i;
-                    s_left = left - before;
-                }
+        for (int i = 0; i < kTopHeld; ++i) held[i] = value(i);
+        float q1 = 0.f;                           // sums of the queries' magnitudes, a warp per head
+        for (int h = warp; h < g; h += kTopWarps) {
+            float x = 0.f;
+            for (int j = lane; j < D; j += 32) {
+                const float q = __uint_as_float(static_cast<uint32_t>(a.Q[(static_cast<int64_t>(token0) * a.Hq + (kvh << a.g_shift) + h) * D + j]) << 16);
+                s.q[h * D + j] = q;
+                x += fabsf(q);
             }
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+            q1 = fmaxf(q1, x != x ? INFINITY : x);
+        }
+        float most = 0.f;
+        for (int i = t; i < (full + kScorePages - 1) / kScorePages; i += kTopThreads)
+            most = fmaxf(most, a.most[(static_cast<int64_t>(slot) * a.Hkv + kvh) * blocks + i]);
+#pragma unroll
+        for (int i = 0; i < kTopHeld; ++i) look(held[i]);
+        for (int i = kTopHeld; i < rounds; ++i) look(value(i));
+        lo = -block_max(-lo, s.value);
+        hi = block_max(hi, s.value);
+        const float size = block_max(q1, s.value) * block_max(most, s.value);
+        if (odd) s.odd = 1;
+        __syncthreads();
+        const bool rough = s.odd != 0 || !(size < 1e37f) || !(hi > lo);      // fp32 says nothing: all are ranked in float64
+        if (!rough) {
+            // ---- the bin of the want-th largest score ----
+            const float inv = kBins / (hi - lo);
+            const auto bin_of = [&](float x) { return min(max(static_cast<int>((x - lo) * inv), 0), kBins - 1); };
+#pragma unroll
+            for (int i = 0; i < kTopHeld; ++i)
+                if (at(i) < last) atomicAdd(&s.bins[bin_of(held[i])], 1);
+            for (int i = kTopHeld; i < rounds; ++i)
+                if (at(i) < last) atomicAdd(&s.bins[bin_of(value(i))], 1);
             __syncthreads();
-            kth |= static_cast<uint64_t>(s_bin) << shift;
-            known |= 255ull << shift;
-            left = s_left;
+            const int top = kBins - 1 - 2 * t, n0 = s.bins[top], n1 = s.bins[top - 1];       // a thread's two, from the largest down
+            int x = n0 + n1;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, x, d);
+                if (lane >= d) x += y;
+            }
+            if (lane == 31) s.count[0][warp] = x;
+            __syncthreads();
+            int over = x - n0 - n1;
+            for (int w = 0; w < warp; ++w) over += s.count[0][w];
+            if (over < want && over + n0 + n1 >= want) s.bin = over + n0 >= want ? top : top - 1;
+            __syncthreads();
+            const int bin = s.bin;
+            float in_lo = INFINITY, in_hi = -INFINITY;                       // smallest and largest score in it
+            const auto inside = [&](int i, float v) {
+                if (at(i) < last && bin_of(v) == bin) {
+                    in_lo = fminf(in_lo, v);
+                    in_hi = fmaxf(in_hi, v);
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < kTopHeld; ++i) inside(i, held[i]);
+            for (int i = kTopHeld; i < rounds; ++i) inside(i, value(i));
+            const float e = 2.f * kScoreError * size;
+            in_lo = -block_max(-in_lo, s.value);
+            in_hi = block_max(in_hi, s.value);
+            above = nextafterf(in_hi + e, INFINITY);                         // (outward: the sums are rounded)
+            below = nextafterf(in_lo - e, -INFINITY);
+        } else {
+            below = -INFINITY;                    // (`above` is infinite)
         }
     }
-    // ---- pages in ascending order: larger keys, and the first `left` equal ones ----
-    int done = 0, done_eq = 0;
+    const auto is_near = [&](float x) { return !(x > above) && !(x < below); };
+
+    // ---- pages between the two borders are ranked in float64 ----
+    if (ranked) {
+        int taken = 0;
+        const auto sort_out = [&](int i, float x) {
+            if (at(i) >= last) return;
+            if (is_near(x)) {
+                const int n = atomicAdd(&s.n_near, 1);
+                if (n < kNear) s.near_at[n] = at(i);
+            } else if (x > above) {
+                ++taken;
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < kTopHeld; ++i) sort_out(i, held[i]);
+        for (int i = kTopHeld; i < rounds; ++i) sort_out(i, value(i));
+        taken = static_cast<int>(__reduce_add_sync(0xffffffffu, taken));
+        __syncthreads();
+        if (lane == 0) s.count[0][warp] = taken;
+        __syncthreads();
+        int left = want;                          // pages to take from those in between
+        for (int w = 0; w < kTopWarps; ++w) left -= s.count[0][w];
+        const int n_near = s.n_near;
+        if (n_near <= kNear) {
+            for (int i = warp; i < n_near; i += kTopWarps) {
+                const int b = s.near_at[i];
+                const uint64_t key = exact_score<D>(a, s.q, g, table[b], kvh);
+                if (lane == 0) {
+                    s.near_key[i] = key;
+                    exact[b] = key;
+                }
+            }
+            __syncthreads();
+            if (t < n_near) {
+                const uint64_t key = s.near_key[t];
+                const int b = s.near_at[t];
+                int before = 0;
+                for (int i = 0; i < n_near; ++i) before += s.near_key[i] > key || (s.near_key[i] == key && s.near_at[i] < b) ? 1 : 0;
+                if (before == left - 1) {
+                    s.cut_key = key;
+                    s.cut_at = b;
+                }
+            }
+            __syncthreads();
+        } else {
+            for (int b = first + warp; b < last; b += kTopWarps)
+                if (is_near(score[b])) {
+                    const uint64_t key = exact_score<D>(a, s.q, g, table[b], kvh);
+                    if (lane == 0) exact[b] = key;
+                }
+            // the left-th largest key, a byte at a time
+            uint64_t kth = 0, settled = 0;
+            for (int shift = 56; shift >= 0; shift -= 8) {
+                __syncthreads();
+                for (int i = t; i < 256; i += kTopThreads) s.bins[i] = 0;
+                __syncthreads();
+                for (int b = first + t; b < last; b += kTopThreads)
+                    if (is_near(score[b])) {
+                        const uint64_t x = exact[b];
+                        if ((x & settled) == kth) atomicAdd(&s.bins[(x >> shift) & 255], 1);
+                    }
+                __syncthreads();
+                if (t == 0) {
+                    int bin = 255, over = 0;
+                    while (over + s.bins[bin] < left) over += s.bins[bin--];
+                    s.bin = bin;
+                    s.above = over;
+                }
+                __syncthreads();
+                kth |= static_cast<uint64_t>(s.bin) << shift;
+                settled |= 255ull << shift;
+                left -= s.above;
+            }
+            // and the left-th page of those that have it
+            int done = 0;
+            for (int b0 = first; b0 < last; b0 += kTopThreads) {
+                const int b = b0 + t;
+                const bool flag[2] = {b < last && is_near(score[b]) && exact[b] == kth, false};
+                int before[2], total[2];
+                block_counts(flag, before, total, s.count);
+                if (flag[0] && done + before[0] == left - 1) {
+                    s.cut_key = kth;
+                    s.cut_at = b;
+                }
+                done += total[0];
+            }
+            __syncthreads();
+        }
+    }
+
+    // ---- the taken pages in ascending order ----
+    const uint64_t cut_key = ranked ? s.cut_key : 0;
+    const int cut_at = ranked ? s.cut_at : 0;
+    int done = 0;
     for (int b0 = 0; b0 < full; b0 += kTopThreads) {
         const int b = b0 + t;
-        const uint64_t x = b < full && full > a.k ? keys[b] : 0;
-        const bool gt = b < full && (full <= a.k || x > kth), eq = b < full && full > a.k && x == kth;
-        const uint32_t gts = __ballot_sync(0xffffffffu, gt), eqs = __ballot_sync(0xffffffffu, eq);
-        __syncthreads();
-        if (lane == 0) {
-            s_gt[warp] = __popc(gts);
-            s_eq[warp] = __popc(eqs);
-        }
-        __syncthreads();
-        int n_gt = 0, n_eq = 0, all_gt = 0, all_eq = 0;
-        for (int w = 0; w < kTopWarps; ++w) {
-            if (w < warp) {
-                n_gt += s_gt[w];
-                n_eq += s_eq[w];
+        bool take = b < full && (all || b < first || b >= last);
+        if (ranked && b >= first && b < last) {
+            const float x = score[b];
+            if (!is_near(x)) {
+                take = x > above;
+            } else {
+                const uint64_t key = exact[b];
+                take = key > cut_key || (key == cut_key && b <= cut_at);
             }
-            all_gt += s_gt[w];
-            all_eq += s_eq[w];
         }
-        const uint32_t lower = (1u << lane) - 1u;
-        n_gt += __popc(gts & lower);
-        n_eq += __popc(eqs & lower);
-        if (gt || (eq && done_eq + n_eq < left)) {
-            const int at = done + n_gt + min(done_eq + n_eq, left) - min(done_eq, left);
-            sel[at] = b;
-            list[at] = table[b];
+        const bool flag[2] = {take, false};
+        int before[2], total[2];
+        block_counts(flag, before, total, s.count);
+        if (take) {
+            sel[done + before[0]] = b;
+            list[done + before[0]] = table[b];
         }
-        done += all_gt + min(done_eq + all_eq, left) - min(done_eq, left);
-        done_eq += all_eq;
+        done += total[0];
     }
     for (int i = k + t; i < a.k; i += kTopThreads) sel[i] = -1;
     if (t == 0 && len > full << a.page_shift) list[k] = table[full];      // the page of the rows after the last full one
@@ -647,10 +914,13 @@ extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, con
 
 namespace {
 struct SparseScratch {
-    size_t keys, list, total;
-    SparseScratch(int64_t rows, int64_t max_pages, int64_t k, int d) {
-        keys = rows_scratch(d).total;
-        list = round_up(keys + static_cast<size_t>(rows * max_pages) * 8, 256);
+    size_t exact, score, most, list, total;
+    SparseScratch(int64_t n_slots, int64_t T, int64_t Hkv, int64_t max_pages, int64_t k, int d) {
+        const int64_t rows = n_slots * T * Hkv;
+        exact = rows_scratch(d).total;
+        score = round_up(exact + static_cast<size_t>(rows * max_pages) * 8, 256);
+        most = round_up(score + static_cast<size_t>(rows * max_pages) * 4, 256);
+        list = round_up(most + static_cast<size_t>(n_slots * Hkv * ((max_pages + kScorePages - 1) / kScorePages)) * 4, 256);
         total = round_up(list + static_cast<size_t>(rows * (k + 1)) * 4, 256);
     }
 };
@@ -663,7 +933,7 @@ bool sparse_ok(int32_t n_slots, int32_t T, int32_t k, int32_t Hq, int32_t Hkv, i
 extern "C" size_t pulsar_sparse_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t max_pages, int32_t k, int32_t Hq, int32_t Hkv,
                                                      int32_t d) {
     if (!sparse_ok(n_slots, T, k, Hq, Hkv, d) || max_pages < 1) return 0;
-    return SparseScratch(static_cast<int64_t>(n_slots) * T * Hkv, max_pages, k, d).total;
+    return SparseScratch(n_slots, T, Hkv, max_pages, k, d).total;
 }
 
 extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, const uint16_t* Vnew, int32_t T, uint16_t* K_pages,
@@ -685,7 +955,7 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
     if (!aligned(page_table, 4) || !aligned(cache_len, 4) || !aligned(n_draft, 4) || !aligned(LSE, 4) || !aligned(sel, 4) || !aligned(workspace, 256))
         return PULSAR_ERR_ALIGNMENT;
     const int64_t rows = static_cast<int64_t>(n_slots) * T * Hkv;
-    const SparseScratch y(rows, max_pages, k, d);
+    const SparseScratch y(n_slots, T, Hkv, max_pages, k, d);
     if (workspace_bytes < y.total) return PULSAR_ERR_WORKSPACE;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
     auto* ws = static_cast<uint8_t*>(workspace);
@@ -707,14 +977,18 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
     b.k = k;
     b.sink = sink;
     b.window = window;
-    b.keys = reinterpret_cast<uint64_t*>(ws + y.keys);
+    b.exact = reinterpret_cast<uint64_t*>(ws + y.exact);
+    b.score = reinterpret_cast<float*>(ws + y.score);
+    b.most = reinterpret_cast<float*>(ws + y.most);
     b.sel = sel;
     b.list = reinterpret_cast<int32_t*>(ws + y.list);
     b.status = device_status;
-    PULSAR_CUDA_OK(launch_kernel(d == 128 ? page_score_kernel<128> : page_score_kernel<64>,
-                                 dim3((max_pages + kScorePages - 1) / kScorePages, Hkv, n_slots), dim3(kScorePages), 0, st, true, b));
+    const int blocks = (max_pages + kScorePages - 1) / kScorePages;
+    PULSAR_CUDA_OK(launch_kernel(d == 128 ? page_score_kernel<128> : page_score_kernel<64>, dim3(blocks, Hkv, n_slots), dim3(kScoreThreads), 0, st,
+                                 true, b));
     count_launch();
-    PULSAR_CUDA_OK(launch_kernel(page_select_kernel, dim3(static_cast<unsigned>(rows)), dim3(kTopThreads), 0, st, true, b));
+    PULSAR_CUDA_OK(launch_kernel(d == 128 ? page_select_kernel<128> : page_select_kernel<64>, dim3(static_cast<unsigned>(rows)), dim3(kTopThreads), 0,
+                                 st, true, b, blocks));
     count_launch();
 
     PagedArgs a{};

@@ -163,3 +163,32 @@ def test_captured_step_follows_the_lengths_on_the_device():
         O, LSE, A, want = R.sparse_attn(Q.cpu(), Kn.cpu(), Vn.cpu(), c, bounds, k, 1, 1)
         assert torch.equal(sel.cpu(), want)
         R.check(out, lse, (O, LSE, A), str(lens))
+
+
+def test_scores_that_are_equal_infinite_or_far_apart_everywhere():
+    """What the fp32 scores cannot tell: all equal, more equal ones at the border than are kept at hand, and sizes beyond fp32."""
+    c = R.Cache([16 * 900 + 1], 16, 1, 64, room=1)
+    Q, Kn, Vn, _ = drafts(1, 1, 4, 1, 64)
+    g = torch.Generator().manual_seed(5)
+    bounds = R.page_bounds(torch.where(c.K.isnan(), torch.zeros_like(c.K), c.K))
+    run(c, Q, Kn, Vn, 40, 1, 1, bounds=torch.ones_like(bounds))
+    two = torch.where(torch.rand(c.n_pages, 1, 1, 1, generator=g) < 0.5, 1.0, 0.0).expand_as(bounds).to(BF).contiguous()
+    run(c, Q, Kn, Vn, 700, 0, 3, bounds=two)
+    huge = (bounds.float() * 1e37).to(BF)
+    run(c, (Q.float() * 1e3).to(BF), Kn, Vn, 33, bounds=huge, scale=1e-6)
+    tiny = (bounds.float() * 1e-38).to(BF)
+    run(c, Q, Kn, Vn, 33, bounds=tiny)
+    some = bounds.clone()
+    some[c.table[0, 7:300:13].long()] = float("nan")
+    run(c, Q, Kn, Vn, 33, 2, 2, bounds=some)
+
+
+@pytest.mark.parametrize("T,Hq,Hkv", [(40, 8, 2), (9, 16, 1), (33, 1, 1)])
+def test_more_query_rows_than_a_tile(T, Hq, Hkv):
+    c = R.Cache([16 * 80 + 9, 16 * 130], 16, Hkv, 128, room=T)
+    run(c, *drafts(2, T, Hq, Hkv, 128)[:3], 7, 1, 2)
+
+
+def test_more_pages_than_a_thread_block_holds():
+    c = R.Cache([16 * 5000 + 3], 16, 1, 64, room=1)
+    run(c, *drafts(1, 1, 2, 1, 64)[:3], 50, 1, 2)

@@ -12,8 +12,9 @@ LIB = os.path.join(HERE, "libpulsar.so")
 NATIVE = os.path.join(HERE, "_native.so")
 NATIVE_SOURCE = os.path.join(CSRC, "binding.cpp")
 NATIVE_KEY = os.path.join(HERE, "build", "_native.key")     # what NATIVE was compiled against
-SOURCES = ["api.cu", "select.cu", "merge.cu", "attn.cu", "decode.cu", "rope.cu", "pages.cu", "paged.cu", "paged_tiles.cu", "paged_merge.cu"]
-HEADERS = [os.path.join(CSRC, h) for h in ("common.cuh", "decode.cuh", "mma.cuh", "paged.cuh", "tensor_map.cuh")]
+SOURCES = ["api.cu", "select.cu", "merge.cu", "attn.cu", "decode.cu", "rope.cu", "pages.cu", "paged.cu", "paged_tiles.cu", "paged_wide.cu",
+           "paged_merge.cu"]
+HEADERS = [os.path.join(CSRC, h) for h in ("common.cuh", "decode.cuh", "mma.cuh", "paged.cuh", "paged_roles.cuh", "tensor_map.cuh")]
 HEADERS.append(os.path.join(os.path.dirname(HERE), "include", "pulsar.h"))
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",

@@ -1,0 +1,247 @@
+// What the tensor-core kernels for drafted trees share: the loader of the pages, and the warps that fetch query rows, work out which
+// node sees which and write the nodes' rows to their pages.  A kernel's configuration C has its shared-memory layout, its barriers
+// and its tile sizes.
+#pragma once
+
+#include "paged.cuh"
+#include "tensor_map.cuh"
+
+namespace pulsar {
+
+constexpr int kTile = 128;                       // keys
+constexpr int kPanelBytes = kTile * 128;         // 64 columns of a tile: 128-byte lines, swizzled
+constexpr int kFreshRows = 64;                   // rows of the nodes' own tile that are loaded
+constexpr float kRescale = 8.f;                  // in log2 units
+constexpr float kUnset = 1e30f;                  // stands for minus a maximum that no logit has set: every logit exceeds it
+constexpr int kLeastTiles = 2;                   // of a CTA, unless all CTAs have fewer
+constexpr int kRowsBarrier = 5;                  // named barriers: 1 .. 4 of the softmax warpgroups, this one of warps 2 and 3
+constexpr int kAllRows = 1 << 20;                // (the rows of an item are cut up between CTAs, not between items)
+constexpr int kQueue = 4;                        // segments that the loader may publish ahead of the slowest consumer
+
+// A CTA's pieces of one item, as the loader publishes them.
+struct __align__(16) Work {
+    int valid;                                   // 0: no more
+    int slot, p_begin, p_end, cache_pieces;
+    int keys, n, row0, n_rows, kvh, token0, head0;
+    int part;                                    // place of the partial, -1: all of the item, its outputs are final
+    int pad_[3];
+};
+static_assert(sizeof(Work) == 64, "");
+
+// Barriers of some warps (whole ones: their lanes come together first).
+__device__ __forceinline__ void named_sync(int id, int threads) {
+    __syncwarp();
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+// Whether any of the barrier's threads says so; the threads wait for each other.
+__device__ __forceinline__ bool named_any(int id, int threads, bool x) {
+    uint32_t y;
+    __syncwarp();
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 q, %1, 0;\n\t"
+        "bar.red.or.pred p, %2, %3, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(y) : "r"(x ? 1u : 0u), "r"(id), "r"(threads) : "memory");
+    return y != 0;
+}
+__device__ __forceinline__ void arrive_a(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+// Two fused multiply-adds (x * s + y), two sums, with one instruction each.
+__device__ __forceinline__ void fma2(float& x0, float& x1, float s, float y0, float y1) {
+    asm("{\n\t.reg .b64 a, b, c;\n\t"
+        "mov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %2};\n\tmov.b64 c, {%3, %4};\n\t"
+        "fma.rn.f32x2 a, a, b, c;\n\t"
+        "mov.b64 {%0, %1}, a;\n\t}"
+        : "+f"(x0), "+f"(x1) : "f"(s), "f"(y0), "f"(y1));
+}
+__device__ __forceinline__ void add2(float& x0, float& x1, float y0, float y1) {
+    asm("{\n\t.reg .b64 a, b;\n\t"
+        "mov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %3};\n\t"
+        "add.rn.f32x2 a, a, b;\n\t"
+        "mov.b64 {%0, %1}, a;\n\t}"
+        : "+f"(x0), "+f"(x1) : "f"(y0), "f"(y1));
+}
+
+// Trees with more than 64 query rows per KV head (paged_wide.cu).  map: K and V of the pool, of the nodes, and Q.
+int32_t launch_tree_wide(const PagedArgs& a, const CUtensorMap (&map)[5], int rows, int d, cudaStream_t stream);
+
+// Shared memory that the roles use besides the tiles, and where the barriers are.
+struct Roles {
+    uint8_t* smem;
+    Work* s_work;                                // [kQueue]
+    uint64_t* s_sees;                            // [kQueue][kMaxTree] a node's ancestors and itself (C::kBySeen: the nodes that see it)
+    uint32_t* s_odd;                             // [kQueue][2] nodes whose value is not finite
+    int* s_up;                                   // [kMaxTree]
+    Slots* slots;
+    uint32_t bar0;
+    volatile int* abort_flag;
+    __device__ __forceinline__ uint32_t bar(int i) const { return bar0 + 8 * static_cast<uint32_t>(i); }
+};
+
+// The next published segment (a warp's lanes together); `ok` turns false where a wait has given up.
+template <class C>
+__device__ __forceinline__ const Work* next_work(const PagedArgs& a, const Roles& r, uint32_t seq, bool& ok) {
+    __syncwarp();
+    ok = __all_sync(0xffffffffu, ok && mbar_wait_a(r.bar(C::bWorkFull + static_cast<int>(seq % kQueue)), (seq / kQueue) & 1, r.abort_flag, a.status));
+    return r.s_work + seq % kQueue;
+}
+
+// ---- loader (one warp): shares out the work, and every lane copies a page ----
+template <class C>
+__device__ __forceinline__ void load_role(const PagedArgs& a, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmKn, const CUtensorMap& tmVn,
+                                          int row_blocks, const Roles& roles) {
+    const int lane = threadIdx.x & 31;
+    uint8_t* smem = roles.smem;
+    Work* s_work = roles.s_work;
+    Slots& slots = *roles.slots;
+    volatile int* abort_flag = roles.abort_flag;
+    const auto bar = [&](int i) { return roles.bar(i); };
+    uint32_t stage = 0, phase = 0;
+    bool ok = true;
+    const int per_tile = kTile >> a.page_shift;
+    const uint32_t page_bytes = static_cast<uint32_t>(C::kPanels) << (a.page_shift + 7);
+    // More rows than a CTA takes: neighbouring CTAs have the same keys at the same time, and a share of the rows each.
+    const int cta = static_cast<int>(blockIdx.x) / row_blocks, n_ctas = static_cast<int>(gridDim.x) / row_blocks;
+    const Shares shares(all_pieces<false, kTile, kAllRows>(a, slots), kLeastTiles, n_ctas);
+    const int begin = shares.begin(cta), end = shares.begin(cta + 1);
+    int slot_now = begin < end ? slot_at(slots, a.n_slots, begin) : 0, at = begin;
+    bool joined = false;                     // an item that begins here goes on elsewhere
+    for (uint32_t seq = 0;; ++seq) {
+        const uint32_t place = seq % kQueue;
+        __syncwarp();
+        ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bWorkEmpty + static_cast<int>(place)), ((seq / kQueue) & 1) ^ 1, abort_flag, a.status));
+        if (!ok) break;
+        if (at >= end) {
+            if (lane == 0) {
+                s_work[place].valid = 0;
+                arrive_a(bar(C::bWorkFull + static_cast<int>(place)));
+            }
+            break;
+        }
+        const Segment s = segment_at<false, kTile, kAllRows>(a, slots, at, end, slot_now);
+        const int row0 = static_cast<int>(blockIdx.x) % row_blocks * C::kRows, n_rows = min(s.n_rows - row0, C::kRows);
+        const int part = 2 * static_cast<int>(blockIdx.x) + (at == begin ? 0 : 1);
+        at = s.item_at + s.p_end;
+        if (n_rows <= 0) {                   // (this slot has fewer rows)
+            --seq;
+            continue;
+        }
+        if (lane == 0) {
+            s_work[place] = Work{1, s.slot, s.p_begin, s.p_end, s.w.cache_pieces, s.w.keys, s.w.n, row0, n_rows, s.kvh, s.token0, s.head0,
+                                 s.p_begin == 0 && s.p_end == s.w.pieces ? -1 : part, {}};
+            arrive_a(bar(C::bWorkFull + static_cast<int>(place)));
+            if (s.p_begin == 0 && s.p_end < s.w.pieces) {
+                a.meta[blockIdx.x] = {part, shares.owner(s.item_at + s.w.pieces - 1) - cta + 1, row_blocks, s.token0, s.head0, row0, n_rows};
+                joined = true;
+            }
+        }
+        const int32_t* list = a.table + static_cast<int64_t>(s.slot) * a.max_pages;
+        const auto has_page = [&](int t) {                         // this lane has a page of tile t to load
+            return lane < per_tile && t < min(s.p_end, s.w.cache_pieces) && ((t * per_tile + lane) << a.page_shift) < s.w.keys;
+        };
+        const auto page_of = [&](int t) { return has_page(t) ? list[t * per_tile + lane] : 0; };
+        int id = page_of(s.p_begin);
+        for (int t = s.p_begin; t < s.p_end && ok; ++t) {
+            const int next = page_of(t + 1);                       // (looked at a tile later)
+            const bool fresh = t >= s.w.cache_pieces;
+            int page = has_page(t) ? id : -1;
+            if (has_page(t) && (id < 0 || id >= a.n_pages)) {
+                report(a.status, PULSAR_DEV_BAD_PAGE);             // (some page is loaded; its rows count as absent)
+                page = 0;
+            }
+            const uint32_t pages = __ballot_sync(0xffffffffu, page >= 0);
+            const uint32_t bytes = fresh ? static_cast<uint32_t>(C::kPanels) * kFreshRows * 128 : __popc(pages) * page_bytes;
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                __syncwarp();
+                ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bKvEmpty + stage), phase ^ 1, abort_flag, a.status));
+                if (!ok) break;
+                const uint32_t full = bar(C::bKvFull + stage), dst = smem_u32(smem) + stage * C::kTileBytes;
+                if (lane == 0) mbar_expect_tx_a(full, bytes);
+                __syncwarp();
+#pragma unroll
+                for (int p = 0; p < C::kPanels; ++p) {
+                    if (fresh) {
+                        if (lane == 0) tma_load_3d_a(dst + p * kPanelBytes, kv ? &tmVn : &tmKn, full, p * 64, s.kvh, s.slot * a.T);
+                    } else if (page >= 0) {
+                        tma_load_3d_a(dst + p * kPanelBytes + (lane << (a.page_shift + 7)), kv ? &tmV : &tmK, full, p * 64, s.kvh,
+                                      page << a.page_shift);
+                    }
+                }
+                if (++stage == C::kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+            id = next;
+        }
+    }
+    if (lane == 0 && !joined) a.meta[blockIdx.x].parts = 0;
+}
+
+// ---- two warps: query rows (TMA), which nodes see which, the nodes' rows to their pages ----
+template <int D, class C>
+__device__ __forceinline__ void rows_role(const PagedArgs& a, const CUtensorMap& tmQ, int t, const Roles& roles) {
+    const int lane = threadIdx.x & 31;
+    uint8_t* smem = roles.smem;
+    uint64_t* s_sees = roles.s_sees;
+    uint32_t* s_odd = roles.s_odd;
+    int* s_up = roles.s_up;
+    volatile int* abort_flag = roles.abort_flag;
+    const int64_t pitch = static_cast<int64_t>(a.Hkv) * D;
+    const auto bar = [&](int i) { return roles.bar(i); };
+    bool ok = true;
+    for (uint32_t seq = 0;; ++seq) {
+        const Work* work = next_work<C>(a, roles, seq, ok);
+        ok = ok && mbar_wait_a(bar(C::bQEmpty), (seq & 1) ^ 1, abort_flag, a.status);
+        if (named_any(kRowsBarrier, 64, !ok) || work->valid == 0) break;
+        const Work s = *work;
+        if (t == 0) {                                  // (rows past the item's are other slots', or zeros: nobody reads their outputs)
+            mbar_expect_tx_a(bar(C::bQFull), C::kQBytes);
+#pragma unroll
+            for (int i = 0; i < C::kQTiles; ++i)
+#pragma unroll
+                for (int p = 0; p < C::kPanels; ++p)
+                    tma_load_3d_a(smem_u32(smem) + C::kQ + (i * C::kPanels + p) * (C::kQRows * 128), &tmQ, bar(C::bQFull), p * 64, s.head0,
+                                  s.token0 + ((s.row0 + i * C::kQRows) >> a.g_shift));
+        }
+        // (the place in the queue, and with it these buffers, is free when the softmax has left the segment kQueue before)
+        const bool has_new = s.p_end > s.cache_pieces;
+        if (has_new) {
+            uint64_t* sees = s_sees + (seq % kQueue) * kMaxTree;
+            ancestors(a, s.slot, s.n, t, sees, s_up, [] { named_sync(kRowsBarrier, 64); });
+            if (C::kBySeen) {                                      // turned round: the nodes that see a node
+                const uint64_t mine = sees[t];
+                uint32_t* seen = reinterpret_cast<uint32_t*>(sees);
+                named_sync(kRowsBarrier, 64);
+#pragma unroll 8
+                for (int node = 0; node < kMaxTree; ++node) {      // this warp's 32 nodes that see `node`
+                    const uint32_t by = __ballot_sync(0xffffffffu, ((mine >> node) & 1ull) != 0ull);
+                    if (lane == (node & 31)) seen[2 * node + (t >> 5)] = by;
+                }
+            }
+        }
+        if (t < 2) s_odd[2 * (seq % kQueue) + t] = 0u;
+        named_sync(kRowsBarrier, 64);
+        if (t == 0) {
+            arrive_a(bar(C::bSees + static_cast<int>(seq % kQueue)));
+            arrive_a(bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));         // (both warps have their copy)
+        }
+        if (has_new && s.row0 == 0) {
+            constexpr int kVecs = D / 8;
+            const int head_at = s.kvh * D;
+            const int len = s.keys;
+            for (int i = t; i < s.n * kVecs; i += 64) {
+                const int row = i / kVecs, v = i % kVecs;
+                const int64_t to = new_row_at(a, s.slot, static_cast<int64_t>(len) + row, pitch);
+                if (to < 0) continue;
+                const int64_t from = (static_cast<int64_t>(s.slot) * a.T + row) * pitch + head_at;
+                reinterpret_cast<uint4*>(a.K + to + head_at)[v] = reinterpret_cast<const uint4*>(a.Knew + from)[v];
+                reinterpret_cast<uint4*>(a.V + to + head_at)[v] = reinterpret_cast<const uint4*>(a.Vnew + from)[v];
+            }
+        }
+    }
+}
+
+}  // namespace pulsar

@@ -15,32 +15,11 @@
 #include <algorithm>
 
 #include "mma.cuh"
-#include "paged.cuh"
-#include "tensor_map.cuh"
+#include "paged_roles.cuh"
 
 namespace pulsar {
 
 namespace {
-
-constexpr int kTile = 128;                       // keys
-constexpr int kPanelBytes = kTile * 128;         // 64 columns of a tile: 128-byte lines, swizzled
-constexpr int kFreshRows = 64;                   // rows of the nodes' own tile that are loaded
-constexpr float kRescale = 8.f;                  // in log2 units
-constexpr float kUnset = 1e30f;                  // stands for minus a maximum that no logit has set: every logit exceeds it
-constexpr int kLeastTiles = 2;                   // of a CTA, unless all CTAs have fewer
-constexpr int kRowsBarrier = 5;                  // named barriers: 1 .. 4 of the softmax warpgroups, this one of warps 2 and 3
-constexpr int kAllRows = 1 << 20;                // (the rows of an item are cut up between CTAs, not between items)
-constexpr int kQueue = 4;                        // segments that the loader may publish ahead of the slowest consumer
-
-// A CTA's pieces of one item, as the loader publishes them.
-struct __align__(16) Work {
-    int valid;                                   // 0: no more
-    int slot, p_begin, p_end, cache_pieces;
-    int keys, n, row0, n_rows, kvh, token0, head0;
-    int part;                                    // place of the partial, -1: all of the item, its outputs are final
-    int pad_[3];
-};
-static_assert(sizeof(Work) == 64, "");
 
 template <int D, int N>
 struct Cfg {
@@ -50,9 +29,11 @@ struct Cfg {
     static constexpr int kGroups = N / kCols;                    // softmax warpgroups
     static constexpr int kSoftWarps = 4 * kGroups;
     static constexpr int kThreads = 128 + 128 * kGroups;
+    static constexpr int kRows = N, kQTiles = 1, kQRows = N;
+    static constexpr bool kBySeen = true;
     static constexpr int kPBytes = (N + 63) / 64 * kPanelBytes;
     static constexpr int kQBytes = kPanels * N * 128;
-    static constexpr int kMisc = static_cast<int>(sizeof(Slots)) + 12 + (kQueue + 1) * kMaxTree * 8 + kQueue * (8 + 64) + 64 * 8 + 7 * N * 4 + N * 8 +
+    static constexpr int kMisc = static_cast<int>(sizeof(Slots)) + 12 + kQueue * kMaxTree * 8 + kQueue * (8 + 64) + 64 * 8 + 7 * N * 4 + N * 8 +
                                  kMaxTree * 4 + 8;
     static constexpr int kFit = (232448 - kPBytes - kQBytes - kMisc) / kTileBytes;
     static constexpr int kStages = kFit < 10 ? kFit : 10;
@@ -69,41 +50,6 @@ struct Cfg {
                          kBars = bWorkEmpty + kQueue;
     static_assert(kBars <= 64 && kStages >= 3, "");
 };
-
-// Barriers of some warps (whole ones: their lanes come together first).
-__device__ __forceinline__ void named_sync(int id, int threads) {
-    __syncwarp();
-    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-}
-// Whether any of the barrier's threads says so; the threads wait for each other.
-__device__ __forceinline__ bool named_any(int id, int threads, bool x) {
-    uint32_t y;
-    __syncwarp();
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.u32 q, %1, 0;\n\t"
-        "bar.red.or.pred p, %2, %3, q;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(y) : "r"(x ? 1u : 0u), "r"(id), "r"(threads) : "memory");
-    return y != 0;
-}
-__device__ __forceinline__ void arrive_a(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-
-// Two fused multiply-adds (x * s + y), two sums, with one instruction each.
-__device__ __forceinline__ void fma2(float& x0, float& x1, float s, float y0, float y1) {
-    asm("{\n\t.reg .b64 a, b, c;\n\t"
-        "mov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %2};\n\tmov.b64 c, {%3, %4};\n\t"
-        "fma.rn.f32x2 a, a, b, c;\n\t"
-        "mov.b64 {%0, %1}, a;\n\t}"
-        : "+f"(x0), "+f"(x1) : "f"(s), "f"(y0), "f"(y1));
-}
-__device__ __forceinline__ void add2(float& x0, float& x1, float y0, float y1) {
-    asm("{\n\t.reg .b64 a, b;\n\t"
-        "mov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %3};\n\t"
-        "add.rn.f32x2 a, a, b;\n\t"
-        "mov.b64 {%0, %1}, a;\n\t}"
-        : "+f"(x0), "+f"(x1) : "f"(y0), "f"(y1));
-}
 
 // Columns [0, C) of TMEM, 32 lanes per warp.
 template <int C>
@@ -156,8 +102,7 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* rest = smem + C::kRest;
     uint64_t* s_seen = reinterpret_cast<uint64_t*>(rest);                              // [kQueue][kMaxTree] the nodes that see a node
-    uint64_t* s_sees = s_seen + kQueue * kMaxTree;                                     // [kMaxTree] a node's ancestors and itself
-    Work* s_work = reinterpret_cast<Work*>(s_sees + kMaxTree);                         // [kQueue]
+    Work* s_work = reinterpret_cast<Work*>(s_seen + kQueue * kMaxTree);                // [kQueue]
     uint64_t* bars = reinterpret_cast<uint64_t*>(s_work + kQueue);                     // [64]
     float* s_col = reinterpret_cast<float*>(bars + 64);                                // [4][N] of each warp's keys: largest logits, sums
     float* s_neg = s_col + 4 * N;                                                      // [N] minus the maximum in use
@@ -213,96 +158,10 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
     tc_fence_after();
     const uint32_t tmem = *tmem_ptr, tO = tmem + 2 * N;
     const int64_t pitch = static_cast<int64_t>(a.Hkv) * D;
-    // The next published segment (a warp's lanes together); false at the end.
-    const auto next_work = [&](uint32_t seq, bool& ok) -> const Work* {
-        __syncwarp();
-        ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bWorkFull + static_cast<int>(seq % kQueue)), (seq / kQueue) & 1, abort_flag, a.status));
-        return s_work + seq % kQueue;
-    };
+    const Roles roles{smem, s_work, s_seen, s_odd, s_up, &slots, bar0, abort_flag};
 
     if (warp == 0) {
-        // ---- loader: every lane copies a page ----
-        uint32_t stage = 0, phase = 0;
-        bool ok = true;
-        const int per_tile = kTile >> a.page_shift;
-        const uint32_t page_bytes = static_cast<uint32_t>(C::kPanels) << (a.page_shift + 7);
-        // More than N rows: neighbouring CTAs have the same keys at the same time, and N of the rows each.
-        const int cta = static_cast<int>(blockIdx.x) / row_blocks, n_ctas = static_cast<int>(gridDim.x) / row_blocks;
-        const Shares shares(all_pieces<false, kTile, kAllRows>(a, slots), kLeastTiles, n_ctas);
-        const int begin = shares.begin(cta), end = shares.begin(cta + 1);
-        int slot_now = begin < end ? slot_at(slots, a.n_slots, begin) : 0, at = begin;
-        bool joined = false;                     // an item that begins here goes on elsewhere
-        for (uint32_t seq = 0;; ++seq) {
-            const uint32_t place = seq % kQueue;
-            __syncwarp();
-            ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bWorkEmpty + static_cast<int>(place)), ((seq / kQueue) & 1) ^ 1, abort_flag, a.status));
-            if (!ok) break;
-            if (at >= end) {
-                if (lane == 0) {
-                    s_work[place].valid = 0;
-                    arrive_a(bar(C::bWorkFull + static_cast<int>(place)));
-                }
-                break;
-            }
-            const Segment s = segment_at<false, kTile, kAllRows>(a, slots, at, end, slot_now);
-            const int row0 = static_cast<int>(blockIdx.x) % row_blocks * N, n_rows = min(s.n_rows - row0, N);
-            const int part = 2 * static_cast<int>(blockIdx.x) + (at == begin ? 0 : 1);
-            at = s.item_at + s.p_end;
-            if (n_rows <= 0) {                   // (this slot has fewer rows)
-                --seq;
-                continue;
-            }
-            if (lane == 0) {
-                s_work[place] = Work{1, s.slot, s.p_begin, s.p_end, s.w.cache_pieces, s.w.keys, s.w.n, row0, n_rows, s.kvh, s.token0, s.head0,
-                                     s.p_begin == 0 && s.p_end == s.w.pieces ? -1 : part, {}};
-                arrive_a(bar(C::bWorkFull + static_cast<int>(place)));
-                if (s.p_begin == 0 && s.p_end < s.w.pieces) {
-                    a.meta[blockIdx.x] = {part, shares.owner(s.item_at + s.w.pieces - 1) - cta + 1, row_blocks, s.token0, s.head0, row0, n_rows};
-                    joined = true;
-                }
-            }
-            const int32_t* list = a.table + static_cast<int64_t>(s.slot) * a.max_pages;
-            const auto has_page = [&](int t) {                         // this lane has a page of tile t to load
-                return lane < per_tile && t < min(s.p_end, s.w.cache_pieces) && ((t * per_tile + lane) << a.page_shift) < s.w.keys;
-            };
-            const auto page_of = [&](int t) { return has_page(t) ? list[t * per_tile + lane] : 0; };
-            int id = page_of(s.p_begin);
-            for (int t = s.p_begin; t < s.p_end && ok; ++t) {
-                const int next = page_of(t + 1);                       // (looked at a tile later)
-                const bool fresh = t >= s.w.cache_pieces;
-                int page = has_page(t) ? id : -1;
-                if (has_page(t) && (id < 0 || id >= a.n_pages)) {
-                    report(a.status, PULSAR_DEV_BAD_PAGE);             // (some page is loaded; its rows count as absent)
-                    page = 0;
-                }
-                const uint32_t pages = __ballot_sync(0xffffffffu, page >= 0);
-                const uint32_t bytes = fresh ? static_cast<uint32_t>(C::kPanels) * kFreshRows * 128 : __popc(pages) * page_bytes;
-#pragma unroll
-                for (int kv = 0; kv < 2; ++kv) {
-                    __syncwarp();
-                    ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bKvEmpty + stage), phase ^ 1, abort_flag, a.status));
-                    if (!ok) break;
-                    const uint32_t full = bar(C::bKvFull + stage), dst = smem_u32(smem) + stage * C::kTileBytes;
-                    if (lane == 0) mbar_expect_tx_a(full, bytes);
-                    __syncwarp();
-#pragma unroll
-                    for (int p = 0; p < C::kPanels; ++p) {
-                        if (fresh) {
-                            if (lane == 0) tma_load_3d_a(dst + p * kPanelBytes, kv ? &tmVn : &tmKn, full, p * 64, s.kvh, s.slot * a.T);
-                        } else if (page >= 0) {
-                            tma_load_3d_a(dst + p * kPanelBytes + (lane << (a.page_shift + 7)), kv ? &tmV : &tmK, full, p * 64, s.kvh,
-                                          page << a.page_shift);
-                        }
-                    }
-                    if (++stage == C::kStages) {
-                        stage = 0;
-                        phase ^= 1;
-                    }
-                }
-                id = next;
-            }
-        }
-        if (lane == 0 && !joined) a.meta[blockIdx.x].parts = 0;
+        load_role<C>(a, tmK, tmV, tmKn, tmVn, row_blocks, roles);
     } else if (warp == 1) {
         // ---- matrix instructions: S of a tile, then PV of the tile before it ----
         const bool leader = elect_one();
@@ -337,7 +196,7 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
             if (last) ++n_done;
         };
         for (uint32_t seq = 0;; ++seq) {
-            const Work* s = next_work(seq, ok);
+            const Work* s = next_work<C>(a, roles, seq, ok);
             if (!ok || s->valid == 0) break;
             const int p_begin = s->p_begin, p_end = s->p_end;
             __syncwarp();
@@ -376,52 +235,7 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
         }
         if (ok && tile > 0) issue_pv(tile - 1);
     } else if (warp < 4) {
-        // ---- query rows, ancestors, the nodes' rows to their pages ----
-        const int t = threadIdx.x - 64;
-        bool ok = true;
-        for (uint32_t seq = 0;; ++seq) {
-            const Work* work = next_work(seq, ok);
-            ok = ok && mbar_wait_a(bar(C::bQEmpty), (seq & 1) ^ 1, abort_flag, a.status);
-            if (named_any(kRowsBarrier, 64, !ok) || work->valid == 0) break;
-            const Work s = *work;
-            if (t == 0) {                                  // (rows past the item's are other slots', or zeros: nobody reads their outputs)
-                mbar_expect_tx_a(bar(C::bQFull), C::kQBytes);
-#pragma unroll
-                for (int p = 0; p < C::kPanels; ++p)
-                    tma_load_3d_a(smem_u32(smem) + C::kQ + p * (N * 128), &tmQ, bar(C::bQFull), p * 64, s.head0, s.token0 + (s.row0 >> a.g_shift));
-            }
-            // (the place in the queue, and with it these buffers, is free when the softmax has left the segment kQueue before)
-            const bool has_new = s.p_end > s.cache_pieces;
-            if (has_new) {
-                ancestors(a, s.slot, s.n, t, s_sees, s_up, [] { named_sync(kRowsBarrier, 64); });
-                const uint64_t mine = s_sees[t];
-                uint32_t* seen = reinterpret_cast<uint32_t*>(s_seen + (seq % kQueue) * kMaxTree);
-#pragma unroll 8
-                for (int node = 0; node < kMaxTree; ++node) {          // this warp's 32 nodes that see `node`
-                    const uint32_t by = __ballot_sync(0xffffffffu, ((mine >> node) & 1ull) != 0ull);
-                    if (lane == (node & 31)) seen[2 * node + (t >> 5)] = by;
-                }
-            }
-            if (t < 2) s_odd[2 * (seq % kQueue) + t] = 0u;
-            named_sync(kRowsBarrier, 64);
-            if (t == 0) {
-                arrive_a(bar(C::bSees + static_cast<int>(seq % kQueue)));
-                arrive_a(bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));         // (both warps have their copy)
-            }
-            if (has_new && s.row0 == 0) {
-                constexpr int kVecs = D / 8;
-                const int head_at = s.kvh * D;
-                const int len = s.keys;
-                for (int i = t; i < s.n * kVecs; i += 64) {
-                    const int row = i / kVecs, v = i % kVecs;
-                    const int64_t to = new_row_at(a, s.slot, static_cast<int64_t>(len) + row, pitch);
-                    if (to < 0) continue;
-                    const int64_t from = (static_cast<int64_t>(s.slot) * a.T + row) * pitch + head_at;
-                    reinterpret_cast<uint4*>(a.K + to + head_at)[v] = reinterpret_cast<const uint4*>(a.Knew + from)[v];
-                    reinterpret_cast<uint4*>(a.V + to + head_at)[v] = reinterpret_cast<const uint4*>(a.Vnew + from)[v];
-                }
-            }
-        }
+        rows_role<D, C>(a, tmQ, static_cast<int>(threadIdx.x) - 64, roles);
     } else {
         // ---- softmax and epilogue ----
         const int quarter = warp & 3, group = (warp - 4) >> 2;
@@ -433,7 +247,7 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
         uint32_t v_stage = 1, v_phase = 0;                 // ring place of the tile's V
         bool ok = true;
         for (uint32_t seg = 0;; ++seg) {
-            const Work& s = *next_work(seg, ok);
+            const Work& s = *next_work<C>(a, roles, seg, ok);
             if (named_any(id, 128, !ok) || s.valid == 0) break;
             const int32_t* list = a.table + static_cast<int64_t>(s.slot) * a.max_pages;
             const int p_begin = s.p_begin, p_end = s.p_end, cache_pieces = s.cache_pieces, n_rows = s.n_rows;
@@ -676,7 +490,8 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
     if (warp == 1) tmem_dealloc(tmem, C::kTmemCols);
 }
 
-int item_rows(int rows) { return rows <= 16 ? 16 : std::min((rows + 31) / 32 * 32, 128); }
+// Query rows of a CTA: with more than 64 the rows stand in the lanes (paged_wide.cu).
+int item_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
 template <int D, int N>
 int32_t launch(const PagedArgs& a, const CUtensorMap (&map)[5], int rows, cudaStream_t stream) {
@@ -702,23 +517,20 @@ int32_t launch_tree_tiles(PagedArgs a, int rows, int d, void* workspace, cudaStr
     const int64_t pool_rows = static_cast<int64_t>(a.n_pages) << a.page_shift, fresh_rows = static_cast<int64_t>(a.n_slots) * a.T;
     if (!make_map_3d(&map[0], a.K, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) || !make_map_3d(&map[1], a.V, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) ||
         !make_map_3d(&map[2], a.Knew, fresh_rows, a.Hkv, d, 1, kFreshRows) || !make_map_3d(&map[3], a.Vnew, fresh_rows, a.Hkv, d, 1, kFreshRows) ||
-        !make_map_3d(&map[4], a.Q, fresh_rows, a.Hq, d, 1 << a.g_shift, n >> a.g_shift))
+        !make_map_3d(&map[4], a.Q, fresh_rows, a.Hq, d, 1 << a.g_shift, std::min(n, 128) >> a.g_shift))
         return PULSAR_ERR_CUDA;
+    if (n > 64) return launch_tree_wide(a, map, rows, d, stream);
     if (d == 128) {
         switch (n) {
             case 16: return launch<128, 16>(a, map, rows, stream);
             case 32: return launch<128, 32>(a, map, rows, stream);
-            case 64: return launch<128, 64>(a, map, rows, stream);
-            case 96: return launch<128, 96>(a, map, rows, stream);
-            default: return launch<128, 128>(a, map, rows, stream);
+            default: return launch<128, 64>(a, map, rows, stream);
         }
     }
     switch (n) {
         case 16: return launch<64, 16>(a, map, rows, stream);
         case 32: return launch<64, 32>(a, map, rows, stream);
-        case 64: return launch<64, 64>(a, map, rows, stream);
-        case 96: return launch<64, 96>(a, map, rows, stream);
-        default: return launch<64, 128>(a, map, rows, stream);
+        default: return launch<64, 64>(a, map, rows, stream);
     }
 }
 

@@ -300,3 +300,21 @@ def test_what_the_binding_refuses():
     with pytest.raises(binding.PulsarError) as e:
         binding.pulsar_tree_attn(*good, workspace=torch.empty(1024, dtype=torch.uint8, device=DEV))
     assert e.value.status == 4
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", [(2, 4, 1, 64), (2, 8, 2, 128), (5, 4, 1, 64), (13, 16, 4, 64), (16, 8, 2, 128), (24, 8, 2, 128),
+                                        (30, 4, 1, 64), (64, 8, 2, 64), (40, 16, 1, 128)])
+def test_values_that_are_not_finite_reach_who_sees_them(T, Hq, Hkv, d):
+    """An infinite component and a NaN one of two nodes' values, in every form that a call can take: the outputs of the nodes that see
+    them are what the definition says, component by component, and everybody else's are as if they were not there."""
+    c = R.Cache([150, 0], 16, Hkv, d, room=T)
+    Q, Kn, Vn, parent = drafts(2, T, Hq, Hkv, d, seed=T)
+    Vn[0, 1, :, 3], Vn[1, T // 2, :, d - 1], Vn[1, 0, 0, 5] = float("inf"), float("nan"), float("-inf")
+    O, LSE = binding.pulsar_tree_attn(*(x.to(DEV) for x in (Q, Kn, Vn, c.K, c.V, c.table, c.lens, parent)))
+    Oref, Lref, A = R.tree_attn(Q, Kn, Vn, c, parent)
+    o = O.double().cpu()
+    assert torch.equal(o.isnan(), Oref.isnan()) and torch.equal(o.isinf(), Oref.isinf()) and bool((o[o.isinf()] == Oref[o.isinf()]).all())
+    fine = Oref.isfinite()
+    assert not bool(fine.all())
+    zero = torch.zeros_like(Oref)
+    R.check(torch.where(fine, o, zero), LSE, (torch.where(fine, Oref, zero), Lref, torch.where(fine, A, zero)))

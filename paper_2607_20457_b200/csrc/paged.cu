@@ -14,372 +14,6 @@ namespace pulsar {
 
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kRows = 8;                        // query rows of an item: the columns of a matrix fragment
-constexpr int kUnitBytes = 4096;
-constexpr int kUnits = 3;                       // of a warp's ring: one in use, two on their way
-constexpr int kRingBytes = kWarps * kUnits * kUnitBytes;
-constexpr int kLeastKeys = 16;                  // of a piece
-constexpr int kLeastPieces = 3 * kWarps;        // of a CTA: three per warp, unless all CTAs have fewer
-
-// Two CTAs per SM: while the keys of one are on their way, the other computes.
-template <int D, bool kSparse>
-__global__ void __launch_bounds__(kThreads, 2)
-paged_rows_kernel(const __grid_constant__ PagedArgs a) {
-    constexpr int kKeys = kUnitBytes / (2 * D);                // keys of a piece: 16 (d = 128), 32 (d = 64)
-    constexpr int kHalves = kKeys / 16;                        // runs of 16 keys lie in one page
-    constexpr int kVecs = D / 8;                               // 16-byte vectors of a row
-    constexpr int kRowsPerCopy = 32 / kVecs;                   // rows a warp copies with one instruction
-    constexpr int kCopies = kKeys / kRowsPerCopy;
-    constexpr int kPitch = D + 4;                              // floats of a partial row: 2 * kPitch = 8 modulo the banks
-    static_assert(kWarps * kRows * kPitch * 4 <= kRingBytes, "the warps' partials take the ring's place");
-    extern __shared__ __align__(1024) uint8_t smem[];
-    float2* w_ml = reinterpret_cast<float2*>(smem + kRingBytes);               // [kRows][kWarps]
-    uint64_t* s_sees = reinterpret_cast<uint64_t*>(w_ml + kRows * kWarps);     // [kMaxTree] a node's ancestors and itself
-    int* s_up = reinterpret_cast<int*>(s_sees + kMaxTree);                     // [kMaxTree]
-    Slots& slots = *reinterpret_cast<Slots*>(s_up + kMaxTree);
-    float* w_o = reinterpret_cast<float*>(smem);                               // [kWarps][kRows][kPitch], where the rings were
-
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int gid = lane >> 2, tig = lane & 3;
-    grid_dependency_wait();
-    grid_launch_dependents();
-
-    // ---- this CTA's share of all pieces of all slots ----
-    if (warp == 0) (void)all_pieces<kSparse, kKeys, kRows>(a, slots);
-    __syncthreads();
-    const Shares shares(slots.before[a.n_slots], kLeastPieces, gridDim.x);
-    const int begin = shares.begin(blockIdx.x), end = shares.begin(blockIdx.x + 1);
-    if (begin >= end) {
-        if (threadIdx.x == 0) a.meta[blockIdx.x].parts = 0;
-        return;
-    }
-    int slot_now = slot_at(slots, a.n_slots, begin);
-
-    const uint32_t ring = smem_u32(smem) + warp * (kUnits * kUnitBytes);
-    const int copy_row = lane / kVecs, copy_vec = lane % kVecs;
-    const int64_t pitch = static_cast<int64_t>(a.Hkv) * D;     // elements between the rows of a head
-    const int page_mask = (1 << a.page_shift) - 1;
-    const int mi = lane >> 3, l8 = lane & 7;
-    const uint32_t k_lane = ring + ((mi & 1) * 8 + l8) * (D * 2), k_x = ((mi >> 1) ^ l8) << 4;     // K: rows are keys
-    const uint32_t v_lane = ring + ((mi >> 1) * 8 + l8) * (D * 2), v_x = ((mi & 1) ^ l8) << 4;     // V: read transposed
-    bool meta_written = false;
-
-    for (int at = begin; at < end;) {
-        // ---- the next item and this CTA's pieces of it ----
-        const Segment seg = segment_at<kSparse, kKeys, kRows>(a, slots, at, end, slot_now);
-        const SlotWork& w = seg.w;
-        const int slot = seg.slot, p_begin = seg.p_begin, p_end = seg.p_end, row0 = seg.row0, n_rows = seg.n_rows, kvh = seg.kvh;
-        const int token = seg.token, token0 = seg.token0, head0 = seg.head0;
-        const bool appends = row0 == 0 && token == 0;
-        const int head_at = kvh * D + copy_vec * 8;
-        const int32_t* list = kSparse ? a.list + (static_cast<int64_t>(token0) * a.Hkv + kvh) * (a.k + 1)
-                                      : a.table + static_cast<int64_t>(slot) * a.max_pages;
-        const uint16_t* fresh_k = a.Knew + (static_cast<int64_t>(slot) * a.T) * pitch + head_at;
-        const uint16_t* fresh_v = a.Vnew + (static_cast<int64_t>(slot) * a.T) * pitch + head_at;
-
-        // Page ids of a piece; -1 where there is no row.
-        struct Ids { int id[kHalves]; };
-        const auto pages_of = [&](int p) {
-            Ids x;
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-                const int row = p * kKeys + 16 * h;
-                x.id[h] = p < p_end && row < w.keys ? list[row >> a.page_shift] : -1;
-            }
-            return x;
-        };
-        // Bit h: the rows of half h exist.
-        const auto good = [&](const Ids& x, int p) {
-            uint32_t ok = 0;
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-                const bool in = x.id[h] >= 0 && x.id[h] < a.n_pages;
-                if (!in && p < p_end && p * kKeys + 16 * h < w.keys && lane == 0) report(a.status, PULSAR_DEV_BAD_PAGE);
-                ok |= (in ? 1u : 0u) << h;
-            }
-            return ok;
-        };
-        // A unit is K or V of a piece.  Row r goes to line r, its vector v to place v ^ (r & 7), so that the eight rows of a
-        // matrix fragment lie in different banks.  Rows that do not exist are zeros.
-        const auto load = [&](const uint16_t* pool, const uint16_t* fresh, const Ids& x, uint32_t ok, int p, int place) {
-            if (p < p_end) {
-                const uint32_t dst = ring + place * kUnitBytes + copy_row * (D * 2);
-#pragma unroll
-                for (int i = 0; i < kCopies; ++i) {
-                    const int r = i * kRowsPerCopy + copy_row, h = i / (kCopies / kHalves);
-                    const uint32_t to = dst + i * (kRowsPerCopy * D * 2) + ((copy_vec ^ (r & 7)) << 4);
-                    bool in;
-                    const uint16_t* src;
-                    if (p < w.cache_pieces) {
-                        const int row = p * kKeys + r;
-                        in = row < w.keys && ((ok >> h) & 1u) != 0u;
-                        src = pool + ((static_cast<int64_t>(x.id[h]) << a.page_shift) + (row & page_mask)) * pitch + head_at;
-                    } else {
-                        const int row = (p - w.cache_pieces) * kKeys + r;
-                        in = row < w.n;
-                        src = fresh + row * pitch;
-                    }
-                    cp_async16(to, in ? src : pool, in ? 16 : 0);
-                }
-            }
-            cp_async_commit();                                     // an empty group past the end keeps the count
-        };
-
-        const int p_first = p_begin + warp;
-        Ids now_ids = pages_of(p_first), next_ids = pages_of(p_first + kWarps);
-        uint32_t now_ok = good(now_ids, min(p_first, w.cache_pieces)), next_ok = 0;
-        load(a.K, fresh_k, now_ids, now_ok, p_first, 0);
-        load(a.V, fresh_v, now_ids, now_ok, p_first, 1);
-
-        // ---- which nodes a node sees ----
-        const bool has_new = p_end > w.cache_pieces;
-        if (!kSparse && has_new && a.parent != nullptr)
-            ancestors(a, slot, w.n, threadIdx.x, s_sees, s_up, [] { __syncthreads(); });
-        uint64_t sees[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int r = 2 * tig + k, x = kSparse ? token : (row0 + r) >> a.g_shift;
-            sees[k] = r >= n_rows || !has_new ? 0ull : kSparse || a.parent == nullptr ? ~0ull >> (63 - x) : s_sees[x];
-        }
-
-        // ---- the query rows as B fragments ----
-        uint32_t q[D / 16][2];
-        {
-            const uint32_t* src = reinterpret_cast<const uint32_t*>(a.Q + row_of(token0, head0, row0, gid < n_rows ? gid : 0, a.g_shift, a.Hq) * D) + tig;
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                q[kk][0] = gid < n_rows ? src[kk * 8] : 0u;
-                q[kk][1] = gid < n_rows ? src[kk * 8 + 4] : 0u;
-            }
-        }
-        // rows 2 tig and 2 tig + 1; o[c]: outputs 16 c + gid and 16 c + 8 + gid of both
-        float o[D / 16][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) o[c][k] = 0.f;
-
-        // Units are consumed in the order K, V, K, V, ... and refilled in that order, each where the unit before it was.
-        int place = 0, free_place = kUnits - 1;
-        const auto next_unit = [&](const uint16_t* pool, const uint16_t* fresh, int p) {
-            cp_async_wait<kUnits - 2>();
-            __syncwarp();
-            load(pool, fresh, next_ids, next_ok, p, free_place);
-            const int here = place;
-            free_place = here;
-            place = here + 1 == kUnits ? 0 : here + 1;
-            return here * kUnitBytes;
-        };
-        for (int p = p_first; p < p_end; p += kWarps) {
-            next_ok = good(next_ids, min(p + kWarps, w.cache_pieces));
-            const int at_k = next_unit(a.K, fresh_k, p + kWarps);
-            const Ids later_ids = pages_of(p + 2 * kWarps);
-            // ---- S^T = K Q^T: keys gid and gid + 8 of each 16, rows 2 tig and 2 tig + 1 ----
-            float s[kKeys / 16][4];
-#pragma unroll
-            for (int j = 0; j < kKeys / 16; ++j) {
-                float t[2][4] = {};                                // two chains of products
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    uint32_t f[4];
-                    ldmatrix4(k_lane + at_k + j * (16 * D * 2) + ((kk * 32) ^ k_x), f);
-                    mma_bf16(t[kk & 1], f, q[kk][0], q[kk][1]);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) s[j][k] = t[0][k] + t[1][k];
-            }
-            // keys that do not exist, or that the node of a row must not see
-            if (p >= w.cache_pieces) {
-                const int first = (p - w.cache_pieces) * kKeys;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t bits = static_cast<uint32_t>(sees[k] >> first);        // (node rows past n are nobody's ancestors)
-#pragma unroll
-                    for (int j = 0; j < kKeys / 16; ++j) {
-                        if (((bits >> (16 * j + gid)) & 1u) == 0u) s[j][k] = -INFINITY;
-                        if (((bits >> (16 * j + gid + 8)) & 1u) == 0u) s[j][k + 2] = -INFINITY;
-                    }
-                }
-            } else if (w.keys - p * kKeys < kKeys || now_ok != (1u << kHalves) - 1u) {
-                const int n_vis = w.keys - p * kKeys;
-#pragma unroll
-                for (int j = 0; j < kKeys / 16; ++j)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (16 * j + gid + (k >> 1) * 8 >= n_vis || ((now_ok >> j) & 1u) == 0u) s[j][k] = -INFINITY;
-            }
-            float x[2], alpha[2], neg[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                x[k] = fmaxf(s[0][k], s[0][k + 2]);
-#pragma unroll
-                for (int j = 1; j < kKeys / 16; ++j) x[k] = max3(x[k], s[j][k], s[j][k + 2]);
-            }
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) {
-                x[0] = fmaxf(x[0], __shfl_xor_sync(0xffffffffu, x[0], d));
-                x[1] = fmaxf(x[1], __shfl_xor_sync(0xffffffffu, x[1], d));
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float m_new = fmaxf(m[k], x[k] * a.scale_log2);
-                alpha[k] = m_new == -INFINITY ? 1.f : ex2(m[k] - m_new);
-                neg[k] = m_new == -INFINITY ? 0.f : -m_new;
-                m[k] = m_new;
-            }
-            uint32_t pb[kKeys / 16][2];
-            l[0] *= alpha[0];
-            l[1] *= alpha[1];
-#pragma unroll
-            for (int j = 0; j < kKeys / 16; ++j) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) s[j][k] = ex2(fmaf(s[j][k], a.scale_log2, neg[k & 1]));
-                l[0] += s[j][0] + s[j][2];
-                l[1] += s[j][1] + s[j][3];
-                pb[j][0] = movmatrix(pack_bf16x2(s[j][0], s[j][1]));      // [key][row] -> [row][key]
-                pb[j][1] = movmatrix(pack_bf16x2(s[j][2], s[j][3]));
-            }
-            if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
-#pragma unroll
-                for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) o[c][k] *= alpha[k & 1];
-            }
-            // ---- O^T += V^T P^T ----
-            const int at_v = next_unit(a.V, fresh_v, p + kWarps);
-            bool plain = true;
-            if (p >= w.cache_pieces) {
-                // A node that a row does not see has weight 0, and 0 times an infinity or a NaN in its value would still reach the
-                // row.  Units with such values are added up one visible product at a time.
-                const uint16_t* unit_v = reinterpret_cast<const uint16_t*>(smem + warp * (kUnits * kUnitBytes) + at_v);
-                uint32_t odd = 0;
-                for (int i = lane; i < kUnitBytes / 4; i += 32) {
-                    const uint32_t x = reinterpret_cast<const uint32_t*>(unit_v)[i];
-                    odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u ? 1u : 0u;
-                }
-                plain = !__any_sync(0xffffffffu, odd != 0u);
-                if (!plain) {
-                    const int first = (p - w.cache_pieces) * kKeys;
-#pragma unroll 1
-                    for (int key = 0; key < kKeys; ++key) {
-                        const uint16_t* v = unit_v + key * D + (gid & 7);
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const float a0 = s[0][k], a1 = s[0][k + 2];
-                            float x = key & 8 ? a1 : a0;
-                            if (kKeys > 16) x = key & 16 ? (key & 8 ? s[kKeys / 16 - 1][k + 2] : s[kKeys / 16 - 1][k]) : x;
-                            x = __shfl_sync(0xffffffffu, x, (key & 7) * 4 + tig);
-                            if (((sees[k] >> (first + key)) & 1u) == 0u) continue;
-#pragma unroll
-                            for (int c = 0; c < D / 16; ++c) {
-                                const uint32_t v0 = v[((2 * c) ^ (key & 7)) * 8], v1 = v[((2 * c + 1) ^ (key & 7)) * 8];
-                                o[c][k] = fmaf(x, __uint_as_float(v0 << 16), o[c][k]);
-                                o[c][k + 2] = fmaf(x, __uint_as_float(v1 << 16), o[c][k + 2]);
-                            }
-                        }
-                    }
-                }
-            }
-            if (plain) {
-#pragma unroll
-                for (int j = 0; j < kKeys / 16; ++j)
-#pragma unroll
-                    for (int c = 0; c < D / 16; ++c) {
-                        uint32_t f[4];
-                        ldmatrix4_trans(v_lane + at_v + j * (16 * D * 2) + ((c * 32) ^ v_x), f);
-                        mma_bf16(o[c], f, pb[j][0], pb[j][1]);
-                    }
-            }
-            // The new tokens' rows go to their pages from the warp that has just read them (nobody reads those rows in this launch).
-            if (appends && p >= w.cache_pieces) {
-#pragma unroll 1
-                for (int i = 0; i < kCopies; ++i) {
-                    const int row = (p - w.cache_pieces) * kKeys + i * kRowsPerCopy + copy_row;
-                    if (row >= w.n) continue;
-                    int64_t to = new_row_at(a, slot, static_cast<int64_t>(w.len) + row, pitch);
-                    if (to < 0) continue;
-                    to += head_at;
-                    *reinterpret_cast<uint4*>(a.K + to) = *reinterpret_cast<const uint4*>(fresh_k + row * pitch);
-                    *reinterpret_cast<uint4*>(a.V + to) = *reinterpret_cast<const uint4*>(fresh_v + row * pitch);
-                }
-            }
-            now_ok = next_ok;
-            next_ids = later_ids;
-        }
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) {
-            l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
-            l[1] += __shfl_xor_sync(0xffffffffu, l[1], d);
-        }
-
-        // ---- the warps' partials, brought to the CTA's maximum and added up, 32 outputs of a row per warp ----
-        if (gid == 0) {
-            w_ml[(2 * tig) * kWarps + warp] = make_float2(m[0], l[0]);
-            w_ml[(2 * tig + 1) * kWarps + warp] = make_float2(m[1], l[1]);
-        }
-        __syncthreads();
-        float f[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) f[k] = w_ml[(2 * tig + k) * kWarps + gid].x;
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) {
-            f[0] = fmaxf(f[0], __shfl_xor_sync(0xffffffffu, f[0], d));
-            f[1] = fmaxf(f[1], __shfl_xor_sync(0xffffffffu, f[1], d));
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            f[k] = weight(m[k], f[k]);
-            if (2 * tig + k < n_rows) {
-                float* dst = w_o + (warp * kRows + 2 * tig + k) * kPitch + gid;
-#pragma unroll
-                for (int c = 0; c < D / 16; ++c) {
-                    dst[16 * c] = o[c][k] * f[k];
-                    dst[16 * c + 8] = o[c][k + 2] * f[k];
-                }
-            }
-        }
-        __syncthreads();
-        const bool whole = p_begin == 0 && p_end == w.pieces;
-        const int64_t part = 2 * static_cast<int64_t>(blockIdx.x) + (at == begin ? 0 : 1);
-        for (int c = warp; c < n_rows * (D / 32); c += kWarps) {
-            const int r = c / (D / 32), at_d = (c % (D / 32)) * 32 + lane;
-            const float* src = w_o + r * kPitch + at_d;
-            float y[2] = {0.f, 0.f};
-#pragma unroll
-            for (int v = 0; v < kWarps; ++v) y[v & 1] += src[v * (kRows * kPitch)];
-            const float2 ml = lane < kWarps ? w_ml[r * kWarps + lane] : make_float2(-INFINITY, 0.f);
-            const float M = warp_max(ml.x), sum = low_lanes_sum<kWarps>(weight(ml.x, M) * ml.y);
-            const float out = (y[0] + y[1]) * (sum == 0.f ? 0.f : 1.f / sum);
-            const float lse = sum == 0.f ? -INFINITY : (M + log2f(sum)) * 0.6931471805599453f;
-            if (!whole) {
-                a.part_O[(part * kRows + r) * D + at_d] = out;
-                if (at_d == 0) a.part_LSE[part * kRows + r] = lse;
-                continue;
-            }
-            const int64_t row = row_of(token0, head0, row0, r, a.g_shift, a.Hq);
-            if (a.out_f32) {
-                static_cast<float*>(a.O)[row * D + at_d] = out;
-            } else {
-                const float z = __shfl_xor_sync(0xffffffffu, out, 1);
-                if ((lane & 1) == 0) *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.O) + row * D + at_d) = pack_bf16x2(out, z);
-            }
-            if (at_d == 0 && a.LSE != nullptr) a.LSE[row] = lse;
-        }
-        // An item that begins here and goes on elsewhere is this CTA's last; the CTAs up to the one with its last piece have a part each.
-        if (p_begin == 0 && p_end < w.pieces) {
-            if (threadIdx.x == 0) {
-                a.meta[blockIdx.x] = {static_cast<int>(part), shares.owner(seg.item_at + w.pieces - 1) - static_cast<int>(blockIdx.x) + 1, 1, token0, head0, row0, n_rows};
-            }
-            meta_written = true;
-        }
-        at = seg.item_at + p_end;
-        __syncthreads();                         // the ring is loaded into again
-    }
-    if (!meta_written && threadIdx.x == 0) a.meta[blockIdx.x].parts = 0;
-}
-
 // ---------------------------------------------------------------------------------------------
 // Scores of the full pages and the k best.
 //
@@ -828,23 +462,10 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
 // ---------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------
-constexpr int kSmemBytes = kRingBytes + kRows * kWarps * 8 + kMaxTree * 8 + kMaxTree * 4 + static_cast<int>(sizeof(Slots));
-
 bool heads_ok(int32_t Hq, int32_t Hkv) {
     if (Hkv < 1 || Hq < Hkv || Hq % Hkv != 0) return false;
     const int g = Hq / Hkv;
     return g == 1 || g == 2 || g == 4 || g == 8 || g == 16;
-}
-
-PartScratch rows_scratch(int d) { return PartScratch(2 * static_cast<size_t>(sm_count()), kRows, d); }
-
-template <typename Kernel>
-int32_t launch_rows(Kernel kernel, const PagedArgs& a, int d, cudaStream_t st) {
-    const unsigned ctas = 2 * static_cast<unsigned>(sm_count());
-    PULSAR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes));
-    PULSAR_CUDA_OK(launch_kernel(kernel, dim3(ctas), dim3(kThreads), kSmemBytes, st, true, a));
-    count_launch();
-    return launch_parts_merge(a, ctas, kRows, d, st);
 }
 
 float scale_log2(float softmax_scale, int32_t d) {
@@ -858,8 +479,7 @@ using namespace pulsar;
 
 extern "C" size_t pulsar_tree_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t Hq, int32_t Hkv, int32_t d) {
     if (n_slots < 1 || n_slots > kMaxSlots || T < 1 || T > kMaxTree || !heads_ok(Hq, Hkv) || (d != 64 && d != 128)) return 0;
-    const int rows = T * (Hq / Hkv);
-    return rows > kRows ? tree_tiles_workspace_bytes(rows, d) : rows_scratch(d).total;
+    return attn_workspace_bytes(T * (Hq / Hkv), d);
 }
 
 extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, const uint16_t* Vnew, int32_t T, uint16_t* K_pages,
@@ -878,9 +498,7 @@ extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, con
     if (!aligned(page_table, 4) || !aligned(cache_len, 4) || !aligned(parent, 4) || !aligned(n_draft, 4) || !aligned(LSE, 4) ||
         !aligned(workspace, 256))
         return PULSAR_ERR_ALIGNMENT;
-    if (!(T * (Hq / Hkv) > kRows ? tree_tiles_ok(n_slots, Hkv, static_cast<int64_t>(max_pages) * page_size, T)
-                                 : pieces_ok(n_slots, Hkv, static_cast<int64_t>(max_pages) * page_size, T, kLeastKeys)))
-        return PULSAR_ERR_SHAPE;
+    if (!attn_pieces_ok(n_slots, Hkv, static_cast<int64_t>(max_pages) * page_size, T)) return PULSAR_ERR_SHAPE;
     if (workspace_bytes < pulsar_tree_attn_workspace_bytes(n_slots, T, Hq, Hkv, d)) return PULSAR_ERR_WORKSPACE;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
     PagedArgs a{};
@@ -906,18 +524,15 @@ extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, con
     a.out_f32 = out_is_f32;
     a.LSE = LSE;
     a.status = device_status;
-    const int rows = T * (Hq / Hkv);
-    if (rows > kRows) return launch_tree_tiles(a, rows, d, workspace, static_cast<cudaStream_t>(stream));
-    rows_scratch(d).place(a, workspace);
-    return launch_rows(d == 128 ? paged_rows_kernel<128, false> : paged_rows_kernel<64, false>, a, d, static_cast<cudaStream_t>(stream));
+    return launch_attn(a, T * (Hq / Hkv), d, workspace, static_cast<cudaStream_t>(stream));
 }
 
 namespace {
 struct SparseScratch {
     size_t exact, score, most, list, total;
-    SparseScratch(int64_t n_slots, int64_t T, int64_t Hkv, int64_t max_pages, int64_t k, int d) {
+    SparseScratch(int64_t n_slots, int64_t T, int64_t Hkv, int64_t max_pages, int64_t k, int g, int d) {
         const int64_t rows = n_slots * T * Hkv;
-        exact = rows_scratch(d).total;
+        exact = attn_workspace_bytes(g, d);
         score = round_up(exact + static_cast<size_t>(rows * max_pages) * 8, 256);
         most = round_up(score + static_cast<size_t>(rows * max_pages) * 4, 256);
         list = round_up(most + static_cast<size_t>(n_slots * Hkv * ((max_pages + kScorePages - 1) / kScorePages)) * 4, 256);
@@ -933,7 +548,7 @@ bool sparse_ok(int32_t n_slots, int32_t T, int32_t k, int32_t Hq, int32_t Hkv, i
 extern "C" size_t pulsar_sparse_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t max_pages, int32_t k, int32_t Hq, int32_t Hkv,
                                                      int32_t d) {
     if (!sparse_ok(n_slots, T, k, Hq, Hkv, d) || max_pages < 1) return 0;
-    return SparseScratch(n_slots, T, Hkv, max_pages, k, d).total;
+    return SparseScratch(n_slots, T, Hkv, max_pages, k, Hq / Hkv, d).total;
 }
 
 extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, const uint16_t* Vnew, int32_t T, uint16_t* K_pages,
@@ -944,7 +559,7 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
                                       size_t workspace_bytes, int32_t* device_status, void* stream) {
     if (!pool_ok(1, n_pages, page_size, Hkv, d, n_slots, max_pages) || !sparse_ok(n_slots, T, k, Hq, Hkv, d) || sink < 0 || window < 0 ||
         static_cast<int64_t>(sink) + window > k ||
-        !pieces_ok(n_slots, static_cast<int64_t>(T) * Hkv * 2, std::min<int64_t>(k + 1, max_pages) * page_size, T, kLeastKeys))
+        !attn_pieces_ok(n_slots, static_cast<int64_t>(T) * Hkv, (static_cast<int64_t>(k) + 1) * page_size, T))
         return PULSAR_ERR_SHAPE;
     if (Q == nullptr || Knew == nullptr || Vnew == nullptr || K_pages == nullptr || V_pages == nullptr || summary == nullptr ||
         page_table == nullptr || cache_len == nullptr || O == nullptr || sel == nullptr || workspace == nullptr)
@@ -955,7 +570,7 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
     if (!aligned(page_table, 4) || !aligned(cache_len, 4) || !aligned(n_draft, 4) || !aligned(LSE, 4) || !aligned(sel, 4) || !aligned(workspace, 256))
         return PULSAR_ERR_ALIGNMENT;
     const int64_t rows = static_cast<int64_t>(n_slots) * T * Hkv;
-    const SparseScratch y(n_slots, T, Hkv, max_pages, k, d);
+    const SparseScratch y(n_slots, T, Hkv, max_pages, k, Hq / Hkv, d);
     if (workspace_bytes < y.total) return PULSAR_ERR_WORKSPACE;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
     auto* ws = static_cast<uint8_t*>(workspace);
@@ -1014,6 +629,5 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
     a.O = O;
     a.LSE = LSE;
     a.status = device_status;
-    rows_scratch(d).place(a, ws);
-    return launch_rows(d == 128 ? paged_rows_kernel<128, true> : paged_rows_kernel<64, true>, a, d, st);
+    return launch_attn(a, Hq / Hkv, d, workspace, st);
 }

@@ -45,6 +45,7 @@ struct PagedArgs {
     const int32_t *table, *len, *n_draft, *parent;
     const int32_t* list;                         // selected pages: [n_slots, T, Hkv, k + 1] page ids, the last row's page among them
     int n_slots, T, Hq, Hkv, g_shift, page_shift, n_pages, max_pages, k;
+    int fresh_rows;                              // rows of the new tokens' tile that are loaded: T, up to a multiple of 8
     float scale_log2;
     void* O;
     int out_f32;
@@ -57,10 +58,10 @@ struct PagedArgs {
 // Joins the partials that `ctas` CTAs have left of items of `rows` rows (paged_merge.cu).
 int32_t launch_parts_merge(const PagedArgs& a, unsigned ctas, int rows, int d, cudaStream_t stream);
 
-// Trees with more than eight query rows per KV head (paged_tiles.cu).
-bool tree_tiles_ok(int64_t n_slots, int64_t Hkv, int64_t keys, int64_t T);
-size_t tree_tiles_workspace_bytes(int rows, int d);
-int32_t launch_tree_tiles(PagedArgs a, int rows, int d, void* workspace, cudaStream_t stream);
+// Attention over the rows of the cache or, where there is a list, over the selected pages (paged_tiles.cu).  rows: of an item.
+bool attn_pieces_ok(int64_t n_slots, int64_t items, int64_t keys, int64_t T);
+size_t attn_workspace_bytes(int rows, int d);
+int32_t launch_attn(PagedArgs a, int rows, int d, void* workspace, cudaStream_t stream);
 
 // Scratch of an attention launch: what its CTAs leave for the merge.  rows: of an item.
 struct PartScratch {

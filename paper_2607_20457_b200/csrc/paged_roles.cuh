@@ -10,7 +10,6 @@ namespace pulsar {
 
 constexpr int kTile = 128;                       // keys
 constexpr int kPanelBytes = kTile * 128;         // 64 columns of a tile: 128-byte lines, swizzled
-constexpr int kFreshRows = 64;                   // rows of the nodes' own tile that are loaded
 constexpr float kRescale = 8.f;                  // in log2 units
 constexpr float kUnset = 1e30f;                  // stands for minus a maximum that no logit has set: every logit exceeds it
 constexpr int kLeastTiles = 2;                   // of a CTA, unless all CTAs have fewer
@@ -24,7 +23,7 @@ struct __align__(16) Work {
     int slot, p_begin, p_end, cache_pieces;
     int keys, n, row0, n_rows, kvh, token0, head0;
     int part;                                    // place of the partial, -1: all of the item, its outputs are final
-    int pad_[3];
+    int len, token, pad_;                        // rows in the slot's cache; selected pages: the item's token
 };
 static_assert(sizeof(Work) == 64, "");
 
@@ -79,6 +78,12 @@ struct Roles {
     __device__ __forceinline__ uint32_t bar(int i) const { return bar0 + 8 * static_cast<uint32_t>(i); }
 };
 
+// The page ids of an item: its slot's table, or its token's and KV head's selected pages.
+template <bool kSparse>
+__device__ __forceinline__ const int32_t* page_list(const PagedArgs& a, int slot, int token0, int kvh) {
+    return kSparse ? a.list + (static_cast<int64_t>(token0) * a.Hkv + kvh) * (a.k + 1) : a.table + static_cast<int64_t>(slot) * a.max_pages;
+}
+
 // The next published segment (a warp's lanes together); `ok` turns false where a wait has given up.
 template <class C>
 __device__ __forceinline__ const Work* next_work(const PagedArgs& a, const Roles& r, uint32_t seq, bool& ok) {
@@ -103,7 +108,7 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const CUtensorMap&
     const uint32_t page_bytes = static_cast<uint32_t>(C::kPanels) << (a.page_shift + 7);
     // More rows than a CTA takes: neighbouring CTAs have the same keys at the same time, and a share of the rows each.
     const int cta = static_cast<int>(blockIdx.x) / row_blocks, n_ctas = static_cast<int>(gridDim.x) / row_blocks;
-    const Shares shares(all_pieces<false, kTile, kAllRows>(a, slots), kLeastTiles, n_ctas);
+    const Shares shares(all_pieces<C::kSparse, kTile, kAllRows>(a, slots), kLeastTiles, n_ctas);
     const int begin = shares.begin(cta), end = shares.begin(cta + 1);
     int slot_now = begin < end ? slot_at(slots, a.n_slots, begin) : 0, at = begin;
     bool joined = false;                     // an item that begins here goes on elsewhere
@@ -119,7 +124,7 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const CUtensorMap&
             }
             break;
         }
-        const Segment s = segment_at<false, kTile, kAllRows>(a, slots, at, end, slot_now);
+        const Segment s = segment_at<C::kSparse, kTile, kAllRows>(a, slots, at, end, slot_now);
         const int row0 = static_cast<int>(blockIdx.x) % row_blocks * C::kRows, n_rows = min(s.n_rows - row0, C::kRows);
         const int part = 2 * static_cast<int>(blockIdx.x) + (at == begin ? 0 : 1);
         at = s.item_at + s.p_end;
@@ -129,14 +134,14 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const CUtensorMap&
         }
         if (lane == 0) {
             s_work[place] = Work{1, s.slot, s.p_begin, s.p_end, s.w.cache_pieces, s.w.keys, s.w.n, row0, n_rows, s.kvh, s.token0, s.head0,
-                                 s.p_begin == 0 && s.p_end == s.w.pieces ? -1 : part, {}};
+                                 s.p_begin == 0 && s.p_end == s.w.pieces ? -1 : part, s.w.len, s.token, 0};
             arrive_a(bar(C::bWorkFull + static_cast<int>(place)));
             if (s.p_begin == 0 && s.p_end < s.w.pieces) {
                 a.meta[blockIdx.x] = {part, shares.owner(s.item_at + s.w.pieces - 1) - cta + 1, row_blocks, s.token0, s.head0, row0, n_rows};
                 joined = true;
             }
         }
-        const int32_t* list = a.table + static_cast<int64_t>(s.slot) * a.max_pages;
+        const int32_t* list = page_list<C::kSparse>(a, s.slot, s.token0, s.kvh);
         const auto has_page = [&](int t) {                         // this lane has a page of tile t to load
             return lane < per_tile && t < min(s.p_end, s.w.cache_pieces) && ((t * per_tile + lane) << a.page_shift) < s.w.keys;
         };
@@ -151,7 +156,7 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const CUtensorMap&
                 page = 0;
             }
             const uint32_t pages = __ballot_sync(0xffffffffu, page >= 0);
-            const uint32_t bytes = fresh ? static_cast<uint32_t>(C::kPanels) * kFreshRows * 128 : __popc(pages) * page_bytes;
+            const uint32_t bytes = fresh ? static_cast<uint32_t>(C::kPanels * a.fresh_rows) * 128 : __popc(pages) * page_bytes;
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 __syncwarp();
@@ -210,8 +215,9 @@ __device__ __forceinline__ void rows_role(const PagedArgs& a, const CUtensorMap&
         const bool has_new = s.p_end > s.cache_pieces;
         if (has_new) {
             uint64_t* sees = s_sees + (seq % kQueue) * kMaxTree;
-            ancestors(a, s.slot, s.n, t, sees, s_up, [] { named_sync(kRowsBarrier, 64); });
-            if (C::kBySeen) {                                      // turned round: the nodes that see a node
+            if (C::kSparse) sees[t] = t <= s.token ? 1ull : 0ull;  // (the item's rows are one token's: it sees the tokens up to itself)
+            else ancestors(a, s.slot, s.n, t, sees, s_up, [] { named_sync(kRowsBarrier, 64); });
+            if (C::kBySeen && !C::kSparse) {                                      // turned round: the nodes that see a node
                 const uint64_t mine = sees[t];
                 uint32_t* seen = reinterpret_cast<uint32_t*>(sees);
                 named_sync(kRowsBarrier, 64);
@@ -228,10 +234,10 @@ __device__ __forceinline__ void rows_role(const PagedArgs& a, const CUtensorMap&
             arrive_a(bar(C::bSees + static_cast<int>(seq % kQueue)));
             arrive_a(bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));         // (both warps have their copy)
         }
-        if (has_new && s.row0 == 0) {
+        if (has_new && s.row0 == 0 && s.token == 0) {
             constexpr int kVecs = D / 8;
             const int head_at = s.kvh * D;
-            const int len = s.keys;
+            const int len = s.len;
             for (int i = t; i < s.n * kVecs; i += 64) {
                 const int row = i / kVecs, v = i % kVecs;
                 const int64_t to = new_row_at(a, s.slot, static_cast<int64_t>(len) + row, pitch);

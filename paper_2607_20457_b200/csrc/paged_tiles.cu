@@ -21,7 +21,7 @@ namespace pulsar {
 
 namespace {
 
-template <int D, int N>
+template <int D, int N, bool kSelected>
 struct Cfg {
     static constexpr int kPanels = D / 64;
     static constexpr int kTileBytes = kPanels * kPanelBytes;
@@ -30,7 +30,7 @@ struct Cfg {
     static constexpr int kSoftWarps = 4 * kGroups;
     static constexpr int kThreads = 128 + 128 * kGroups;
     static constexpr int kRows = N, kQTiles = 1, kQRows = N;
-    static constexpr bool kBySeen = true;
+    static constexpr bool kBySeen = true, kSparse = kSelected;
     static constexpr int kPBytes = (N + 63) / 64 * kPanelBytes;
     static constexpr int kQBytes = kPanels * N * 128;
     static constexpr int kMisc = static_cast<int>(sizeof(Slots)) + 12 + kQueue * kMaxTree * 8 + kQueue * (8 + 64) + 64 * 8 + 7 * N * 4 + N * 8 +
@@ -92,12 +92,12 @@ __device__ __forceinline__ void column_sums(float (&x)[C], int lane) {
     }
 }
 
-template <int D, int N>
-__global__ void __launch_bounds__(Cfg<D, N>::kThreads, 1)
-tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+template <int D, int N, bool kSparse>
+__global__ void __launch_bounds__(Cfg<D, N, kSparse>::kThreads, 1)
+paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                   const __grid_constant__ CUtensorMap tmKn, const __grid_constant__ CUtensorMap tmVn, const __grid_constant__ CUtensorMap tmQ,
                   int row_blocks) {
-    using C = Cfg<D, N>;
+    using C = Cfg<D, N, kSparse>;
     constexpr int kCols = C::kCols;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* rest = smem + C::kRest;
@@ -249,7 +249,7 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
         for (uint32_t seg = 0;; ++seg) {
             const Work& s = *next_work<C>(a, roles, seg, ok);
             if (named_any(id, 128, !ok) || s.valid == 0) break;
-            const int32_t* list = a.table + static_cast<int64_t>(s.slot) * a.max_pages;
+            const int32_t* list = page_list<kSparse>(a, s.slot, s.token0, s.kvh);
             const int p_begin = s.p_begin, p_end = s.p_end, cache_pieces = s.cache_pieces, n_rows = s.n_rows;
             float sum[kCols];
 #pragma unroll
@@ -493,45 +493,44 @@ tree_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ C
 // Query rows of a CTA: with more than 64 the rows stand in the lanes (paged_wide.cu).
 int item_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
-template <int D, int N>
-int32_t launch(const PagedArgs& a, const CUtensorMap (&map)[5], int rows, cudaStream_t stream) {
-    using C = Cfg<D, N>;
+template <int D, int N, bool kSparse>
+int32_t launch(const PagedArgs& a, const CUtensorMap (&map)[5], cudaStream_t stream) {
+    using C = Cfg<D, N, kSparse>;
+    const auto kernel = paged_tiles_kernel<D, N, kSparse>;
     const unsigned ctas = static_cast<unsigned>(sm_count());
-    PULSAR_CUDA_OK(cudaFuncSetAttribute(tree_tiles_kernel<D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
-    PULSAR_CUDA_OK(launch_kernel(tree_tiles_kernel<D, N>, dim3(ctas), dim3(C::kThreads), C::kSmem, stream, true, a, map[0], map[1], map[2], map[3],
-                                 map[4], (rows + N - 1) / N));
+    PULSAR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    PULSAR_CUDA_OK(launch_kernel(kernel, dim3(ctas), dim3(C::kThreads), C::kSmem, stream, true, a, map[0], map[1], map[2], map[3], map[4], 1));
     count_launch();
     return launch_parts_merge(a, ctas, N, D, stream);
+}
+template <int D>
+int32_t launch_rows(const PagedArgs& a, const CUtensorMap (&map)[5], int n, cudaStream_t stream) {
+    if (a.list != nullptr) return launch<D, 16, true>(a, map, stream);
+    switch (n) {
+        case 16: return launch<D, 16, false>(a, map, stream);
+        case 32: return launch<D, 32, false>(a, map, stream);
+        default: return launch<D, 64, false>(a, map, stream);
+    }
 }
 
 }  // namespace
 
-bool tree_tiles_ok(int64_t n_slots, int64_t Hkv, int64_t keys, int64_t T) { return pieces_ok(n_slots, Hkv, keys, T, kTile); }
+bool attn_pieces_ok(int64_t n_slots, int64_t items, int64_t keys, int64_t T) { return pieces_ok(n_slots, items, keys, T, kTile); }
 
-size_t tree_tiles_workspace_bytes(int rows, int d) { return PartScratch(sm_count(), item_rows(rows), d).total; }
+size_t attn_workspace_bytes(int rows, int d) { return PartScratch(sm_count(), item_rows(rows), d).total; }
 
-int32_t launch_tree_tiles(PagedArgs a, int rows, int d, void* workspace, cudaStream_t stream) {
+int32_t launch_attn(PagedArgs a, int rows, int d, void* workspace, cudaStream_t stream) {
     const int n = item_rows(rows);
     PartScratch(sm_count(), n, d).place(a, workspace);
+    a.fresh_rows = static_cast<int>(round_up(a.T, 8));
     CUtensorMap map[5];
     const int64_t pool_rows = static_cast<int64_t>(a.n_pages) << a.page_shift, fresh_rows = static_cast<int64_t>(a.n_slots) * a.T;
     if (!make_map_3d(&map[0], a.K, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) || !make_map_3d(&map[1], a.V, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) ||
-        !make_map_3d(&map[2], a.Knew, fresh_rows, a.Hkv, d, 1, kFreshRows) || !make_map_3d(&map[3], a.Vnew, fresh_rows, a.Hkv, d, 1, kFreshRows) ||
+        !make_map_3d(&map[2], a.Knew, fresh_rows, a.Hkv, d, 1, a.fresh_rows) || !make_map_3d(&map[3], a.Vnew, fresh_rows, a.Hkv, d, 1, a.fresh_rows) ||
         !make_map_3d(&map[4], a.Q, fresh_rows, a.Hq, d, 1 << a.g_shift, std::min(n, 128) >> a.g_shift))
         return PULSAR_ERR_CUDA;
     if (n > 64) return launch_tree_wide(a, map, rows, d, stream);
-    if (d == 128) {
-        switch (n) {
-            case 16: return launch<128, 16>(a, map, rows, stream);
-            case 32: return launch<128, 32>(a, map, rows, stream);
-            default: return launch<128, 64>(a, map, rows, stream);
-        }
-    }
-    switch (n) {
-        case 16: return launch<64, 16>(a, map, rows, stream);
-        case 32: return launch<64, 32>(a, map, rows, stream);
-        default: return launch<64, 64>(a, map, rows, stream);
-    }
+    return d == 128 ? launch_rows<128>(a, map, n, stream) : launch_rows<64>(a, map, n, stream);
 }
 
 }  // namespace pulsar

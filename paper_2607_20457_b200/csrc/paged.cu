@@ -1,10 +1,10 @@
 // Attention over a paged key/value cache: drafted trees (every cached row) and selected pages (include/pulsar.h).
 //
-// Lengths live on the device, so a launch does not know how much work it has.  A work item is up to eight query rows of one KV
-// head (tree: nodes x heads of the group; selected pages: the group's heads of one token) against a list of keys, cut into pieces
-// of 16 keys (d = 128; 32 with d = 64).  Every CTA adds up the pieces of all slots, takes an equal share of them, whichever items they
-// belong to, and leaves a partial (normalised output and l = ln sum exp) where it holds an item only in part; a second
-// launch joins those (paged_merge.cu).
+// Lengths live on the device, so a launch does not know how much work it has.  A work item is the query rows of one KV head (tree: nodes
+// x heads of the group; selected pages: the group's heads of one token) against a list of keys, cut into tiles of 128.  Every CTA adds
+// up the tiles of all slots, takes an equal share of them, whichever items they belong to, and leaves a partial (normalised output and
+// l = ln sum exp) where it holds an item only in part; a second launch joins those (paged_merge.cu).  This file has the selection of
+// the pages and the entry points.
 #include <algorithm>
 
 #include "mma.cuh"
@@ -498,7 +498,7 @@ extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, con
     if (!aligned(page_table, 4) || !aligned(cache_len, 4) || !aligned(parent, 4) || !aligned(n_draft, 4) || !aligned(LSE, 4) ||
         !aligned(workspace, 256))
         return PULSAR_ERR_ALIGNMENT;
-    if (!attn_pieces_ok(n_slots, Hkv, static_cast<int64_t>(max_pages) * page_size, T)) return PULSAR_ERR_SHAPE;
+    if (!pieces_ok(n_slots, Hkv, static_cast<int64_t>(max_pages) * page_size)) return PULSAR_ERR_SHAPE;
     if (workspace_bytes < pulsar_tree_attn_workspace_bytes(n_slots, T, Hq, Hkv, d)) return PULSAR_ERR_WORKSPACE;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
     PagedArgs a{};
@@ -559,7 +559,7 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
                                       size_t workspace_bytes, int32_t* device_status, void* stream) {
     if (!pool_ok(1, n_pages, page_size, Hkv, d, n_slots, max_pages) || !sparse_ok(n_slots, T, k, Hq, Hkv, d) || sink < 0 || window < 0 ||
         static_cast<int64_t>(sink) + window > k ||
-        !attn_pieces_ok(n_slots, static_cast<int64_t>(T) * Hkv, (static_cast<int64_t>(k) + 1) * page_size, T))
+        !pieces_ok(n_slots, static_cast<int64_t>(T) * Hkv, (static_cast<int64_t>(k) + 1) * page_size))
         return PULSAR_ERR_SHAPE;
     if (Q == nullptr || Knew == nullptr || Vnew == nullptr || K_pages == nullptr || V_pages == nullptr || summary == nullptr ||
         page_table == nullptr || cache_len == nullptr || O == nullptr || sel == nullptr || workspace == nullptr)

@@ -13,9 +13,7 @@ inline bool pool_ok(int64_t n_layers, int32_t n_pages, int32_t page_size, int32_
            static_cast<int64_t>(n_slots) * max_pages < (int64_t{1} << 31);
 }
 // Whether the pieces of an attention call can be counted in 32 bits, whatever the lengths on the device are.
-inline bool pieces_ok(int64_t n_slots, int64_t max_items, int64_t keys, int64_t T, int piece) {
-    return n_slots * max_items * ((keys + piece - 1) / piece + (T + piece - 1) / piece) < (int64_t{1} << 31);
-}
+inline bool pieces_ok(int64_t n_slots, int64_t max_items, int64_t keys) { return n_slots * max_items * (keys / 128 + 2) < (int64_t{1} << 31); }
 inline int log2_exact(int x) {
     int s = 0;
     while ((1 << s) < x) ++s;
@@ -59,7 +57,6 @@ struct PagedArgs {
 int32_t launch_parts_merge(const PagedArgs& a, unsigned ctas, int rows, int d, cudaStream_t stream);
 
 // Attention over the rows of the cache or, where there is a list, over the selected pages (paged_tiles.cu).  rows: of an item.
-bool attn_pieces_ok(int64_t n_slots, int64_t items, int64_t keys, int64_t T);
 size_t attn_workspace_bytes(int rows, int d);
 int32_t launch_attn(PagedArgs a, int rows, int d, void* workspace, cudaStream_t stream);
 
@@ -88,23 +85,30 @@ __device__ __forceinline__ int checked_len(int len, int64_t capacity, bool tell,
     return len < 0 ? 0 : static_cast<int>(capacity);
 }
 
-// Bookkeeping of a slot, the same in every CTA.  Pieces of all slots together are fewer than 2^31 (checked on the host: pieces_ok).
+constexpr int kTile = 128;                       // keys of a piece
+
+// Bookkeeping of a slot, the same in every CTA.  Tiles of all slots together are fewer than 2^31 (checked on the host: pieces_ok).
+// The new tokens follow the cached rows in the last tile, from the next multiple of 16 on, or have a tile of their own where they do
+// not fit: a decoding step behind 100 rows is one tile, not two.
 struct SlotWork {
     int len, n;                                  // rows in the cache; new tokens
     int keys;                                    // cached rows an item reads
-    int cache_pieces, pieces, items;
+    int pieces, items;
+    int new_tile, new_at;                        // the tile with the new tokens, and their place in it
 };
-template <bool kSparse, int kKeys, int kRows>
+template <bool kSparse>
 __device__ __forceinline__ SlotWork slot_work(const PagedArgs& a, int len, int n) {
     SlotWork w;
     w.len = len;
     w.n = n;
     const int full = len >> a.page_shift;
     w.keys = kSparse ? (min(a.k, full) << a.page_shift) + (len - (full << a.page_shift)) : len;
-    w.cache_pieces = (w.keys + kKeys - 1) / kKeys;
-    w.pieces = w.cache_pieces + (n + kKeys - 1) / kKeys;
-    const int g = 1 << a.g_shift;
-    w.items = kSparse ? n * a.Hkv * ((g + kRows - 1) / kRows) : a.Hkv * ((n * g + kRows - 1) / kRows);
+    const int whole = w.keys / kTile, tail = w.keys % kTile, at = (tail + 15) / 16 * 16;
+    const bool joint = tail > 0 && at + a.fresh_rows <= kTile;
+    w.new_tile = whole + (tail > 0 && !joint ? 1 : 0);
+    w.new_at = joint ? at : 0;
+    w.pieces = w.new_tile + 1;
+    w.items = n == 0 ? 0 : kSparse ? n * a.Hkv : a.Hkv;
     return w;
 }
 
@@ -121,7 +125,7 @@ struct Slots {
     unsigned char n[kMaxSlots];
 };
 // One warp fills it in; returns the pieces of all slots.
-template <bool kSparse, int kKeys, int kRows>
+template <bool kSparse>
 __device__ __forceinline__ int all_pieces(const PagedArgs& a, Slots& slots) {
     const int lane = threadIdx.x & 31;
     int total = 0;
@@ -131,7 +135,7 @@ __device__ __forceinline__ int all_pieces(const PagedArgs& a, Slots& slots) {
         if (s < a.n_slots) {
             const int len = checked_len(a.len[s], static_cast<int64_t>(a.max_pages) << a.page_shift, blockIdx.x == 0, a.status);
             const int n = a.n_draft != nullptr ? min(max(a.n_draft[s], 0), a.T) : a.T;
-            const SlotWork w = slot_work<kSparse, kKeys, kRows>(a, len, n);
+            const SlotWork w = slot_work<kSparse>(a, len, n);
             x = w.pieces * w.items;
             slots.len[s] = len;
             slots.n[s] = static_cast<unsigned char>(n);
@@ -182,26 +186,23 @@ __device__ __forceinline__ int slot_at(const Slots& slots, int n_slots, int at) 
 struct Segment {
     SlotWork w;
     int slot, p_begin, p_end;
-    int row0, n_rows, kvh, token, token0, head0;
+    int n_rows, kvh, token, token0, head0;       // query rows; KV head; sparse: the token; first token among all, first head
     int item_at;                                 // the item's first piece among all
 };
-template <bool kSparse, int kKeys, int kRows>
+template <bool kSparse>
 __device__ __forceinline__ Segment segment_at(const PagedArgs& a, const Slots& slots, int at, int end, int& slot) {
     Segment s;
     while (slots.before[slot + 1] <= at) ++slot;
     s.slot = slot;
-    s.w = slot_work<kSparse, kKeys, kRows>(a, slots.len[slot], slots.n[slot]);
-    const int first = slots.before[slot], g = 1 << a.g_shift;
+    s.w = slot_work<kSparse>(a, slots.len[slot], slots.n[slot]);
+    const int first = slots.before[slot];
     const int item = static_cast<int>(static_cast<uint32_t>(at - first) / static_cast<uint32_t>(s.w.pieces));
     s.item_at = first + item * s.w.pieces;
     s.p_begin = at - s.item_at;
     s.p_end = min(end - s.item_at, s.w.pieces);
-    const int rows = kSparse ? g : s.w.n * g, row_blocks = (rows + kRows - 1) / kRows;
-    const int unit = row_blocks == 1 ? item : item / row_blocks;         // KV head, or token and KV head
-    s.row0 = (item - unit * row_blocks) * kRows;
-    s.kvh = kSparse ? unit % a.Hkv : unit;
-    s.token = kSparse ? unit / a.Hkv : 0;
-    s.n_rows = min(kRows, rows - s.row0);
+    s.kvh = kSparse ? item % a.Hkv : item;
+    s.token = kSparse ? item / a.Hkv : 0;
+    s.n_rows = (kSparse ? 1 : s.w.n) << a.g_shift;
     s.token0 = slot * a.T + s.token;
     s.head0 = s.kvh << a.g_shift;
     return s;

@@ -8,22 +8,20 @@
 
 namespace pulsar {
 
-constexpr int kTile = 128;                       // keys
 constexpr int kPanelBytes = kTile * 128;         // 64 columns of a tile: 128-byte lines, swizzled
 constexpr float kRescale = 8.f;                  // in log2 units
 constexpr float kUnset = 1e30f;                  // stands for minus a maximum that no logit has set: every logit exceeds it
 constexpr int kLeastTiles = 2;                   // of a CTA, unless all CTAs have fewer
 constexpr int kRowsBarrier = 5;                  // named barriers: 1 .. 4 of the softmax warpgroups, this one of warps 2 and 3
-constexpr int kAllRows = 1 << 20;                // (the rows of an item are cut up between CTAs, not between items)
 constexpr int kQueue = 4;                        // segments that the loader may publish ahead of the slowest consumer
 
 // A CTA's pieces of one item, as the loader publishes them.
 struct __align__(16) Work {
     int valid;                                   // 0: no more
-    int slot, p_begin, p_end, cache_pieces;
+    int slot, p_begin, p_end, new_tile;
     int keys, n, row0, n_rows, kvh, token0, head0;
     int part;                                    // place of the partial, -1: all of the item, its outputs are final
-    int len, token, pad_;                        // rows in the slot's cache; selected pages: the item's token
+    int len, token, new_at;                      // rows in the slot's cache; selected pages: the item's token; see SlotWork
 };
 static_assert(sizeof(Work) == 64, "");
 
@@ -62,8 +60,27 @@ __device__ __forceinline__ void add2(float& x0, float& x1, float y0, float y1) {
         : "+f"(x0), "+f"(x1) : "f"(y0), "f"(y1));
 }
 
-// Trees with more than 64 query rows per KV head (paged_wide.cu).  map: K and V of the pool, of the nodes, and Q.
-int32_t launch_tree_wide(const PagedArgs& a, const CUtensorMap (&map)[5], int rows, int d, cudaStream_t stream);
+// Tensor maps of a launch: the pool's pages, runs of 16 rows of them, the new tokens' rows, and the query rows.
+struct Maps {
+    CUtensorMap K, V, K16, V16, Kn, Vn, Q;
+};
+__device__ __forceinline__ void prefetch_maps(const Maps& m) {
+    tma_prefetch_desc(&m.K);
+    tma_prefetch_desc(&m.V);
+    tma_prefetch_desc(&m.K16);
+    tma_prefetch_desc(&m.V16);
+    tma_prefetch_desc(&m.Kn);
+    tma_prefetch_desc(&m.Vn);
+    tma_prefetch_desc(&m.Q);
+}
+
+// How many times 16 keys of tile t the product with V has to read.
+__device__ __forceinline__ int used_steps(int t, int keys, int new_tile, int new_end) {
+    return ((t == new_tile ? new_end : min(keys - t * kTile, kTile)) + 15) / 16;
+}
+
+// Trees with more than 64 query rows per KV head (paged_wide.cu).
+int32_t launch_tree_wide(const PagedArgs& a, const Maps& map, int rows, int d, cudaStream_t stream);
 
 // Shared memory that the roles use besides the tiles, and where the barriers are.
 struct Roles {
@@ -94,8 +111,7 @@ __device__ __forceinline__ const Work* next_work(const PagedArgs& a, const Roles
 
 // ---- loader (one warp): shares out the work, and every lane copies a page ----
 template <class C>
-__device__ __forceinline__ void load_role(const PagedArgs& a, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmKn, const CUtensorMap& tmVn,
-                                          int row_blocks, const Roles& roles) {
+__device__ __forceinline__ void load_role(const PagedArgs& a, const Maps& map, int row_blocks, const Roles& roles) {
     const int lane = threadIdx.x & 31;
     uint8_t* smem = roles.smem;
     Work* s_work = roles.s_work;
@@ -104,11 +120,9 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const CUtensorMap&
     const auto bar = [&](int i) { return roles.bar(i); };
     uint32_t stage = 0, phase = 0;
     bool ok = true;
-    const int per_tile = kTile >> a.page_shift;
-    const uint32_t page_bytes = static_cast<uint32_t>(C::kPanels) << (a.page_shift + 7);
     // More rows than a CTA takes: neighbouring CTAs have the same keys at the same time, and a share of the rows each.
     const int cta = static_cast<int>(blockIdx.x) / row_blocks, n_ctas = static_cast<int>(gridDim.x) / row_blocks;
-    const Shares shares(all_pieces<C::kSparse, kTile, kAllRows>(a, slots), kLeastTiles, n_ctas);
+    const Shares shares(all_pieces<C::kSparse>(a, slots), kLeastTiles, n_ctas);
     const int begin = shares.begin(cta), end = shares.begin(cta + 1);
     int slot_now = begin < end ? slot_at(slots, a.n_slots, begin) : 0, at = begin;
     bool joined = false;                     // an item that begins here goes on elsewhere
@@ -124,7 +138,7 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const CUtensorMap&
             }
             break;
         }
-        const Segment s = segment_at<C::kSparse, kTile, kAllRows>(a, slots, at, end, slot_now);
+        const Segment s = segment_at<C::kSparse>(a, slots, at, end, slot_now);
         const int row0 = static_cast<int>(blockIdx.x) % row_blocks * C::kRows, n_rows = min(s.n_rows - row0, C::kRows);
         const int part = 2 * static_cast<int>(blockIdx.x) + (at == begin ? 0 : 1);
         at = s.item_at + s.p_end;
@@ -133,8 +147,8 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const CUtensorMap&
             continue;
         }
         if (lane == 0) {
-            s_work[place] = Work{1, s.slot, s.p_begin, s.p_end, s.w.cache_pieces, s.w.keys, s.w.n, row0, n_rows, s.kvh, s.token0, s.head0,
-                                 s.p_begin == 0 && s.p_end == s.w.pieces ? -1 : part, s.w.len, s.token, 0};
+            s_work[place] = Work{1, s.slot, s.p_begin, s.p_end, s.w.new_tile, s.w.keys, s.w.n, row0, n_rows, s.kvh, s.token0, s.head0,
+                                 s.p_begin == 0 && s.p_end == s.w.pieces ? -1 : part, s.w.len, s.token, s.w.new_at};
             arrive_a(bar(C::bWorkFull + static_cast<int>(place)));
             if (s.p_begin == 0 && s.p_end < s.w.pieces) {
                 a.meta[blockIdx.x] = {part, shares.owner(s.item_at + s.w.pieces - 1) - cta + 1, row_blocks, s.token0, s.head0, row0, n_rows};
@@ -142,37 +156,35 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const CUtensorMap&
             }
         }
         const int32_t* list = page_list<C::kSparse>(a, s.slot, s.token0, s.kvh);
-        const auto has_page = [&](int t) {                         // this lane has a page of tile t to load
-            return lane < per_tile && t < min(s.p_end, s.w.cache_pieces) && ((t * per_tile + lane) << a.page_shift) < s.w.keys;
-        };
-        const auto page_of = [&](int t) { return has_page(t) ? list[t * per_tile + lane] : 0; };
+        // A tile's rows are copied page by page, a page per lane; those before new tokens in the same tile 16 by 16, up to where these begin.
+        const auto shift_of = [&](int t) { return t == s.w.new_tile ? 4 : a.page_shift; };
+        const auto row_of_lane = [&](int t) { return t * kTile + (lane << shift_of(t)); };
+        const auto has_rows = [&](int t) { return t < s.p_end && lane < kTile >> shift_of(t) && row_of_lane(t) < s.w.keys; };
+        const auto page_of = [&](int t) { return has_rows(t) ? list[row_of_lane(t) >> a.page_shift] : 0; };
         int id = page_of(s.p_begin);
         for (int t = s.p_begin; t < s.p_end && ok; ++t) {
             const int next = page_of(t + 1);                       // (looked at a tile later)
-            const bool fresh = t >= s.w.cache_pieces;
-            int page = has_page(t) ? id : -1;
-            if (has_page(t) && (id < 0 || id >= a.n_pages)) {
+            const bool fresh = t == s.w.new_tile, rows = has_rows(t);
+            int page = id;
+            if (rows && (id < 0 || id >= a.n_pages)) {
                 report(a.status, PULSAR_DEV_BAD_PAGE);             // (some page is loaded; its rows count as absent)
                 page = 0;
             }
-            const uint32_t pages = __ballot_sync(0xffffffffu, page >= 0);
-            const uint32_t bytes = fresh ? static_cast<uint32_t>(C::kPanels * a.fresh_rows) * 128 : __popc(pages) * page_bytes;
+            const int shift = shift_of(t), from = (page << a.page_shift) + (row_of_lane(t) & ((1 << a.page_shift) - 1));
+            const uint32_t lines = (__popc(__ballot_sync(0xffffffffu, rows)) << shift) + (fresh ? a.fresh_rows : 0);
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 __syncwarp();
                 ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bKvEmpty + stage), phase ^ 1, abort_flag, a.status));
                 if (!ok) break;
                 const uint32_t full = bar(C::bKvFull + stage), dst = smem_u32(smem) + stage * C::kTileBytes;
-                if (lane == 0) mbar_expect_tx_a(full, bytes);
+                if (lane == 0) mbar_expect_tx_a(full, static_cast<uint32_t>(C::kPanels) * lines * 128);
                 __syncwarp();
+                const CUtensorMap* pool = fresh ? (kv ? &map.V16 : &map.K16) : (kv ? &map.V : &map.K);
 #pragma unroll
                 for (int p = 0; p < C::kPanels; ++p) {
-                    if (fresh) {
-                        if (lane == 0) tma_load_3d_a(dst + p * kPanelBytes, kv ? &tmVn : &tmKn, full, p * 64, s.kvh, s.slot * a.T);
-                    } else if (page >= 0) {
-                        tma_load_3d_a(dst + p * kPanelBytes + (lane << (a.page_shift + 7)), kv ? &tmV : &tmK, full, p * 64, s.kvh,
-                                      page << a.page_shift);
-                    }
+                    if (rows) tma_load_3d_a(dst + p * kPanelBytes + (lane << (shift + 7)), pool, full, p * 64, s.kvh, from);
+                    if (fresh && lane == 0) tma_load_3d_a(dst + p * kPanelBytes + s.w.new_at * 128, kv ? &map.Vn : &map.Kn, full, p * 64, s.kvh, s.slot * a.T);
                 }
                 if (++stage == C::kStages) {
                     stage = 0;
@@ -187,7 +199,7 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const CUtensorMap&
 
 // ---- two warps: query rows (TMA), which nodes see which, the nodes' rows to their pages ----
 template <int D, class C>
-__device__ __forceinline__ void rows_role(const PagedArgs& a, const CUtensorMap& tmQ, int t, const Roles& roles) {
+__device__ __forceinline__ void rows_role(const PagedArgs& a, const Maps& map, int t, const Roles& roles) {
     const int lane = threadIdx.x & 31;
     uint8_t* smem = roles.smem;
     uint64_t* s_sees = roles.s_sees;
@@ -208,11 +220,13 @@ __device__ __forceinline__ void rows_role(const PagedArgs& a, const CUtensorMap&
             for (int i = 0; i < C::kQTiles; ++i)
 #pragma unroll
                 for (int p = 0; p < C::kPanels; ++p)
-                    tma_load_3d_a(smem_u32(smem) + C::kQ + (i * C::kPanels + p) * (C::kQRows * 128), &tmQ, bar(C::bQFull), p * 64, s.head0,
+                    tma_load_3d_a(smem_u32(smem) + C::kQ + (i * C::kPanels + p) * (C::kQRows * 128), &map.Q, bar(C::bQFull), p * 64, s.head0,
                                   s.token0 + ((s.row0 + i * C::kQRows) >> a.g_shift));
         }
         // (the place in the queue, and with it these buffers, is free when the softmax has left the segment kQueue before)
-        const bool has_new = s.p_end > s.cache_pieces;
+        const bool has_new = s.p_end > s.new_tile;
+        if (t < 2) s_odd[2 * (seq % kQueue) + t] = 0u;
+        named_sync(kRowsBarrier, 64);
         if (has_new) {
             uint64_t* sees = s_sees + (seq % kQueue) * kMaxTree;
             if (C::kSparse) sees[t] = t <= s.token ? 1ull : 0ull;  // (the item's rows are one token's: it sees the tokens up to itself)
@@ -228,23 +242,32 @@ __device__ __forceinline__ void rows_role(const PagedArgs& a, const CUtensorMap&
                 }
             }
         }
-        if (t < 2) s_odd[2 * (seq % kQueue) + t] = 0u;
+        constexpr int kVecs = D / 8;
+        const int64_t from0 = static_cast<int64_t>(s.slot) * a.T * pitch + s.kvh * D;
+        if (has_new) {
+#pragma unroll 4
+            for (int i = t; i < s.n * kVecs; i += 64) {
+                const uint4 y = reinterpret_cast<const uint4*>(a.Vnew + from0 + (i / kVecs) * pitch)[i % kVecs];
+                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+                bool odd = false;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) odd |= (w[k] & 0x7f80u) == 0x7f80u || (w[k] & 0x7f800000u) == 0x7f800000u;
+                if (odd) atomicOr(&s_odd[2 * (seq % kQueue) + (i / kVecs >> 5)], 1u << (i / kVecs & 31));
+            }
+        }
         named_sync(kRowsBarrier, 64);
         if (t == 0) {
             arrive_a(bar(C::bSees + static_cast<int>(seq % kQueue)));
             arrive_a(bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));         // (both warps have their copy)
         }
         if (has_new && s.row0 == 0 && s.token == 0) {
-            constexpr int kVecs = D / 8;
-            const int head_at = s.kvh * D;
-            const int len = s.len;
             for (int i = t; i < s.n * kVecs; i += 64) {
                 const int row = i / kVecs, v = i % kVecs;
-                const int64_t to = new_row_at(a, s.slot, static_cast<int64_t>(len) + row, pitch);
+                const int64_t to = new_row_at(a, s.slot, static_cast<int64_t>(s.len) + row, pitch);
                 if (to < 0) continue;
-                const int64_t from = (static_cast<int64_t>(s.slot) * a.T + row) * pitch + head_at;
-                reinterpret_cast<uint4*>(a.K + to + head_at)[v] = reinterpret_cast<const uint4*>(a.Knew + from)[v];
-                reinterpret_cast<uint4*>(a.V + to + head_at)[v] = reinterpret_cast<const uint4*>(a.Vnew + from)[v];
+                const int64_t from = from0 + row * pitch;
+                reinterpret_cast<uint4*>(a.K + to + s.kvh * D)[v] = reinterpret_cast<const uint4*>(a.Knew + from)[v];
+                reinterpret_cast<uint4*>(a.V + to + s.kvh * D)[v] = reinterpret_cast<const uint4*>(a.Vnew + from)[v];
             }
         }
     }

@@ -94,9 +94,7 @@ __device__ __forceinline__ void column_sums(float (&x)[C], int lane) {
 
 template <int D, int N, bool kSparse>
 __global__ void __launch_bounds__(Cfg<D, N, kSparse>::kThreads, 1)
-paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                  const __grid_constant__ CUtensorMap tmKn, const __grid_constant__ CUtensorMap tmVn, const __grid_constant__ CUtensorMap tmQ,
-                  int row_blocks) {
+paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Maps map, int row_blocks) {
     using C = Cfg<D, N, kSparse>;
     constexpr int kCols = C::kCols;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -141,11 +139,7 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
             mbar_init(bars + C::bWorkEmpty + i, C::kSoftWarps + 2);                    // and the issuer, and warps 2 and 3
         }
         mbar_fence_init();
-        tma_prefetch_desc(&tmK);
-        tma_prefetch_desc(&tmV);
-        tma_prefetch_desc(&tmKn);
-        tma_prefetch_desc(&tmVn);
-        tma_prefetch_desc(&tmQ);
+        prefetch_maps(map);
     }
     if (warp == 1) {
         tmem_alloc(tmem_ptr, C::kTmemCols);
@@ -161,7 +155,7 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
     const Roles roles{smem, s_work, s_seen, s_odd, s_up, &slots, bar0, abort_flag};
 
     if (warp == 0) {
-        load_role<C>(a, tmK, tmV, tmKn, tmVn, row_blocks, roles);
+        load_role<C>(a, map, row_blocks, roles);
     } else if (warp == 1) {
         // ---- matrix instructions: S of a tile, then PV of the tile before it ----
         const bool leader = elect_one();
@@ -173,6 +167,7 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
         uint32_t tile = 0, n_done = 0;                     // tiles issued, segments finished
         uint32_t stage = 0, phase = 0;                     // of the next K or V
         bool ok = true, first = false, last = false;       // of the tile whose PV is due
+        int steps = 0;                                     // and 16 keys times this many of it
         const auto wait = [&](int b, uint32_t parity) {
             __syncwarp();
             ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(b), parity, abort_flag, a.status));
@@ -187,7 +182,7 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
             if (leader) {
 #pragma unroll
                 for (int kk = 0; kk < kTile / 16; ++kk)
-                    umma_ss(tO, desc_v + static_cast<uint64_t>(v_stage * (C::kTileBytes >> 4) + kk * 128), desc_p + static_cast<uint64_t>(kk * 128),
+                    if (kk < steps) umma_ss(tO, desc_v + static_cast<uint64_t>(v_stage * (C::kTileBytes >> 4) + kk * 128), desc_p + static_cast<uint64_t>(kk * 128),
                             kIdescO, first && kk == 0 ? 0u : 1u);
                 umma_commit_a(bar(C::bKvEmpty + static_cast<int>(v_stage)));
                 umma_commit_a(bar(C::bPEmpty));
@@ -198,7 +193,7 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
         for (uint32_t seq = 0;; ++seq) {
             const Work* s = next_work<C>(a, roles, seq, ok);
             if (!ok || s->valid == 0) break;
-            const int p_begin = s->p_begin, p_end = s->p_end;
+            const int p_begin = s->p_begin, p_end = s->p_end, keys = s->keys, new_tile = s->new_tile, new_end = s->new_at + s->n;
             __syncwarp();
             if (lane == 0) arrive_a(bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));
             for (int t = p_begin; t < p_end && ok; ++t, ++tile) {
@@ -231,11 +226,12 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
                 }
                 first = t == p_begin;
                 last = t + 1 == p_end;
+                steps = used_steps(t, keys, new_tile, new_end);
             }
         }
         if (ok && tile > 0) issue_pv(tile - 1);
     } else if (warp < 4) {
-        rows_role<D, C>(a, tmQ, static_cast<int>(threadIdx.x) - 64, roles);
+        rows_role<D, C>(a, map, static_cast<int>(threadIdx.x) - 64, roles);
     } else {
         // ---- softmax and epilogue ----
         const int quarter = warp & 3, group = (warp - 4) >> 2;
@@ -250,20 +246,21 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
             const Work& s = *next_work<C>(a, roles, seg, ok);
             if (named_any(id, 128, !ok) || s.valid == 0) break;
             const int32_t* list = page_list<kSparse>(a, s.slot, s.token0, s.kvh);
-            const int p_begin = s.p_begin, p_end = s.p_end, cache_pieces = s.cache_pieces, n_rows = s.n_rows;
+            const int p_begin = s.p_begin, p_end = s.p_end, new_tile = s.new_tile, n_rows = s.n_rows;
             float sum[kCols];
 #pragma unroll
             for (int c = 0; c < kCols; ++c) sum[c] = 0.f;
             const auto page_of = [&](int t) {              // the page of this thread's key of tile t, -1: there is no such key
                 const int row = t * kTile + key;
-                return t < min(p_end, cache_pieces) && row < s.keys ? list[row >> a.page_shift] : -1;
+                return t < p_end && row < s.keys ? list[row >> a.page_shift] : -1;
             };
             int page = page_of(p_begin);
             bool failed = false;
             for (int t = p_begin; t < p_end; ++t, ++tile) {
                 const int next = page_of(t + 1);           // (looked at a tile later)
-                const bool fresh = t >= cache_pieces;
-                const bool here = fresh ? key < s.n : page >= 0 && page < a.n_pages;
+                const bool fresh = t == new_tile;
+                const int node = fresh ? key - s.new_at : -1;                  // of the new tokens, where this key is one
+                const bool cached = page >= 0 && page < a.n_pages, is_node = node >= 0 && node < s.n;
                 const uint32_t tS = tmem + (tile & 1) * N + col0 + my_lanes;
                 __syncwarp();
                 ok = ok && mbar_wait_a(bar(C::bSFull + static_cast<int>(tile & 1)), (tile >> 1) & 1, abort_flag, a.status);
@@ -273,11 +270,11 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
                     __syncwarp();
                     ok = ok && mbar_wait_a(bar(C::bSees + static_cast<int>(seg % kQueue)), (seg / kQueue) & 1, abort_flag, a.status);
                     const int gs = a.g_shift, per = 1 << gs;
-                    const uint64_t seen = here ? s_seen[(seg % kQueue) * kMaxTree + key] >> ((s.row0 + col0) >> gs) : 0ull;
+                    const uint64_t seen = is_node ? s_seen[(seg % kQueue) * kMaxTree + node] >> ((s.row0 + col0) >> gs) : cached ? ~0ull : 0ull;
                     visible = 0u;                          // every node's bit becomes the bits of its rows
                     for (int c = 0; c < kCols; c += per)
                         if (((seen >> (c >> gs)) & 1ull) != 0ull) visible |= (per == 32 ? ~0u : (1u << per) - 1u) << c;
-                } else if (!here) {
+                } else if (!cached) {
                     visible = 0u;
                 }
                 const bool masked = fresh || __any_sync(0xffffffffu, visible != ~0u);
@@ -372,28 +369,14 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
                 for (int v = 0; v < kCols / 8; ++v)
                     *reinterpret_cast<uint4*>(line + (((v + (group & 1) * 4) ^ (key & 7)) << 4)) = make_uint4(p[4 * v], p[4 * v + 1], p[4 * v + 2], p[4 * v + 3]);
                 if (masked && group == 0) {
-                    // Rows of V that do not exist may hold anything, and 0 * NaN is NaN: they become zeros.  So does a node's value
-                    // that is not finite: nodes that do not see it have weight 0.  The epilogue adds it where it is seen.
+                    // Rows of V that do not exist may hold anything, and 0 * NaN is NaN: they become zeros, as far as the product
+                    // reads.  So does a new token's value that is not finite: those that do not see it have weight 0.  The epilogue adds
+                    // it where it is seen.
                     __syncwarp();
                     ok = ok && mbar_wait_a(bar(C::bKvFull + static_cast<int>(v_stage)), v_phase, abort_flag, a.status);
-                    uint8_t* value = smem + v_stage * C::kTileBytes + key * 128;
-                    bool clear = !here;
-                    if (fresh && here) {
-                        uint32_t odd = 0;
-#pragma unroll
-                        for (int v = 0; v < D / 8; ++v) {
-                            const uint4 y = *reinterpret_cast<const uint4*>(value + (v >> 3) * kPanelBytes + (((v ^ key) & 7) << 4));
-                            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                odd |= (w[k] & 0x7f80u) == 0x7f80u || (w[k] & 0x7f800000u) == 0x7f800000u ? 1u : 0u;
-                        }
-                        if (odd != 0u) {
-                            clear = true;
-                            atomicOr(&s_odd[2 * (seg % kQueue) + (key >> 5)], 1u << (key & 31));
-                        }
-                    }
-                    if (clear) {
+                    const bool odd = is_node && ((s_odd[2 * (seg % kQueue) + (node >> 5)] >> (node & 31)) & 1u) != 0u;
+                    if ((odd || (!cached && !is_node)) && key < 16 * used_steps(t, s.keys, new_tile, s.new_at + s.n)) {
+                        uint8_t* value = smem + v_stage * C::kTileBytes + key * 128;
 #pragma unroll
                         for (int v = 0; v < D / 8; ++v)
                             *reinterpret_cast<uint4*>(value + (v >> 3) * kPanelBytes + (((v ^ key) & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
@@ -435,7 +418,7 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
             ok = ok && mbar_wait_a(bar(C::bOFull), seg & 1, abort_flag, a.status);
             if (named_any(id, 128, !ok)) break;
             tc_fence_after();
-            const uint64_t odd = p_end <= cache_pieces ? 0ull : s_odd[2 * (seg % kQueue)] | static_cast<uint64_t>(s_odd[2 * (seg % kQueue) + 1]) << 32;
+            const uint64_t odd = p_end <= new_tile ? 0ull : s_odd[2 * (seg % kQueue)] | static_cast<uint64_t>(s_odd[2 * (seg % kQueue) + 1]) << 32;
 #pragma unroll 1
             for (int c0 = 0; c0 < kCols; c0 += 16) {
                 uint32_t r[16];
@@ -450,25 +433,32 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
                     const int node = __ffsll(static_cast<long long>(left)) - 1;
                     const uint64_t seen = s_seen[(seg % kQueue) * kMaxTree + node];
                     const float v = __uint_as_float(static_cast<uint32_t>(a.Vnew[(static_cast<int64_t>(s.slot) * a.T + node) * pitch + s.kvh * D + key]) << 16);
-                    const uint8_t* line = smem + C::kP + (group >> 1) * kPanelBytes + node * 128;
+                    const int at = s.new_at + node;
+                    const uint8_t* line = smem + C::kP + (group >> 1) * kPanelBytes + at * 128;
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
                         const int col = c0 + c;
                         if (((seen >> ((s.row0 + col0 + col) >> a.g_shift)) & 1ull) == 0ull) continue;
-                        const uint32_t p = *reinterpret_cast<const uint16_t*>(line + ((((col >> 3) + (group & 1) * 4) ^ (node & 7)) << 4) + (col & 7) * 2);
+                        const uint32_t p = *reinterpret_cast<const uint16_t*>(line + ((((col >> 3) + (group & 1) * 4) ^ (at & 7)) << 4) + (col & 7) * 2);
                         o[c] = fmaf(__uint_as_float(p << 16), v, o[c]);
                     }
                 }
+                int64_t to[16];                            // (read before the first store, which they could depend on)
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    to[c] = s_to[col0 + c0 + c] + key;
+                    o[c] *= s_inv[col0 + c0 + c];
+                }
                 const int n = min(16, n_rows - (col0 + c0));
-                float* to_f = whole ? static_cast<float*>(a.O) : a.part_O;
                 if (!whole || a.out_f32) {
+                    float* out = whole ? static_cast<float*>(a.O) : a.part_O;
 #pragma unroll
                     for (int c = 0; c < 16; ++c)
-                        if (c < n) to_f[s_to[col0 + c0 + c] + key] = o[c] * s_inv[col0 + c0 + c];
+                        if (c < n) out[to[c]] = o[c];
                 } else {
 #pragma unroll
                     for (int c = 0; c < 16; ++c)
-                        if (c < n) static_cast<__nv_bfloat16*>(a.O)[s_to[col0 + c0 + c] + key] = __float2bfloat16_rn(o[c] * s_inv[col0 + c0 + c]);
+                        if (c < n) static_cast<__nv_bfloat16*>(a.O)[to[c]] = __float2bfloat16_rn(o[c]);
                 }
             }
             tc_fence_before();
@@ -494,17 +484,17 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
 int item_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
 template <int D, int N, bool kSparse>
-int32_t launch(const PagedArgs& a, const CUtensorMap (&map)[5], cudaStream_t stream) {
+int32_t launch(const PagedArgs& a, const Maps& map, cudaStream_t stream) {
     using C = Cfg<D, N, kSparse>;
     const auto kernel = paged_tiles_kernel<D, N, kSparse>;
     const unsigned ctas = static_cast<unsigned>(sm_count());
     PULSAR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
-    PULSAR_CUDA_OK(launch_kernel(kernel, dim3(ctas), dim3(C::kThreads), C::kSmem, stream, true, a, map[0], map[1], map[2], map[3], map[4], 1));
+    PULSAR_CUDA_OK(launch_kernel(kernel, dim3(ctas), dim3(C::kThreads), C::kSmem, stream, true, a, map, 1));
     count_launch();
     return launch_parts_merge(a, ctas, N, D, stream);
 }
 template <int D>
-int32_t launch_rows(const PagedArgs& a, const CUtensorMap (&map)[5], int n, cudaStream_t stream) {
+int32_t launch_rows(const PagedArgs& a, const Maps& map, int n, cudaStream_t stream) {
     if (a.list != nullptr) return launch<D, 16, true>(a, map, stream);
     switch (n) {
         case 16: return launch<D, 16, false>(a, map, stream);
@@ -515,20 +505,22 @@ int32_t launch_rows(const PagedArgs& a, const CUtensorMap (&map)[5], int n, cuda
 
 }  // namespace
 
-bool attn_pieces_ok(int64_t n_slots, int64_t items, int64_t keys, int64_t T) { return pieces_ok(n_slots, items, keys, T, kTile); }
-
 size_t attn_workspace_bytes(int rows, int d) { return PartScratch(sm_count(), item_rows(rows), d).total; }
 
 int32_t launch_attn(PagedArgs a, int rows, int d, void* workspace, cudaStream_t stream) {
     const int n = item_rows(rows);
     PartScratch(sm_count(), n, d).place(a, workspace);
     a.fresh_rows = static_cast<int>(round_up(a.T, 8));
-    CUtensorMap map[5];
+    Maps map;
     const int64_t pool_rows = static_cast<int64_t>(a.n_pages) << a.page_shift, fresh_rows = static_cast<int64_t>(a.n_slots) * a.T;
-    if (!make_map_3d(&map[0], a.K, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) || !make_map_3d(&map[1], a.V, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) ||
-        !make_map_3d(&map[2], a.Knew, fresh_rows, a.Hkv, d, 1, a.fresh_rows) || !make_map_3d(&map[3], a.Vnew, fresh_rows, a.Hkv, d, 1, a.fresh_rows) ||
-        !make_map_3d(&map[4], a.Q, fresh_rows, a.Hq, d, 1 << a.g_shift, std::min(n, 128) >> a.g_shift))
-        return PULSAR_ERR_CUDA;
+    bool ok = make_map_3d(&map.K, a.K, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) && make_map_3d(&map.V, a.V, pool_rows, a.Hkv, d, 1, 1 << a.page_shift) &&
+              make_map_3d(&map.Kn, a.Knew, fresh_rows, a.Hkv, d, 1, a.fresh_rows) && make_map_3d(&map.Vn, a.Vnew, fresh_rows, a.Hkv, d, 1, a.fresh_rows) &&
+              make_map_3d(&map.Q, a.Q, fresh_rows, a.Hq, d, 1 << a.g_shift, std::min(n, 128) >> a.g_shift);
+    map.K16 = map.K;
+    map.V16 = map.V;
+    if (a.page_shift != 4)
+        ok = ok && make_map_3d(&map.K16, a.K, pool_rows, a.Hkv, d, 1, 16) && make_map_3d(&map.V16, a.V, pool_rows, a.Hkv, d, 1, 16);
+    if (!ok) return PULSAR_ERR_CUDA;
     if (n > 64) return launch_tree_wide(a, map, rows, d, stream);
     return d == 128 ? launch_rows<128>(a, map, n, stream) : launch_rows<64>(a, map, n, stream);
 }

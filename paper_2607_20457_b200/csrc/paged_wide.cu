@@ -47,9 +47,7 @@ __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 
 
 template <int D, bool kTwo>
 __global__ void __launch_bounds__(kThreads, 1)
-tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                 const __grid_constant__ CUtensorMap tmKn, const __grid_constant__ CUtensorMap tmVn, const __grid_constant__ CUtensorMap tmQ,
-                 int row_blocks) {
+tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Maps map, int row_blocks) {
     using C = Wide<D, kTwo>;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* s_sees = reinterpret_cast<uint64_t*>(smem + C::kRest);
@@ -85,11 +83,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
             mbar_init(bars + C::bWorkEmpty + i, 8 + 2);
         }
         mbar_fence_init();
-        tma_prefetch_desc(&tmK);
-        tma_prefetch_desc(&tmV);
-        tma_prefetch_desc(&tmKn);
-        tma_prefetch_desc(&tmVn);
-        tma_prefetch_desc(&tmQ);
+        prefetch_maps(map);
     }
     if (warp == 1) {
         tmem_alloc(tmem_ptr, 512);
@@ -104,7 +98,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
     const Roles roles{smem, s_work, s_sees, s_odd, s_up, &slots, bar0, abort_flag};
 
     if (warp == 0) {
-        load_role<C>(a, tmK, tmV, tmKn, tmVn, row_blocks, roles);
+        load_role<C>(a, map, row_blocks, roles);
     } else if (warp == 1) {
         // ---- matrix instructions.  They run in the order of issue, so S of a stream's next tile may follow PV of the tile before into the
         // same columns, and a full S means that the PV before it is done. ----
@@ -114,6 +108,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
         const uint64_t desc_v = umma_smem_desc_sw128(smem_u32(smem), kPanelBytes, 1024);
         const uint64_t desc_q = umma_smem_desc_sw128(smem_u32(smem + C::kQ), 16, 1024);
         uint32_t tile = 0, stage = 0, phase = 0, v_stage = 0, v_phase = 0;
+        int steps = 0;                                     // of 16 keys, of the tile whose PV is due
         uint32_t o_use[2] = {0, 0};                        // items that the stream has begun
         bool ok = true, first = false, last = false;       // of the tile whose PV is due (kTwo: the item's first, last; else the stream's)
         const auto wait = [&](int b, uint32_t parity) {
@@ -141,7 +136,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
             if (leader) {
 #pragma unroll
                 for (int kk = 0; kk < kTile / 16; ++kk)
-                    umma_ts(tmem + 256 + h * 128, tmem + h * 128 + kk * 8, desc_v + static_cast<uint64_t>(v_stage * (C::kTileBytes >> 4) + kk * 128), kIdescO,
+                    if (kk < steps) umma_ts(tmem + 256 + h * 128, tmem + h * 128 + kk * 8, desc_v + static_cast<uint64_t>(v_stage * (C::kTileBytes >> 4) + kk * 128), kIdescO,
                             first && kk == 0 ? 0u : 1u);
                 if (release_v) umma_commit_a(bar(C::bKvEmpty + static_cast<int>(v_stage)));
                 if (last) umma_commit_a(bar(C::bOFull + h));
@@ -157,7 +152,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
         for (uint32_t seq = 0;; ++seq) {
             const Work* s = next_work<C>(a, roles, seq, ok);
             if (!ok || s->valid == 0) break;
-            const int p_begin = s->p_begin, p_end = s->p_end;
+            const int p_begin = s->p_begin, p_end = s->p_end, keys = s->keys, new_tile = s->new_tile, new_end = s->new_at + s->n;
             __syncwarp();
             if (lane == 0) arrive_a(bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));
             for (int t = p_begin; t < p_end && ok; ++t, ++tile) {
@@ -190,6 +185,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
                 next_stage();
                 first = t - p_begin < (kTwo ? 1 : 2);
                 last = t >= p_end - (kTwo ? 1 : 2);
+                steps = used_steps(t, keys, new_tile, new_end);
             }
         }
         if (ok && tile > 0) {
@@ -202,7 +198,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
             }
         }
     } else if (warp < 4) {
-        rows_role<D, C>(a, tmQ, static_cast<int>(threadIdx.x) - 64, roles);
+        rows_role<D, C>(a, map, static_cast<int>(threadIdx.x) - 64, roles);
     } else {
         // ---- softmax and epilogue: a thread per row ----
         const int h = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
@@ -220,11 +216,11 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
                 break;
             }
             if (s.valid == 0) break;
-            const int p_begin = s.p_begin, p_end = s.p_end, cache_pieces = s.cache_pieces, keys = s.keys, n = s.n;
+            const int p_begin = s.p_begin, p_end = s.p_end, new_tile = s.new_tile, keys = s.keys;
             const int my_row = (kTwo ? h * 128 : 0) + row;                  // of the CTA's rows
             const bool exists = my_row < s.n_rows;
             const int32_t* list = a.table + static_cast<int64_t>(s.slot) * a.max_pages;
-            const auto has_page = [&](int t) { return lane < per_tile && t < min(p_end, cache_pieces) && ((t * per_tile + lane) << a.page_shift) < keys; };
+            const auto has_page = [&](int t) { return lane < per_tile && t < p_end && ((t * per_tile + lane) << a.page_shift) < keys; };
             const auto page_of = [&](int t) { return has_page(t) ? list[t * per_tile + lane] : 0; };
             constexpr int kStep = kTwo ? 1 : 2;
             const int t_first = kTwo ? p_begin : p_begin + static_cast<int>((h ^ tile) & 1u);      // this stream's first tile
@@ -235,31 +231,36 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
             for (int t = p_begin; t < p_end; ++t, ++tile) {
                 if (kTwo || t >= t_first && ((t - t_first) & 1) == 0) {
                     const int next = page_of(t + kStep);                    // (looked at a tile later)
-                    const bool fresh = t >= cache_pieces;
+                    const bool fresh = t == new_tile;
                     __syncwarp();
                     ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bSFull + h), (kTwo ? tile : tile >> 1) & 1, abort_flag, a.status));
                     // ---- which of the tile's keys the row sees: a bit each ----
                     uint32_t see[4] = {~0u, ~0u, ~0u, ~0u};
-                    bool plain = true;
+                    bool plain = true, is_key = true;
+                    const uint32_t bad = __ballot_sync(0xffffffffu, has_page(t) && (id < 0 || id >= a.n_pages));
+                    if (fresh || bad != 0u || keys - t * kTile < kTile) {
+                        plain = false;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            see[c] = low_bits(keys - t * kTile - 32 * c);
+                            for (int k = 0; k < 32; k += 16)                // (pages are 16 rows or more)
+                                if ((bad >> ((32 * c + k) >> a.page_shift)) & 1u) see[c] &= ~(0xffffu << k);
+                        }
+                    }
+                    if (!plain && (!kTwo || h == 0)) is_key = ((row < 32 ? see[0] : row < 64 ? see[1] : row < 96 ? see[2] : see[3]) >> (row & 31)) & 1u;
                     if (fresh) {
                         ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bSees + static_cast<int>(seg % kQueue)), (seg / kQueue) & 1, abort_flag, a.status));
                         sees = exists ? s_sees[(seg % kQueue) * kMaxTree + ((s.row0 + my_row) >> a.g_shift)] : 0ull;
-                        see[0] = static_cast<uint32_t>(sees);
-                        see[1] = static_cast<uint32_t>(sees >> 32);
-                        see[2] = see[3] = 0u;
-                        plain = false;
-                        had_fresh = true;
-                    } else {
-                        const uint32_t bad = __ballot_sync(0xffffffffu, has_page(t) && (id < 0 || id >= a.n_pages));
-                        if (bad != 0u || keys - t * kTile < kTile) {
-                            plain = false;
+                        // its nodes from new_at on: 64 bits moved up by a multiple of 16
+                        const int up = s.new_at & 31, word = s.new_at >> 5;
+                        const uint32_t lo = static_cast<uint32_t>(sees), hi = static_cast<uint32_t>(sees >> 32);
+                        const uint32_t b[3] = {lo << up, __funnelshift_l(lo, hi, up), up == 0 ? 0u : hi >> (32 - up)};
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                see[c] = low_bits(keys - t * kTile - 32 * c);
-                                for (int k = 0; k < 32; k += 16)            // (pages are 16 rows or more)
-                                    if ((bad >> ((32 * c + k) >> a.page_shift)) & 1u) see[c] &= ~(0xffffu << k);
-                            }
-                        }
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int k = 0; k < 3; ++k)
+                                if (c == word + k) see[c] |= b[k];
+                        had_fresh = true;
                     }
                     tc_fence_after();
                     float x[32];
@@ -319,27 +320,13 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
                     }
                     if (!plain && (!kTwo || h == 0)) {
                         // Rows of V that do not exist become zeros, and so does a node's value that is not finite (0 * NaN is NaN): see
-                        // paged_tiles.cu.  Thread `row` has key `row`.
+                        // paged_tiles.cu.  Thread `row` has key `row` here.
                         ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bKvFull + static_cast<int>(v_stage)), v_phase, abort_flag, a.status));
-                        uint8_t* value = smem + v_stage * C::kTileBytes + row * 128;
-                        const uint32_t word = row < 32 ? see[0] : row < 64 ? see[1] : row < 96 ? see[2] : see[3];
-                        bool clear = fresh ? row >= n : ((word >> (row & 31)) & 1u) == 0u;
-                        if (fresh && !clear) {
-                            uint32_t odd = 0;
-#pragma unroll
-                            for (int v = 0; v < D / 8; ++v) {
-                                const uint4 y = *reinterpret_cast<const uint4*>(value + (v >> 3) * kPanelBytes + (((v ^ row) & 7) << 4));
-                                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                                for (int k = 0; k < 4; ++k)
-                                    odd |= (w[k] & 0x7f80u) == 0x7f80u || (w[k] & 0x7f800000u) == 0x7f800000u ? 1u : 0u;
-                            }
-                            if (odd != 0u) {
-                                clear = true;
-                                atomicOr(&s_odd[2 * (seg % kQueue) + (row >> 5)], 1u << (row & 31));
-                            }
-                        }
-                        if (clear) {
+                        const int node = fresh ? row - s.new_at : -1;
+                        const bool is_node = node >= 0 && node < s.n;
+                        const bool odd = is_node && ((s_odd[2 * (seg % kQueue) + (node >> 5)] >> (node & 31)) & 1u) != 0u;
+                        if ((odd || (!is_key && !is_node)) && row < 16 * used_steps(t, keys, new_tile, s.new_at + s.n)) {
+                            uint8_t* value = smem + v_stage * C::kTileBytes + row * 128;
 #pragma unroll
                             for (int v = 0; v < D / 8; ++v)
                                 *reinterpret_cast<uint4*>(value + (v >> 3) * kPanelBytes + (((v ^ row) & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
@@ -470,19 +457,18 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 }
 
 template <int D, bool kTwo>
-int32_t launch(const PagedArgs& a, const CUtensorMap (&map)[5], int rows, cudaStream_t stream) {
+int32_t launch(const PagedArgs& a, const Maps& map, int rows, cudaStream_t stream) {
     using C = Wide<D, kTwo>;
     const unsigned ctas = static_cast<unsigned>(sm_count());
     PULSAR_CUDA_OK(cudaFuncSetAttribute(tree_wide_kernel<D, kTwo>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
-    PULSAR_CUDA_OK(launch_kernel(tree_wide_kernel<D, kTwo>, dim3(ctas), dim3(kThreads), C::kSmem, stream, true, a, map[0], map[1], map[2], map[3], map[4],
-                                 (rows + C::kRows - 1) / C::kRows));
+    PULSAR_CUDA_OK(launch_kernel(tree_wide_kernel<D, kTwo>, dim3(ctas), dim3(kThreads), C::kSmem, stream, true, a, map, (rows + C::kRows - 1) / C::kRows));
     count_launch();
     return launch_parts_merge(a, ctas, C::kRows, D, stream);
 }
 
 }  // namespace
 
-int32_t launch_tree_wide(const PagedArgs& a, const CUtensorMap (&map)[5], int rows, int d, cudaStream_t stream) {
+int32_t launch_tree_wide(const PagedArgs& a, const Maps& map, int rows, int d, cudaStream_t stream) {
     if (d == 128) return rows > 128 ? launch<128, true>(a, map, rows, stream) : launch<128, false>(a, map, rows, stream);
     return rows > 128 ? launch<64, true>(a, map, rows, stream) : launch<64, false>(a, map, rows, stream);
 }

@@ -124,11 +124,11 @@ struct Slots {
     int len[kMaxSlots];
     unsigned char n[kMaxSlots];
 };
-// One warp fills it in; returns the pieces of all slots.
+// One warp fills it in; returns the pieces of all slots, and how many items they are of.
 template <bool kSparse>
-__device__ __forceinline__ int all_pieces(const PagedArgs& a, Slots& slots) {
+__device__ __forceinline__ int all_pieces(const PagedArgs& a, Slots& slots, int& items) {
     const int lane = threadIdx.x & 31;
-    int total = 0;
+    int total = 0, mine = 0;
     for (int s0 = 0; s0 < a.n_slots; s0 += 32) {
         const int s = s0 + lane;
         int x = 0;
@@ -137,6 +137,7 @@ __device__ __forceinline__ int all_pieces(const PagedArgs& a, Slots& slots) {
             const int n = a.n_draft != nullptr ? min(max(a.n_draft[s], 0), a.T) : a.T;
             const SlotWork w = slot_work<kSparse>(a, len, n);
             x = w.pieces * w.items;
+            mine += w.items;
             slots.len[s] = len;
             slots.n[s] = static_cast<unsigned char>(n);
         }
@@ -150,6 +151,7 @@ __device__ __forceinline__ int all_pieces(const PagedArgs& a, Slots& slots) {
         total += __shfl_sync(0xffffffffu, y, 31);
     }
     if (lane == 0) slots.before[a.n_slots] = total;
+    items = __reduce_add_sync(0xffffffffu, mine);
     __syncwarp();
     return total;
 }
@@ -157,8 +159,8 @@ __device__ __forceinline__ int all_pieces(const PagedArgs& a, Slots& slots) {
 // Equal shares of `total` pieces: the first `more` of n have one more than the others.
 struct Shares {
     uint32_t n, each, more;
-    __device__ __forceinline__ Shares(int total, int least, int ctas) {
-        n = static_cast<uint32_t>(max(1, min(ctas, total / least)));
+    __device__ __forceinline__ Shares(int total, int wanted, int ctas) {
+        n = static_cast<uint32_t>(max(1, min(ctas, min(wanted, total))));
         each = static_cast<uint32_t>(total) / n;
         more = static_cast<uint32_t>(total) - each * n;
     }
@@ -222,35 +224,6 @@ __device__ __forceinline__ int64_t new_row_at(const PagedArgs& a, int slot, int6
     return ((static_cast<int64_t>(page) << a.page_shift) + (row & ((1 << a.page_shift) - 1))) * pitch;
 }
 
-// A node's ancestors and itself, as a bit per node, for the first kMaxTree threads that call this together (sync: their barrier,
-// sees: their result [kMaxTree], up: scratch [kMaxTree]).  Pointers to ancestors are doubled: six steps for 64 nodes.
-template <typename Sync>
-__device__ __forceinline__ void ancestors(const PagedArgs& a, int slot, int n, int t, uint64_t* sees, int* up, Sync sync) {
-    int to = -1;
-    if (t < n) {
-        to = a.parent != nullptr ? a.parent[static_cast<int64_t>(slot) * a.T + t] : t - 1;
-        if (to < -1 || to >= t) {
-            report(a.status, PULSAR_DEV_BAD_TREE);
-            to = -1;
-        }
-    }
-    uint64_t mine = t < kMaxTree ? 1ull << t : 0ull;
-#pragma unroll 1
-    for (int step = 1; step < kMaxTree; step <<= 1) {
-        if (t < kMaxTree) {
-            sees[t] = mine;
-            up[t] = to;
-        }
-        sync();
-        if (t < kMaxTree && to >= 0) {
-            mine |= sees[to];
-            to = up[to];
-        }
-        sync();
-    }
-    if (t < kMaxTree) sees[t] = mine;
-    sync();
-}
 #endif
 
 }  // namespace pulsar

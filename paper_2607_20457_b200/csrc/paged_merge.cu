@@ -1,4 +1,4 @@
-// Joins the parts of the items that several CTAs of an attention launch share: O = sum_j e^{l_j - l} A_j (Appendix H's closed form),
+// Behind an attention launch: writes the new tokens' rows to their pages, and joins the parts of the items that several of its CTAs share: O = sum_j e^{l_j - l} A_j (Appendix H's closed form),
 // in the order of the keys, whatever order the CTAs ran in.
 //
 // What bounds it is latency: reads of l, then of the outputs, from L2.  A warp takes kTogether rows side by side, with the parts' l in its
@@ -15,16 +15,40 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kUnder = 4;                        // parts of a row under way
 
+// The new tokens' rows to their pages: copied here, by CTAs of their own, because the attention's warps have better things to do (a
+// warp of its own took 16 us for 64 rows) and nobody reads those rows before the next call.
+template <int D>
+__device__ __forceinline__ void append_rows(const PagedArgs& a) {
+    constexpr int kVecs = D / 8;
+    const uint32_t row_vecs = static_cast<uint32_t>(a.Hkv * kVecs), step = gridDim.x * 32 * kWarps;
+    const uint64_t all = static_cast<uint64_t>(a.n_slots) * a.T * row_vecs;
+    for (uint64_t i = blockIdx.x * (32 * kWarps) + threadIdx.x; i < all; i += step) {
+        const uint32_t token = static_cast<uint32_t>(i / row_vecs), v = static_cast<uint32_t>(i - static_cast<uint64_t>(token) * row_vecs);
+        const int slot = static_cast<int>(token / a.T), t = static_cast<int>(token - slot * a.T);
+        const uint4 k = reinterpret_cast<const uint4*>(a.Knew)[i], x = reinterpret_cast<const uint4*>(a.Vnew)[i];
+        if (a.n_draft != nullptr && t >= a.n_draft[slot]) continue;
+        const int len = checked_len(a.len[slot], static_cast<int64_t>(a.max_pages) << a.page_shift, false, nullptr);
+        const int64_t to = new_row_at(a, slot, static_cast<int64_t>(len) + t, static_cast<int64_t>(a.Hkv) * D);
+        if (to < 0) continue;
+        reinterpret_cast<uint4*>(a.K + to)[v] = k;
+        reinterpret_cast<uint4*>(a.V + to)[v] = x;
+    }
+}
+
 template <int D, int kTogether>
 __global__ void __launch_bounds__(32 * kWarps)
-paged_merge_kernel(const Meta* __restrict__ meta, const float* __restrict__ part_O, const float* __restrict__ part_LSE, int n, int g_shift, int Hq,
-                   void* O, int out_f32, float* LSE) {
+paged_merge_kernel(const __grid_constant__ PagedArgs a, int n) {
+    const float *part_O = a.part_O, *part_LSE = a.part_LSE;
     constexpr int kPer = D / 32;                 // consecutive outputs of a lane
     using Vec = typename std::conditional<kPer == 4, float4, float2>::type;
     grid_dependency_wait();
     grid_launch_dependents();
-    const Meta x = meta[blockIdx.x];
-    const int lane = threadIdx.x & 31, r0 = (blockIdx.y * kWarps + (threadIdx.x >> 5)) * kTogether;
+    if (blockIdx.y == 0) {
+        append_rows<D>(a);
+        return;
+    }
+    const Meta x = a.meta[blockIdx.x];
+    const int lane = threadIdx.x & 31, r0 = ((blockIdx.y - 1) * kWarps + (threadIdx.x >> 5)) * kTogether;
     if (x.parts < 2 || r0 >= x.rows) return;
     const auto place_of = [&](int j) { return static_cast<int64_t>(j == 0 ? x.first : 2 * (static_cast<int>(blockIdx.x) + j * x.step)) * n + r0; };
     float m[kTogether], total[kTogether], acc[kTogether][kPer];
@@ -83,16 +107,16 @@ paged_merge_kernel(const Meta* __restrict__ meta, const float* __restrict__ part
     for (int r = 0; r < kTogether; ++r) {
         if (r0 + r >= x.rows) break;
         const float inv = total[r] == 0.f ? 0.f : 1.f / total[r];
-        const int64_t row = row_of(x.token0, x.head0, x.row0, r0 + r, g_shift, Hq);
-        if (out_f32) {
+        const int64_t row = row_of(x.token0, x.head0, x.row0, r0 + r, a.g_shift, a.Hq);
+        if (a.out_f32) {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) static_cast<float*>(O)[row * D + lane * kPer + i] = acc[r][i] * inv;
+            for (int i = 0; i < kPer; ++i) static_cast<float*>(a.O)[row * D + lane * kPer + i] = acc[r][i] * inv;
         } else {
 #pragma unroll
             for (int i = 0; i < kPer; i += 2)
-                reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(O) + row * D + lane * kPer)[i / 2] = pack_bf16x2(acc[r][i] * inv, acc[r][i + 1] * inv);
+                reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.O) + row * D + lane * kPer)[i / 2] = pack_bf16x2(acc[r][i] * inv, acc[r][i + 1] * inv);
         }
-        if (lane == 0 && LSE != nullptr) LSE[row] = total[r] == 0.f ? -INFINITY : m[r] + logf(total[r]);
+        if (lane == 0 && a.LSE != nullptr) a.LSE[row] = total[r] == 0.f ? -INFINITY : m[r] + logf(total[r]);
     }
 }
 
@@ -103,8 +127,7 @@ int32_t launch_parts_merge(const PagedArgs& a, unsigned ctas, int rows, int d, c
     const auto kernel = d == 128 ? (together == 1 ? paged_merge_kernel<128, 1> : together == 2 ? paged_merge_kernel<128, 2> : paged_merge_kernel<128, 4>)
                                  : (together == 1 ? paged_merge_kernel<64, 1> : together == 2 ? paged_merge_kernel<64, 2> : paged_merge_kernel<64, 4>);
     const unsigned row_ctas = static_cast<unsigned>((rows + together * kWarps - 1) / (together * kWarps));
-    PULSAR_CUDA_OK(launch_kernel(kernel, dim3(ctas, row_ctas), dim3(32 * kWarps), 0, stream, true, a.meta, a.part_O, a.part_LSE, rows, a.g_shift, a.Hq, a.O,
-                                 a.out_f32, a.LSE));
+    PULSAR_CUDA_OK(launch_kernel(kernel, dim3(ctas, 1 + row_ctas), dim3(32 * kWarps), 0, stream, true, a, rows));
     count_launch();
     return PULSAR_OK;
 }

@@ -1,5 +1,5 @@
-// What the tensor-core kernels for drafted trees share: the loader of the pages, and the warps that fetch query rows, work out which
-// node sees which and write the nodes' rows to their pages.  A kernel's configuration C has its shared-memory layout, its barriers
+// What the attention kernels over a paged cache share: the loader of the pages, and the warps that fetch query rows and work out
+// which token sees which.  A kernel's configuration C has its shared-memory layout, its barriers
 // and its tile sizes.
 #pragma once
 
@@ -11,8 +11,7 @@ namespace pulsar {
 constexpr int kPanelBytes = kTile * 128;         // 64 columns of a tile: 128-byte lines, swizzled
 constexpr float kRescale = 8.f;                  // in log2 units
 constexpr float kUnset = 1e30f;                  // stands for minus a maximum that no logit has set: every logit exceeds it
-constexpr int kLeastTiles = 2;                   // of a CTA, unless all CTAs have fewer
-constexpr int kRowsBarrier = 5;                  // named barriers: 1 .. 4 of the softmax warpgroups, this one of warps 2 and 3
+constexpr int kLeastTiles = 2;                   // of a CTA, where items are cut up
 constexpr int kQueue = 4;                        // segments that the loader may publish ahead of the slowest consumer
 
 // A CTA's pieces of one item, as the loader publishes them.
@@ -122,7 +121,9 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const Maps& map, i
     bool ok = true;
     // More rows than a CTA takes: neighbouring CTAs have the same keys at the same time, and a share of the rows each.
     const int cta = static_cast<int>(blockIdx.x) / row_blocks, n_ctas = static_cast<int>(gridDim.x) / row_blocks;
-    const Shares shares(all_pieces<C::kSparse>(a, slots), kLeastTiles, n_ctas);
+    int items;
+    const int total = all_pieces<C::kSparse>(a, slots, items);
+    const Shares shares(total, max(total / kLeastTiles, items), n_ctas);
     const int begin = shares.begin(cta), end = shares.begin(cta + 1);
     int slot_now = begin < end ? slot_at(slots, a.n_slots, begin) : 0, at = begin;
     bool joined = false;                     // an item that begins here goes on elsewhere
@@ -197,78 +198,109 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const Maps& map, i
     if (lane == 0 && !joined) a.meta[blockIdx.x].parts = 0;
 }
 
-// ---- two warps: query rows (TMA), which nodes see which, the nodes' rows to their pages ----
-template <int D, class C>
-__device__ __forceinline__ void rows_role(const PagedArgs& a, const Maps& map, int t, const Roles& roles) {
+// ---- a warp: query rows (TMA) ----
+template <class C>
+__device__ __forceinline__ void rows_role(const PagedArgs& a, const Maps& map, const Roles& roles) {
     const int lane = threadIdx.x & 31;
-    uint8_t* smem = roles.smem;
-    uint64_t* s_sees = roles.s_sees;
-    uint32_t* s_odd = roles.s_odd;
-    int* s_up = roles.s_up;
-    volatile int* abort_flag = roles.abort_flag;
-    const int64_t pitch = static_cast<int64_t>(a.Hkv) * D;
-    const auto bar = [&](int i) { return roles.bar(i); };
     bool ok = true;
     for (uint32_t seq = 0;; ++seq) {
         const Work* work = next_work<C>(a, roles, seq, ok);
-        ok = ok && mbar_wait_a(bar(C::bQEmpty), (seq & 1) ^ 1, abort_flag, a.status);
-        if (named_any(kRowsBarrier, 64, !ok) || work->valid == 0) break;
+        ok = __all_sync(0xffffffffu, ok && mbar_wait_a(roles.bar(C::bQEmpty), (seq & 1) ^ 1, roles.abort_flag, a.status));
+        if (!ok || work->valid == 0) break;
         const Work s = *work;
-        if (t == 0) {                                  // (rows past the item's are other slots', or zeros: nobody reads their outputs)
-            mbar_expect_tx_a(bar(C::bQFull), C::kQBytes);
+        __syncwarp();
+        if (lane == 0) {                                   // (rows past the item's are other slots', or zeros: nobody reads their outputs)
+            arrive_a(roles.bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));
+            mbar_expect_tx_a(roles.bar(C::bQFull), C::kQBytes);
 #pragma unroll
             for (int i = 0; i < C::kQTiles; ++i)
 #pragma unroll
                 for (int p = 0; p < C::kPanels; ++p)
-                    tma_load_3d_a(smem_u32(smem) + C::kQ + (i * C::kPanels + p) * (C::kQRows * 128), &map.Q, bar(C::bQFull), p * 64, s.head0,
+                    tma_load_3d_a(smem_u32(roles.smem) + C::kQ + (i * C::kPanels + p) * (C::kQRows * 128), &map.Q, roles.bar(C::bQFull), p * 64, s.head0,
                                   s.token0 + ((s.row0 + i * C::kQRows) >> a.g_shift));
         }
+    }
+}
+
+// ---- a warp: which new tokens see which, and which of their values are not finite.  A lane has tokens lane and lane + 32. ----
+template <int D, class C>
+__device__ __forceinline__ void nodes_role(const PagedArgs& a, const Roles& roles) {
+    constexpr int kVecs = D / 8;
+    const int lane = threadIdx.x & 31;
+    const int64_t pitch = static_cast<int64_t>(a.Hkv) * D;
+    int* s_up = roles.s_up;
+    bool ok = true;
+    for (uint32_t seq = 0;; ++seq) {
         // (the place in the queue, and with it these buffers, is free when the softmax has left the segment kQueue before)
-        const bool has_new = s.p_end > s.new_tile;
-        if (t < 2) s_odd[2 * (seq % kQueue) + t] = 0u;
-        named_sync(kRowsBarrier, 64);
-        if (has_new) {
-            uint64_t* sees = s_sees + (seq % kQueue) * kMaxTree;
-            if (C::kSparse) sees[t] = t <= s.token ? 1ull : 0ull;  // (the item's rows are one token's: it sees the tokens up to itself)
-            else ancestors(a, s.slot, s.n, t, sees, s_up, [] { named_sync(kRowsBarrier, 64); });
-            if (C::kBySeen && !C::kSparse) {                                      // turned round: the nodes that see a node
-                const uint64_t mine = sees[t];
-                uint32_t* seen = reinterpret_cast<uint32_t*>(sees);
-                named_sync(kRowsBarrier, 64);
-#pragma unroll 8
-                for (int node = 0; node < kMaxTree; ++node) {      // this warp's 32 nodes that see `node`
-                    const uint32_t by = __ballot_sync(0xffffffffu, ((mine >> node) & 1ull) != 0ull);
-                    if (lane == (node & 31)) seen[2 * node + (t >> 5)] = by;
+        const Work* work = next_work<C>(a, roles, seq, ok);
+        if (!ok || work->valid == 0) break;
+        const int n = work->p_end > work->new_tile ? work->n : 0, slot = work->slot, token = work->token;
+        uint64_t* sees = roles.s_sees + (seq % kQueue) * kMaxTree;
+        uint32_t* s_odd = roles.s_odd + 2 * (seq % kQueue);
+        if (lane < 2) s_odd[lane] = 0u;
+        __syncwarp();
+        const uint4* value = reinterpret_cast<const uint4*>(a.Vnew + static_cast<int64_t>(slot) * a.T * pitch + work->kvh * D);
+#pragma unroll 4
+        for (int i = lane; i < n * kVecs; i += 32) {
+            const uint4 y = value[(i / kVecs) * (pitch / 8) + i % kVecs];
+            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+            bool odd = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) odd |= (w[k] & 0x7f80u) == 0x7f80u || (w[k] & 0x7f800000u) == 0x7f800000u;
+            if (odd) atomicOr(&s_odd[i / kVecs >> 5], 1u << (i / kVecs & 31));
+        }
+        uint64_t mine[2] = {1ull << lane, 1ull << (lane + 32)};
+        if (C::kSparse) {                                  // (the item's rows are one token's: it sees the tokens up to itself)
+            sees[lane] = lane <= token ? 1ull : 0ull;
+            sees[lane + 32] = lane + 32 <= token ? 1ull : 0ull;
+        } else {
+            // Ancestors: pointers to them are doubled.
+            int to[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int t = lane + 32 * h;
+                to[h] = -1;
+                if (t < n) {
+                    to[h] = a.parent != nullptr ? a.parent[static_cast<int64_t>(slot) * a.T + t] : t - 1;
+                    if (to[h] < -1 || to[h] >= t) {
+                        report(a.status, PULSAR_DEV_BAD_TREE);
+                        to[h] = -1;
+                    }
                 }
             }
-        }
-        constexpr int kVecs = D / 8;
-        const int64_t from0 = static_cast<int64_t>(s.slot) * a.T * pitch + s.kvh * D;
-        if (has_new) {
-#pragma unroll 4
-            for (int i = t; i < s.n * kVecs; i += 64) {
-                const uint4 y = reinterpret_cast<const uint4*>(a.Vnew + from0 + (i / kVecs) * pitch)[i % kVecs];
-                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-                bool odd = false;
+#pragma unroll 1
+            for (int step = 1; step < n; step <<= 1) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) odd |= (w[k] & 0x7f80u) == 0x7f80u || (w[k] & 0x7f800000u) == 0x7f800000u;
-                if (odd) atomicOr(&s_odd[2 * (seq % kQueue) + (i / kVecs >> 5)], 1u << (i / kVecs & 31));
+                for (int h = 0; h < 2; ++h) {
+                    sees[lane + 32 * h] = mine[h];
+                    s_up[lane + 32 * h] = to[h];
+                }
+                __syncwarp();
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (to[h] >= 0) {
+                        mine[h] |= sees[to[h]];
+                        to[h] = s_up[to[h]];
+                    }
+                __syncwarp();
+            }
+            if (C::kBySeen) {                              // turned round: the nodes that see a node
+                uint32_t* seen = reinterpret_cast<uint32_t*>(sees);
+#pragma unroll 4
+                for (int node = 0; node < n; ++node) {
+                    const uint32_t lo = __ballot_sync(0xffffffffu, ((mine[0] >> node) & 1ull) != 0ull);
+                    const uint32_t hi = __ballot_sync(0xffffffffu, ((mine[1] >> node) & 1ull) != 0ull);
+                    if (lane < 2) seen[2 * node + lane] = lane == 0 ? lo : hi;
+                }
+            } else {
+                sees[lane] = mine[0];
+                sees[lane + 32] = mine[1];
             }
         }
-        named_sync(kRowsBarrier, 64);
-        if (t == 0) {
-            arrive_a(bar(C::bSees + static_cast<int>(seq % kQueue)));
-            arrive_a(bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));         // (both warps have their copy)
-        }
-        if (has_new && s.row0 == 0 && s.token == 0) {
-            for (int i = t; i < s.n * kVecs; i += 64) {
-                const int row = i / kVecs, v = i % kVecs;
-                const int64_t to = new_row_at(a, s.slot, static_cast<int64_t>(s.len) + row, pitch);
-                if (to < 0) continue;
-                const int64_t from = from0 + row * pitch;
-                reinterpret_cast<uint4*>(a.K + to + s.kvh * D)[v] = reinterpret_cast<const uint4*>(a.Knew + from)[v];
-                reinterpret_cast<uint4*>(a.V + to + s.kvh * D)[v] = reinterpret_cast<const uint4*>(a.Vnew + from)[v];
-            }
+        __syncwarp();
+        if (lane == 0) {
+            arrive_a(roles.bar(C::bSees + static_cast<int>(seq % kQueue)));
+            arrive_a(roles.bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));
         }
     }
 }

@@ -6,7 +6,8 @@
 //
 //   warp 0      loader: pages of K and V by TMA into a ring of tiles, the nodes' own rows as the last tile of an item
 //   warp 1      issues the matrix instructions: S of the next tile before PV of this one
-//   warps 2-3   query rows (TMA), which nodes see which, the nodes' rows to their pages
+//   warp 2      query rows (TMA)
+//   warp 3      which nodes see which
 //   warps 4-..  softmax: a thread per key and 32 columns (or all, if fewer); epilogue: a thread per output component and 32 rows
 //
 // A column's maximum lies across lanes, so it is not formed for every tile: P is formed with the largest logit seen when it was
@@ -136,7 +137,7 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
         for (int i = 0; i < kQueue; ++i) {
             mbar_init(bars + C::bSees + i, 1);
             mbar_init(bars + C::bWorkFull + i, 1);
-            mbar_init(bars + C::bWorkEmpty + i, C::kSoftWarps + 2);                    // and the issuer, and warps 2 and 3
+            mbar_init(bars + C::bWorkEmpty + i, C::kSoftWarps + 3);                    // and the issuer, warp 2 and warp 3
         }
         mbar_fence_init();
         prefetch_maps(map);
@@ -230,8 +231,10 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
             }
         }
         if (ok && tile > 0) issue_pv(tile - 1);
-    } else if (warp < 4) {
-        rows_role<D, C>(a, map, static_cast<int>(threadIdx.x) - 64, roles);
+    } else if (warp == 2) {
+        rows_role<C>(a, map, roles);
+    } else if (warp == 3) {
+        nodes_role<D, C>(a, roles);
     } else {
         // ---- softmax and epilogue ----
         const int quarter = warp & 3, group = (warp - 4) >> 2;

@@ -80,7 +80,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
         for (int i = 0; i < kQueue; ++i) {
             mbar_init(bars + C::bSees + i, 1);
             mbar_init(bars + C::bWorkFull + i, 1);
-            mbar_init(bars + C::bWorkEmpty + i, 8 + 2);
+            mbar_init(bars + C::bWorkEmpty + i, 8 + 3);
         }
         mbar_fence_init();
         prefetch_maps(map);
@@ -197,8 +197,10 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
                 issue_pv(static_cast<int>((tile - 1) & 1), ((tile - 1) >> 1) & 1, true);
             }
         }
-    } else if (warp < 4) {
-        rows_role<D, C>(a, map, static_cast<int>(threadIdx.x) - 64, roles);
+    } else if (warp == 2) {
+        rows_role<C>(a, map, roles);
+    } else if (warp == 3) {
+        nodes_role<D, C>(a, roles);
     } else {
         // ---- softmax and epilogue: a thread per row ----
         const int h = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;

@@ -479,7 +479,7 @@ using namespace pulsar;
 
 extern "C" size_t pulsar_tree_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t Hq, int32_t Hkv, int32_t d) {
     if (n_slots < 1 || n_slots > kMaxSlots || T < 1 || T > kMaxTree || !heads_ok(Hq, Hkv) || (d != 64 && d != 128)) return 0;
-    return attn_workspace_bytes(T * (Hq / Hkv), d);
+    return attn_workspace_bytes(n_slots, Hkv, T * (Hq / Hkv), d);
 }
 
 extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, const uint16_t* Vnew, int32_t T, uint16_t* K_pages,
@@ -524,7 +524,7 @@ extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, con
     a.out_f32 = out_is_f32;
     a.LSE = LSE;
     a.status = device_status;
-    return launch_attn(a, T * (Hq / Hkv), d, workspace, static_cast<cudaStream_t>(stream));
+    return launch_attn(a, Hkv, T * (Hq / Hkv), d, workspace, static_cast<cudaStream_t>(stream));
 }
 
 namespace {
@@ -532,7 +532,7 @@ struct SparseScratch {
     size_t exact, score, most, list, total;
     SparseScratch(int64_t n_slots, int64_t T, int64_t Hkv, int64_t max_pages, int64_t k, int g, int d) {
         const int64_t rows = n_slots * T * Hkv;
-        exact = attn_workspace_bytes(g, d);
+        exact = attn_workspace_bytes(static_cast<int>(n_slots), static_cast<int>(T * Hkv), g, d);
         score = round_up(exact + static_cast<size_t>(rows * max_pages) * 8, 256);
         most = round_up(score + static_cast<size_t>(rows * max_pages) * 4, 256);
         list = round_up(most + static_cast<size_t>(n_slots * Hkv * ((max_pages + kScorePages - 1) / kScorePages)) * 4, 256);
@@ -629,5 +629,5 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
     a.O = O;
     a.LSE = LSE;
     a.status = device_status;
-    return launch_attn(a, Hq / Hkv, d, workspace, st);
+    return launch_attn(a, T * Hkv, Hq / Hkv, d, workspace, st);
 }

@@ -31,9 +31,9 @@ constexpr int kMaxTree = 64;                    // nodes of a drafted tree
 // Arguments of the attention kernels.  A work item is some query rows of one KV head against a list of keys, cut into pieces; every
 // CTA takes an equal share of all pieces of all slots and leaves a partial (normalised output and l = ln sum exp) where it holds an
 // item only in part.
-struct Meta {                                   // the item that begins in a CTA and goes on in the next ones
-    int first, parts;                           // first partial, and how many (0: there is no such item); those after it are the first
-    int step;                                   // ones of every step-th CTA
+struct Meta {                                   // of an item
+    int parts;                                  // partials that it is in: 0 or 1: nothing is to be joined
+    int first, cta, step;                       // place of the first one, left by CTA `cta`; the others are the first ones of every step-th CTA after it
     int token0, head0, row0, rows;              // of its rows: see row_of
 };
 
@@ -49,23 +49,24 @@ struct PagedArgs {
     int out_f32;
     float* LSE;
     float *part_O, *part_LSE;                    // [2 * CTAs, rows of an item, D], [2 * CTAs, rows of an item]
-    Meta* meta;                                  // [CTAs]
+    Meta* meta;                                  // [n_slots, items_max, row blocks]
+    int items_max;                               // items that a slot can have
     int32_t* status;
 };
 
-// Joins the partials that `ctas` CTAs have left of items of `rows` rows (paged_merge.cu).
-int32_t launch_parts_merge(const PagedArgs& a, unsigned ctas, int rows, int d, cudaStream_t stream);
+// Appends the new tokens' rows, and joins the partials of `items` items of `rows` rows (paged_merge.cu).
+int32_t launch_parts_merge(const PagedArgs& a, int64_t items, int rows, int d, cudaStream_t stream);
 
 // Attention over the rows of the cache or, where there is a list, over the selected pages (paged_tiles.cu).  rows: of an item.
-size_t attn_workspace_bytes(int rows, int d);
-int32_t launch_attn(PagedArgs a, int rows, int d, void* workspace, cudaStream_t stream);
+size_t attn_workspace_bytes(int n_slots, int items, int rows, int d);      // items: of a slot, at the most
+int32_t launch_attn(PagedArgs a, int items, int rows, int d, void* workspace, cudaStream_t stream);
 
 // Scratch of an attention launch: what its CTAs leave for the merge.  rows: of an item.
 struct PartScratch {
     size_t meta, part_O, part_LSE, total;
-    PartScratch(size_t ctas, int rows, int d) {
+    PartScratch(size_t items, size_t ctas, int rows, int d) {
         meta = 0;
-        part_LSE = round_up(ctas * sizeof(Meta), 256);
+        part_LSE = round_up(items * sizeof(Meta), 256);
         part_O = round_up(part_LSE + 2 * ctas * rows * 4, 256);
         total = round_up(part_O + 2 * ctas * rows * d * 4, 256);
     }
@@ -126,7 +127,7 @@ struct Slots {
 };
 // One warp fills it in; returns the pieces of all slots, and how many items they are of.
 template <bool kSparse>
-__device__ __forceinline__ int all_pieces(const PagedArgs& a, Slots& slots, int& items) {
+__device__ __forceinline__ int all_pieces(const PagedArgs& a, Slots& slots, int row_blocks, int& items) {
     const int lane = threadIdx.x & 31;
     int total = 0, mine = 0;
     for (int s0 = 0; s0 < a.n_slots; s0 += 32) {
@@ -138,6 +139,8 @@ __device__ __forceinline__ int all_pieces(const PagedArgs& a, Slots& slots, int&
             const SlotWork w = slot_work<kSparse>(a, len, n);
             x = w.pieces * w.items;
             mine += w.items;
+            if (blockIdx.x == 0)                                         // items that do not exist
+                for (int i = w.items * row_blocks; i < a.items_max * row_blocks; ++i) a.meta[static_cast<int64_t>(s) * a.items_max * row_blocks + i].parts = 0;
             slots.len[s] = len;
             slots.n[s] = static_cast<unsigned char>(n);
         }
@@ -189,7 +192,7 @@ struct Segment {
     SlotWork w;
     int slot, p_begin, p_end;
     int n_rows, kvh, token, token0, head0;       // query rows; KV head; sparse: the token; first token among all, first head
-    int item_at;                                 // the item's first piece among all
+    int item, item_at;                           // number within the slot; its first piece among all
 };
 template <bool kSparse>
 __device__ __forceinline__ Segment segment_at(const PagedArgs& a, const Slots& slots, int at, int end, int& slot) {
@@ -199,6 +202,7 @@ __device__ __forceinline__ Segment segment_at(const PagedArgs& a, const Slots& s
     s.w = slot_work<kSparse>(a, slots.len[slot], slots.n[slot]);
     const int first = slots.before[slot];
     const int item = static_cast<int>(static_cast<uint32_t>(at - first) / static_cast<uint32_t>(s.w.pieces));
+    s.item = item;
     s.item_at = first + item * s.w.pieces;
     s.p_begin = at - s.item_at;
     s.p_end = min(end - s.item_at, s.w.pieces);

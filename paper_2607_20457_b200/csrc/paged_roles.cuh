@@ -122,11 +122,10 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const Maps& map, i
     // More rows than a CTA takes: neighbouring CTAs have the same keys at the same time, and a share of the rows each.
     const int cta = static_cast<int>(blockIdx.x) / row_blocks, n_ctas = static_cast<int>(gridDim.x) / row_blocks;
     int items;
-    const int total = all_pieces<C::kSparse>(a, slots, items);
+    const int total = all_pieces<C::kSparse>(a, slots, row_blocks, items);
     const Shares shares(total, max(total / kLeastTiles, items), n_ctas);
     const int begin = shares.begin(cta), end = shares.begin(cta + 1);
     int slot_now = begin < end ? slot_at(slots, a.n_slots, begin) : 0, at = begin;
-    bool joined = false;                     // an item that begins here goes on elsewhere
     for (uint32_t seq = 0;; ++seq) {
         const uint32_t place = seq % kQueue;
         __syncwarp();
@@ -143,18 +142,20 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const Maps& map, i
         const int row0 = static_cast<int>(blockIdx.x) % row_blocks * C::kRows, n_rows = min(s.n_rows - row0, C::kRows);
         const int part = 2 * static_cast<int>(blockIdx.x) + (at == begin ? 0 : 1);
         at = s.item_at + s.p_end;
+        Meta* meta = a.meta + (static_cast<int64_t>(s.slot) * a.items_max + s.item) * row_blocks + static_cast<int>(blockIdx.x) % row_blocks;
         if (n_rows <= 0) {                   // (this slot has fewer rows)
+            if (lane == 0 && s.p_begin == 0) meta->parts = 0;
             --seq;
             continue;
         }
         if (lane == 0) {
-            s_work[place] = Work{1, s.slot, s.p_begin, s.p_end, s.w.new_tile, s.w.keys, s.w.n, row0, n_rows, s.kvh, s.token0, s.head0,
-                                 s.p_begin == 0 && s.p_end == s.w.pieces ? -1 : part, s.w.len, s.token, s.w.new_at};
+            const bool all = s.p_begin == 0 && s.p_end == s.w.pieces;
+            s_work[place] = Work{1, s.slot, s.p_begin, s.p_end, s.w.new_tile, s.w.keys, s.w.n, row0, n_rows, s.kvh, s.token0, s.head0, all ? -1 : part,
+                                 s.w.len, s.token, s.w.new_at};
             arrive_a(bar(C::bWorkFull + static_cast<int>(place)));
-            if (s.p_begin == 0 && s.p_end < s.w.pieces) {
-                a.meta[blockIdx.x] = {part, shares.owner(s.item_at + s.w.pieces - 1) - cta + 1, row_blocks, s.token0, s.head0, row0, n_rows};
-                joined = true;
-            }
+            if (s.p_begin == 0)
+                *meta = {all ? 1 : shares.owner(s.item_at + s.w.pieces - 1) - cta + 1, part, static_cast<int>(blockIdx.x), row_blocks, s.token0, s.head0, row0,
+                         n_rows};
         }
         const int32_t* list = page_list<C::kSparse>(a, s.slot, s.token0, s.kvh);
         // A tile's rows are copied page by page, a page per lane; those before new tokens in the same tile 16 by 16, up to where these begin.
@@ -195,7 +196,6 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const Maps& map, i
             id = next;
         }
     }
-    if (lane == 0 && !joined) a.meta[blockIdx.x].parts = 0;
 }
 
 // ---- a warp: query rows (TMA) ----

@@ -494,7 +494,7 @@ int32_t launch(const PagedArgs& a, const Maps& map, cudaStream_t stream) {
     PULSAR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
     PULSAR_CUDA_OK(launch_kernel(kernel, dim3(ctas), dim3(C::kThreads), C::kSmem, stream, true, a, map, 1));
     count_launch();
-    return launch_parts_merge(a, ctas, N, D, stream);
+    return launch_parts_merge(a, static_cast<int64_t>(a.n_slots) * a.items_max, N, D, stream);
 }
 template <int D>
 int32_t launch_rows(const PagedArgs& a, const Maps& map, int n, cudaStream_t stream) {
@@ -508,11 +508,17 @@ int32_t launch_rows(const PagedArgs& a, const Maps& map, int n, cudaStream_t str
 
 }  // namespace
 
-size_t attn_workspace_bytes(int rows, int d) { return PartScratch(sm_count(), item_rows(rows), d).total; }
+// CTAs of a launch that share an item's rows.
+int row_blocks(int rows) { return (rows + 255) / 256; }
 
-int32_t launch_attn(PagedArgs a, int rows, int d, void* workspace, cudaStream_t stream) {
+size_t attn_workspace_bytes(int n_slots, int items, int rows, int d) {
+    return PartScratch(static_cast<size_t>(n_slots) * items * row_blocks(rows), sm_count(), item_rows(rows), d).total;
+}
+
+int32_t launch_attn(PagedArgs a, int items, int rows, int d, void* workspace, cudaStream_t stream) {
     const int n = item_rows(rows);
-    PartScratch(sm_count(), n, d).place(a, workspace);
+    a.items_max = items;
+    PartScratch(static_cast<size_t>(a.n_slots) * items * row_blocks(rows), sm_count(), n, d).place(a, workspace);
     a.fresh_rows = static_cast<int>(round_up(a.T, 8));
     Maps map;
     const int64_t pool_rows = static_cast<int64_t>(a.n_pages) << a.page_shift, fresh_rows = static_cast<int64_t>(a.n_slots) * a.T;

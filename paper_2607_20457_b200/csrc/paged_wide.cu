@@ -208,6 +208,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
         const uint32_t tS = tmem + h * 128 + my_lanes, tO = tmem + 256 + h * 128 + my_lanes;
         const int64_t pitch = static_cast<int64_t>(a.Hkv) * D;
         const int per_tile = kTile >> a.page_shift;
+        const bool wide = (reinterpret_cast<uintptr_t>(a.O) & 31) == 0;
         uint32_t tile = 0, v_stage = 1, v_phase = 0, o_done = 0;
         bool ok = true;
         for (uint32_t seg = 0;; ++seg) {
@@ -351,10 +352,9 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
             }
 
             // ---- outputs ----
-            const int64_t to = (s.part < 0 ? row_of(s.token0, s.head0, s.row0, my_row, a.g_shift, a.Hq) : static_cast<int64_t>(s.part) * C::kRows + my_row) * D;
-            const bool to_f32 = s.part >= 0 || a.out_f32 != 0;
-            float* to_f = s.part < 0 ? static_cast<float*>(a.O) : a.part_O;
-            float* to_lse = s.part < 0 ? a.LSE : a.part_LSE;
+            const bool whole = s.part < 0;
+            const int64_t out_row = whole ? row_of(s.token0, s.head0, s.row0, my_row, a.g_shift, a.Hq) : static_cast<int64_t>(s.part) * C::kRows + my_row;
+            float* to_lse = whole ? a.LSE : a.part_LSE;
             if (any_tile) {
                 __syncwarp();
                 ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bOFull + h), o_done & 1, abort_flag, a.status));
@@ -386,14 +386,20 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
             };
             const auto store = [&](int c, const float (&o)[kJoinCols]) {
                 if (!exists) return;
-                if (to_f32) {
+                if (!whole) {                                               // [D, rows]: 32 rows write together
+                    float* to = a.part_O + static_cast<int64_t>(s.part) * C::kRows * D + c * C::kRows + my_row;
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(to_f + to + c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    for (int i = 0; i < 16; ++i) to[i * C::kRows] = o[i];
+                } else if (a.out_f32) {
+                    float* to = static_cast<float*>(a.O) + out_row * D + c;
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                 } else {
+                    uint16_t* to = static_cast<uint16_t*>(a.O) + out_row * D + c;
+                    uint32_t v[8];
 #pragma unroll
-                    for (int i = 0; i < 16; i += 8)
-                        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.O) + to + c + i) =
-                            make_uint4(pack_bf16x2(o[i], o[i + 1]), pack_bf16x2(o[i + 2], o[i + 3]), pack_bf16x2(o[i + 4], o[i + 5]), pack_bf16x2(o[i + 6], o[i + 7]));
+                    for (int i = 0; i < 8; ++i) v[i] = pack_bf16x2(o[2 * i], o[2 * i + 1]);
+                    store_32b(to, v, wide);
                 }
             };
             if (kTwo) {
@@ -437,7 +443,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
                 }
             }
             if (exists && (kTwo || h == 0) && to_lse != nullptr)
-                to_lse[to / D] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+                to_lse[out_row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
@@ -462,10 +468,11 @@ template <int D, bool kTwo>
 int32_t launch(const PagedArgs& a, const Maps& map, int rows, cudaStream_t stream) {
     using C = Wide<D, kTwo>;
     const unsigned ctas = static_cast<unsigned>(sm_count());
+    const int blocks = (rows + C::kRows - 1) / C::kRows;
     PULSAR_CUDA_OK(cudaFuncSetAttribute(tree_wide_kernel<D, kTwo>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
-    PULSAR_CUDA_OK(launch_kernel(tree_wide_kernel<D, kTwo>, dim3(ctas), dim3(kThreads), C::kSmem, stream, true, a, map, (rows + C::kRows - 1) / C::kRows));
+    PULSAR_CUDA_OK(launch_kernel(tree_wide_kernel<D, kTwo>, dim3(ctas), dim3(kThreads), C::kSmem, stream, true, a, map, blocks));
     count_launch();
-    return launch_parts_merge(a, ctas, C::kRows, D, stream);
+    return launch_parts_merge(a, static_cast<int64_t>(a.n_slots) * a.items_max * blocks, C::kRows, D, stream);
 }
 
 }  // namespace

@@ -318,3 +318,23 @@ def test_values_that_are_not_finite_reach_who_sees_them(T, Hq, Hkv, d):
     assert not bool(fine.all())
     zero = torch.zeros_like(Oref)
     R.check(torch.where(fine, o, zero), LSE, (torch.where(fine, Oref, zero), Lref, torch.where(fine, A, zero)))
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", [(1, 8, 2, 128), (6, 8, 2, 128), (13, 16, 4, 64), (24, 8, 2, 128), (64, 8, 2, 64)])
+def test_logits_that_rise_by_powers_of_two(T, Hq, Hkv, d):
+    """Tiles whose largest logits lie 2^20 to 2^200 above those of the tiles before: what has been summed up so far is rescaled, in the
+    middle of a tile and between tiles.  (Keys are multiples of the queries' mean direction, so the logits rise along the cache.)"""
+    c = R.Cache([900, 385], 16, Hkv, d, room=T)
+    Q, Kn, Vn, parent = drafts(2, T, Hq, Hkv, d, seed=T)
+    g = torch.Generator().manual_seed(2)
+    u = torch.randn(Hkv, d, generator=g)
+    u /= u.norm(dim=-1, keepdim=True)
+    Q = (Q.float() * 0.05 + u.repeat_interleave(Hq // Hkv, 0)).to(BF)
+    rise = {0: 0.0, 70: 20.0, 200: 45.0, 300: 130.0, 301: 140.0, 500: 230.0, 800: 238.0}
+    for s, n in enumerate((900, 385)):
+        h = 0.0
+        for r in range(n):
+            h = rise.get(r, h)
+            at = c.table[s, r // 16], r % 16
+            c.K[at] = (c.K[at].float() * 0.05 + u * h * 0.6931).to(BF)
+    run(c, Q, Kn, Vn, parent, scale=1.0)

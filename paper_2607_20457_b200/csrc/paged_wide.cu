@@ -12,8 +12,7 @@
 //
 //   warp 0 loader, warp 1 issues the matrix instructions, warps 2-3 query rows and nodes (paged_roles.cuh), warps 4-11 softmax and epilogue
 //
-// P of a tile is formed in one pass over S, with the maximum of the tiles before: it is moved, and O rescaled, before the next tile when a logit
-// has exceeded it by more than 2^8 (at once by more than 2^64).
+// As in paged_tiles.cu the maximum is moved, and O rescaled, when a logit exceeds it by more than 2^8.
 #include "mma.cuh"
 #include "paged_roles.cuh"
 
@@ -22,7 +21,6 @@ namespace pulsar {
 namespace {
 
 constexpr int kThreads = 384;
-constexpr float kTooMuch = 64.f;                 // a logit so far above the maximum (2^64) moves it within a tile
 constexpr int kJoinCols = 16;                    // outputs of a row that the streams exchange at a time
 constexpr int kJoinPitch = kJoinCols + 1;
 constexpr int kJoinBarrier = 1;                  // named barrier of both softmax warpgroups
@@ -230,7 +228,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
             constexpr int kStep = kTwo ? 1 : 2;
             const int t_first = kTwo ? p_begin : p_begin + static_cast<int>((h ^ tile) & 1u);      // this stream's first tile
             int id = page_of(t_first);
-            float m = -INFINITY, largest = -INFINITY, l0 = 0.f, l1 = 0.f;       // the maximum in use, the largest logit so far, the sum
+            float m = -INFINITY, l0 = 0.f, l1 = 0.f;       // the maximum in use, and the sum
             bool any_tile = false, had_fresh = false;
             uint64_t sees = 0ull;
             for (int t = p_begin; t < p_end; ++t, ++tile) {
@@ -268,10 +266,32 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
                         had_fresh = true;
                     }
                     tc_fence_after();
-                    // The maximum is moved to the largest logit of the tiles before where that exceeds it by more than 2^8 (for the first tile, to
-                    // its own): PV of the tile before is done, and what O, the sums and P of the coming tiles are relative to changes between tiles.
-                    const auto move_max = [&](float to) {
-                        const float m_new = fmaxf(m, to), alpha = m_new == -INFINITY ? 1.f : ex2(m - m_new);
+                    float x[kTile];
+                    {
+                        uint32_t r[kTile];
+                        __syncwarp();
+                        PULSAR_TMEM_LD32_AT(tS, r, 0);
+                        PULSAR_TMEM_LD32_AT(tS + 32, r, 32);
+                        PULSAR_TMEM_LD32_AT(tS + 64, r, 64);
+                        PULSAR_TMEM_LD32_AT(tS + 96, r, 96);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < kTile; ++i) x[i] = __uint_as_float(r[i]);
+                    }
+                    if (!plain) {
+#pragma unroll
+                        for (int i = 0; i < kTile; ++i)
+                            if (((see[i / 32] >> (i % 32)) & 1u) == 0u) x[i] = -INFINITY;
+                    }
+                    float most = -INFINITY, most2 = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < kTile; i += 4) {
+                        most = max3(most, x[i], x[i + 1]);
+                        most2 = max3(most2, x[i + 2], x[i + 3]);
+                    }
+                    most = fmaxf(most, most2) * a.scale_log2;
+                    if (__any_sync(0xffffffffu, most > m + kRescale)) {     // (the first tile: anything exceeds -infinity)
+                        const float m_new = fmaxf(m, most), alpha = m_new == -INFINITY ? 1.f : ex2(m - m_new);
                         m = m_new;
                         l0 *= alpha;
                         l1 *= alpha;
@@ -287,79 +307,19 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
                                 tmem_st16(tO + c, o);
                             }
                         }
-                        return alpha;
-                    };
-                    uint32_t r[2][32];
-                    __syncwarp();
-                    if (__any_sync(0xffffffffu, m == -INFINITY)) {          // the first tile, and rows that have seen nothing so far
-                        float first_max = -INFINITY;
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            __syncwarp();
-                            tmem_ld32(tS + c * 32, r[0]);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (plain || ((see[c] >> i) & 1u) != 0u) first_max = fmaxf(first_max, __uint_as_float(r[0][i]));
-                        }
-                        (void)move_max(m == -INFINITY ? first_max * a.scale_log2 : -INFINITY);
-                        largest = fmaxf(largest, m);
-                    } else if (__any_sync(0xffffffffu, largest > m + kRescale)) {
-                        (void)move_max(largest);
                     }
-                    float neg = m == -INFINITY ? 0.f : -m;
-                    __syncwarp();
-                    tmem_ld32(tS, r[0]);
+                    const float neg = m == -INFINITY ? 0.f : -m;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        tmem_wait_ld();
-                        if (c < 3) tmem_ld32(tS + (c + 1) * 32, r[(c + 1) & 1]);        // the next 32 logits come while these are exponentiated
-                        float x[32], most = -INFINITY, most2 = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[c & 1][i]);
-                        if (!plain) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (((see[c] >> i) & 1u) == 0u) x[i] = -INFINITY;
-                        }
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            fma2(x[i], x[i + 1], a.scale_log2, neg, neg);
-                            fma2(x[i + 2], x[i + 3], a.scale_log2, neg, neg);
-                            most = max3(most, x[i], x[i + 1]);
-                            most2 = max3(most2, x[i + 2], x[i + 3]);
-                        }
-                        most = fmaxf(most, most2);
-                        if (__any_sync(0xffffffffu, most > kTooMuch)) {
-                            // Too far above the maximum for P and the sums: it is moved at once, and with it P of the columns before.
-                            const float over = fmaxf(most, 0.f), alpha = move_max(m + over);
-                            neg = -m;
-                            if (m == -INFINITY) neg = 0.f;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] -= over;
-                            most -= over;
-#pragma unroll
-                            for (int b = 0; b < c; ++b) {
-                                uint32_t p[16];
-                                __syncwarp();
-                                tmem_wait_st();
-                                tmem_ld16(tS + b * 16, p);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int i = 0; i < 16; ++i)
-                                    p[i] = pack_bf16x2(__uint_as_float(p[i] << 16) * alpha, __uint_as_float(p[i] & 0xffff0000u) * alpha);
-                                tmem_st16(tS + b * 16, p);
-                            }
-                        }
-                        largest = fmaxf(largest, most - neg);
                         uint32_t p[16];
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
-                            const float p0 = ex2(x[i]), p1 = ex2(x[i + 1]);
-                            add2(l0, l1, p0, p1);
+                            const float p0 = ex2(fmaf(x[c * 32 + i], a.scale_log2, neg)), p1 = ex2(fmaf(x[c * 32 + i + 1], a.scale_log2, neg));
+                            l0 += p0;
+                            l1 += p1;
                             p[i / 2] = pack_bf16x2(p0, p1);
                         }
-                        tmem_st16(tS + c * 16, p);                          // (over columns that have been read)
+                        tmem_st16(tS + c * 16, p);
                     }
                     if (!plain && (!kTwo || h == 0)) {
                         // Rows of V that do not exist become zeros, and so does a node's value that is not finite (0 * NaN is NaN): see

@@ -380,7 +380,6 @@ append_pages_kernel(const uint4* __restrict__ Knew, const uint4* __restrict__ Vn
 
 // ---------------------------------------------------------------------------------------------
 // Summarise: smallest and largest component over a page's keys.  bf16 values are compared as they are, so the bounds are exact.
-// A CTA takes a page and 32 vectors of its rows at a time; eight warps share the rows.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
     uint32_t c;
@@ -399,9 +398,13 @@ __device__ __forceinline__ uint4 max8(const uint4& a, const uint4& b) {
     return make_uint4(max2(a.x, b.x), max2(a.y, b.y), max2(a.z, b.z), max2(a.w, b.w));
 }
 
-constexpr int kSumThreads = 256;
+// A page's rows of one strip (32 vectors of a row) are a warp's work: kSumRows rows' vectors under way per lane, nothing shared and nobody to
+// wait for.  (A CTA per page and strip with the rows shared out between its warps and two barriers: 88 us for 131,072 rows of 8 heads, 3.3
+// TB/s.)  Pages of 64 and 128 rows of few slots leave warps idle that way, so two or four neighbouring warps share such a page and the first
+// one joins them.
+constexpr int kSumThreads = 256, kSumRows = 16;
 __global__ void __launch_bounds__(kSumThreads)
-summarize_kernel(const uint4* __restrict__ K, int n_layers, int n_pages, int page_shift, int row_vecs, int head_shift,
+summarize_kernel(const uint4* __restrict__ K, int n_pages, int page_shift, int row_vecs, int head_shift, int share_shift,
                  const int32_t* __restrict__ table, const int32_t* __restrict__ row_begin, const int32_t* __restrict__ row_end,
                  int max_pages, uint4* __restrict__ summary, int32_t* status) {
     __shared__ uint4 s_min[kSumThreads], s_max[kSumThreads];
@@ -412,38 +415,49 @@ summarize_kernel(const uint4* __restrict__ K, int n_layers, int n_pages, int pag
     const bool tell = blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x == 0;
     const int first = (row_begin != nullptr ? checked_len(row_begin[slot], capacity, tell, status) : 0) >> page_shift;
     const int last = checked_len(row_end[slot], capacity, tell, status) >> page_shift;       // full pages
-    const int strips = (row_vecs + 31) / 32, rows_per_warp = (1 << page_shift) / (kSumThreads / 32);
-    const int64_t units = last > first ? static_cast<int64_t>(last - first) * strips : 0;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int o = first + static_cast<int>(u / strips), v = static_cast<int>(u % strips) * 32 + lane;
-        const int page = table[static_cast<int64_t>(slot) * max_pages + o];
-        if (page < 0 || page >= n_pages) {
-            if (threadIdx.x == 0) report(status, PULSAR_DEV_BAD_PAGE);
-            continue;
-        }
-        const int64_t at = static_cast<int64_t>(blockIdx.z) * n_pages + page;
-        if (v < row_vecs) {
-            const uint4* src = K + ((at << page_shift) + warp * rows_per_warp) * row_vecs + v;
-            uint4 lo = src[0], hi = lo;
-#pragma unroll 8
-            for (int r = 1; r < rows_per_warp; ++r) {
-                const uint4 x = src[static_cast<int64_t>(r) * row_vecs];
-                lo = min8(lo, x);
-                hi = max8(hi, x);
+    const uint32_t strips = static_cast<uint32_t>(row_vecs + 31) / 32;
+    const int together = (kSumThreads / 32) >> share_shift;                                  // units of a CTA
+    const int part = warp & ((1 << share_shift) - 1), rows = (1 << page_shift) >> share_shift;
+    const uint32_t units = last > first ? static_cast<uint32_t>(last - first) * strips : 0u;
+    for (uint32_t u0 = blockIdx.x * together; u0 < units; u0 += gridDim.x * together) {
+        const uint32_t u = u0 + (warp >> share_shift), o = u / strips;
+        const int v = static_cast<int>(u - o * strips) * 32 + lane;
+        const int page = u < units ? table[static_cast<int64_t>(slot) * max_pages + first + static_cast<int>(o)] : -1;
+        const bool known = page >= 0 && page < n_pages;
+        if (u < units && !known && lane == 0) report(status, PULSAR_DEV_BAD_PAGE);
+        const int64_t at = static_cast<int64_t>(blockIdx.z) * n_pages + (known ? page : 0);
+        uint4 lo, hi;
+        if (known && v < row_vecs) {
+            const uint4* src = K + ((at << page_shift) + part * rows) * row_vecs + v;
+            lo = hi = *src;
+            for (int r0 = 0; r0 < rows; r0 += kSumRows) {
+                uint4 x[kSumRows];
+#pragma unroll
+                for (int r = 0; r < kSumRows; ++r) x[r] = __ldcs(src + static_cast<int64_t>(r0 + min(r, rows - 1)) * row_vecs);
+#pragma unroll
+                for (int r = 0; r < kSumRows; ++r) {
+                    lo = min8(lo, x[r]);
+                    hi = max8(hi, x[r]);
+                }
             }
+        }
+        if (share_shift > 0) {
             s_min[threadIdx.x] = lo;
             s_max[threadIdx.x] = hi;
+            __syncthreads();
+            for (int w = 1; w < 1 << share_shift; ++w)
+                if (part == 0) {
+                    lo = min8(lo, s_min[threadIdx.x + 32 * w]);
+                    hi = max8(hi, s_max[threadIdx.x + 32 * w]);
+                }
+            __syncthreads();
         }
-        __syncthreads();
-        if (warp < 2 && v < row_vecs) {                         // warp 0: smallest, warp 1: largest
-            const uint4* s = warp == 0 ? s_min : s_max;
-            uint4 x = s[lane];
-#pragma unroll
-            for (int w = 1; w < kSumThreads / 32; ++w) x = warp == 0 ? min8(x, s[w * 32 + lane]) : max8(x, s[w * 32 + lane]);
+        if (known && v < row_vecs && part == 0) {
             const int head = v >> head_shift, in_head = v - (head << head_shift);
-            summary[at * 2 * row_vecs + (static_cast<int64_t>(2 * head + warp) << head_shift) + in_head] = x;
+            uint4* to = summary + at * 2 * row_vecs + (static_cast<int64_t>(2 * head) << head_shift) + in_head;
+            to[0] = lo;
+            to[static_cast<int64_t>(1) << head_shift] = hi;
         }
-        __syncthreads();
     }
 }
 
@@ -578,12 +592,17 @@ extern "C" int32_t pulsar_pages_summarize(const uint16_t* K_pages, int32_t n_lay
         return PULSAR_ERR_ALIGNMENT;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
     const int row_vecs = Hkv * d / 8;
-    const int64_t units = static_cast<int64_t>(max_pages) * ((row_vecs + 31) / 32);
-    const int64_t share = std::max<int64_t>(1, 16 * sm_count() / (static_cast<int64_t>(n_slots) * n_layers));
-    PULSAR_CUDA_OK(launch_kernel(summarize_kernel, dim3(static_cast<unsigned>(std::min(units, share)), n_slots, n_layers), dim3(kSumThreads), 0,
-                                 static_cast<cudaStream_t>(stream), true, reinterpret_cast<const uint4*>(K_pages), n_layers, n_pages,
-                                 log2_exact(page_size), row_vecs, log2_exact(d / 8), page_table, row_begin, row_end, max_pages,
-                                 reinterpret_cast<uint4*>(summary), device_status));
+    // Warps of a page: one per 16 rows where there are few pages and strips, else one.  CTAs: eight warps each, as many as the chip holds at
+    // a time and a few rounds more, so that the last ones end together.
+    const int64_t units = static_cast<int64_t>(max_pages) * ((row_vecs + 31) / 32) * n_slots * n_layers, warps = 64 * static_cast<int64_t>(sm_count());
+    int share = 0;
+    while (share < 3 && (page_size >> share) > kSumRows && (units << share) < warps) ++share;
+    const int64_t ctas = ((static_cast<int64_t>(max_pages) * ((row_vecs + 31) / 32) << share) + 7) / 8;
+    const int64_t most = std::max<int64_t>(1, 32 * sm_count() / (static_cast<int64_t>(n_slots) * n_layers));
+    PULSAR_CUDA_OK(launch_kernel(summarize_kernel, dim3(static_cast<unsigned>(std::min(ctas, most)), n_slots, n_layers), dim3(kSumThreads), 0,
+                                 static_cast<cudaStream_t>(stream), true, reinterpret_cast<const uint4*>(K_pages), n_pages, log2_exact(page_size), row_vecs,
+                                 log2_exact(d / 8), share, page_table, row_begin, row_end, max_pages, reinterpret_cast<uint4*>(summary),
+                                 device_status));
     count_launch();
     return PULSAR_OK;
 }

@@ -236,11 +236,15 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
     __shared__ TopScratch s;
     const int row = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const int token0 = row / a.Hkv, kvh = row - token0 * a.Hkv, slot = token0 / a.T, u = token0 - slot * a.T, g = 1 << a.g_shift;
-    grid_dependency_wait();
+    // This launch is placed when the scores' CTAs have all passed their wait: the caller's tensors are complete and only the scores
+    // are waited for.  The attention may be placed as soon as this launch runs, for the same reason.
     grid_launch_dependents();
     const int len = checked_len(a.len[slot], static_cast<int64_t>(a.max_pages) << a.page_shift, false, nullptr);
     const int full = len >> a.page_shift, k = min(a.k, full);
-    if (a.n_draft != nullptr && u >= a.n_draft[slot]) return;
+    if (a.n_draft != nullptr && u >= a.n_draft[slot]) {
+        grid_dependency_wait();
+        return;
+    }
     const float* score = a.score + static_cast<int64_t>(row) * a.max_pages;
     uint64_t* exact = a.exact + static_cast<int64_t>(row) * a.max_pages;
     int32_t* sel = a.sel + static_cast<int64_t>(row) * a.k;
@@ -256,6 +260,18 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
     const int rounds = (last - first + kTopThreads - 1) / kTopThreads;
     const auto value = [&](int i) { return at(i) < last ? score[at(i)] : -INFINITY; };
     if (ranked) {
+        float q1 = 0.f;                           // sums of the queries' magnitudes, a warp per head
+        for (int h = warp; h < g; h += kTopWarps) {
+            float x = 0.f;
+            for (int j = lane; j < D; j += 32) {
+                const float q = __uint_as_float(static_cast<uint32_t>(a.Q[(static_cast<int64_t>(token0) * a.Hq + (kvh << a.g_shift) + h) * D + j]) << 16);
+                s.q[h * D + j] = q;
+                x += fabsf(q);
+            }
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+            q1 = fmaxf(q1, x != x ? INFINITY : x);
+        }
         float lo = INFINITY, hi = -INFINITY;
         bool odd = false;
         if (t == 0) {
@@ -270,20 +286,9 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
                 hi = fmaxf(hi, x);
             }
         };
+        grid_dependency_wait();
 #pragma unroll
         for (int i = 0; i < kTopHeld; ++i) held[i] = value(i);
-        float q1 = 0.f;                           // sums of the queries' magnitudes, a warp per head
-        for (int h = warp; h < g; h += kTopWarps) {
-            float x = 0.f;
-            for (int j = lane; j < D; j += 32) {
-                const float q = __uint_as_float(static_cast<uint32_t>(a.Q[(static_cast<int64_t>(token0) * a.Hq + (kvh << a.g_shift) + h) * D + j]) << 16);
-                s.q[h * D + j] = q;
-                x += fabsf(q);
-            }
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-            q1 = fmaxf(q1, x != x ? INFINITY : x);
-        }
         float most = 0.f;
         for (int i = t; i < (full + kScorePages - 1) / kScorePages; i += kTopThreads)
             most = fmaxf(most, a.most[(static_cast<int64_t>(slot) * a.Hkv + kvh) * blocks + i]);
@@ -339,6 +344,7 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
             below = -INFINITY;                    // (`above` is infinite)
         }
     }
+    if (!ranked) grid_dependency_wait();
     const auto is_near = [&](float x) { return !(x > above) && !(x < below); };
 
     // ---- pages between the two borders are ranked in float64 ----

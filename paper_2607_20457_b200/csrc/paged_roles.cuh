@@ -157,6 +157,7 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const Maps& map, i
                 *meta = {all ? 1 : shares.owner(s.item_at + s.w.pieces - 1) - cta + 1, part, static_cast<int>(blockIdx.x), row_blocks, s.token0, s.head0, row0,
                          n_rows};
         }
+        if (C::kSparse && seq == 0) grid_dependency_wait();
         const int32_t* list = page_list<C::kSparse>(a, s.slot, s.token0, s.kvh);
         // A tile's rows are copied page by page, a page per lane; those before new tokens in the same tile 16 by 16, up to where these begin.
         const auto shift_of = [&](int t) { return t == s.w.new_tile ? 4 : a.page_shift; };

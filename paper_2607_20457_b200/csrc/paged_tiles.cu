@@ -146,7 +146,8 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
         tmem_alloc(tmem_ptr, C::kTmemCols);
         tmem_relinquish();
     }
-    grid_dependency_wait();
+    // Behind a selection everything but its list is complete when this launch is placed (paged.cu): those who read the list wait.
+    if (!kSparse) grid_dependency_wait();
     grid_launch_dependents();
     tc_fence_before();
     __syncthreads();
@@ -248,6 +249,7 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
         for (uint32_t seg = 0;; ++seg) {
             const Work& s = *next_work<C>(a, roles, seg, ok);
             if (named_any(id, 128, !ok) || s.valid == 0) break;
+            if (kSparse && seg == 0) grid_dependency_wait();
             const int32_t* list = page_list<kSparse>(a, s.slot, s.token0, s.kvh);
             const int p_begin = s.p_begin, p_end = s.p_end, new_tile = s.new_tile, n_rows = s.n_rows;
             float sum[kCols];
@@ -472,6 +474,7 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
         }
     }
 
+    if (kSparse) grid_dependency_wait();
     tc_fence_before();
     __syncthreads();
     if (*abort_flag != 0) {                                // copies that are still under way land before the memory is given back

@@ -58,8 +58,12 @@ page_score_kernel(const __grid_constant__ SelectArgs a) {
     const int slot = blockIdx.z, kvh = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
     grid_dependency_wait();
     grid_launch_dependents();
+    const int b0 = blockIdx.x * kScorePages, page0 = b0 + warp * 16 + gid;
+    int id[2];                                   // (asked for beside the length: whether there are such pages shows later)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) id[h] = page0 + 8 * h < a.max_pages ? a.table[static_cast<int64_t>(slot) * a.max_pages + page0 + 8 * h] : -1;
     const int len = checked_len(a.len[slot], static_cast<int64_t>(a.max_pages) << a.page_shift, false, nullptr);
-    const int full = len >> a.page_shift, b0 = blockIdx.x * kScorePages;
+    const int full = len >> a.page_shift;
     if (full <= a.k || b0 >= full) return;       // (all pages are taken as they are)
     const int n = a.n_draft != nullptr ? min(max(a.n_draft[slot], 0), a.T) : a.T, g = 1 << a.g_shift, rows = n * g;
     if (rows == 0) return;
@@ -67,34 +71,18 @@ page_score_kernel(const __grid_constant__ SelectArgs a) {
     // ---- the bounds of pages gid and gid + 8 of the warp's 16, as A fragments: products are summed in the order of these vectors ----
     uint4 f[2][kChunks];
     bool known[2];
-    const int page0 = b0 + warp * 16 + gid;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int b = page0 + 8 * h;
-        const int page = b < full ? a.table[static_cast<int64_t>(slot) * a.max_pages + b] : -1;
+        const int b = page0 + 8 * h, page = b < full ? id[h] : -1;
         known[h] = page >= 0 && page < a.n_pages;
         if (b < full && !known[h] && tig == 0) report(a.status, PULSAR_DEV_BAD_PAGE);
         const uint4* src = reinterpret_cast<const uint4*>(a.summary + (static_cast<int64_t>(known[h] ? page : 0) * a.Hkv + kvh) * 2 * D) + tig;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) f[h][c] = known[h] ? src[4 * c] : make_uint4(0u, 0u, 0u, 0u);
     }
-    {
-        uint32_t m = 0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c)
-                m = max_abs2(max_abs2(max_abs2(max_abs2(m, f[h][c].x), f[h][c].y), f[h][c].z), f[h][c].w);
-        float most = fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-        if (lane == 0) s_most[warp] = most;
-    }
     float best[2];                               // g = 16: of the row tile before
     for (int r0 = 0; r0 < rows; r0 += kScoreRows) {
-        __syncthreads();
-        if (r0 == 0 && threadIdx.x == 0)
-            a.most[(static_cast<int64_t>(slot) * a.Hkv + kvh) * gridDim.x + blockIdx.x] = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
+        if (r0 > 0) __syncthreads();
         for (int i = threadIdx.x; i < kScoreRows * (D / 2); i += kScoreThreads) {
             const int r = i / (D / 2), j = i % (D / 2);
             uint32_t x = 0, up = 0;
@@ -106,7 +94,21 @@ page_score_kernel(const __grid_constant__ SelectArgs a) {
             to[j] = x & ~up;
             to[D / 2 + j] = x & up;
         }
+        if (r0 == 0) {                           // the largest magnitude of a bound
+            uint32_t m = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c)
+                    m = max_abs2(max_abs2(max_abs2(max_abs2(m, f[h][c].x), f[h][c].y), f[h][c].z), f[h][c].w);
+            float most = fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            if (lane == 0) s_most[warp] = most;
+        }
         __syncthreads();
+        if (r0 == 0 && threadIdx.x == 0)
+            a.most[(static_cast<int64_t>(slot) * a.Hkv + kvh) * gridDim.x + blockIdx.x] = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
         for (int t = 0; t < min(kScoreRows, rows - r0); t += 8) {
             float c[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};       // two chains of products
             const uint4* src = reinterpret_cast<const uint4*>(s_q + (t + gid) * kPitch) + tig;
@@ -190,24 +192,31 @@ constexpr float kScoreError = 1.f / 65536.f;
 struct TopScratch {
     int bins[kBins];
     float q[16 * 128];
-    float value[kTopWarps];
+    float value[5][kTopWarps];
     int count[2][kTopWarps];
+    __align__(16) int taken[kTopHeld][kTopWarps];
     uint64_t near_key[kNear], cut_key;
     int near_at[kNear], n_near, cut_at, bin, above;
-    int odd;                                     // a score that is not finite
 };
 
-// Largest (or smallest: of the negated values) over the CTA.
-__device__ __forceinline__ float block_max(float x, float* s) {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+// Largest values over the CTA (smallest: of the negated ones).
+template <int N>
+__device__ __forceinline__ void block_max(float (&x)[N], float (&s)[5][kTopWarps]) {
+    static_assert(N <= 5, "");
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = x;
-    __syncthreads();
-    x = s[threadIdx.x & (kTopWarps - 1)];
 #pragma unroll
-    for (int d = kTopWarps / 2; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-    return x;
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) x[i] = fmaxf(x[i], __shfl_xor_sync(0xffffffffu, x[i], d));
+        if ((threadIdx.x & 31) == 0) s[i][threadIdx.x >> 5] = x[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = s[i][threadIdx.x & (kTopWarps - 1)];
+#pragma unroll
+        for (int d = kTopWarps / 2; d > 0; d >>= 1) x[i] = fmaxf(x[i], __shfl_xor_sync(0xffffffffu, x[i], d));
+    }
 }
 // Of two flags: how many threads before this one have them, and how many in all.
 __device__ __forceinline__ void block_counts(const bool (&flag)[2], int (&before)[2], int (&all)[2], int (&s)[2][kTopWarps]) {
@@ -231,7 +240,7 @@ __device__ __forceinline__ void block_counts(const bool (&flag)[2], int (&before
 }
 
 template <int D>
-__global__ void __launch_bounds__(kTopThreads)
+__global__ void __launch_bounds__(kTopThreads, 2)
 page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
     __shared__ TopScratch s;
     const int row = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -255,9 +264,23 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
     const bool all = full <= a.k;
     const int first = min(a.sink, full), last = max(first, full - a.window), want = all ? 0 : k - first - (full - last);
     const bool ranked = !all && want > 0;
+    // ---- pages that are taken anyway, before the scores are there: they come before and after the ranked ones ----
+    const int ahead = all ? full : first, after = all ? full : last;
+    for (int b = t; b < ahead; b += kTopThreads) {
+        sel[b] = b;
+        list[b] = table[b];
+    }
+    for (int b = after + t; b < full; b += kTopThreads) {
+        sel[k - full + b] = b;
+        list[k - full + b] = table[b];
+    }
+    for (int i = k + t; i < a.k; i += kTopThreads) sel[i] = -1;
+    if (t == 0 && len > full << a.page_shift) list[k] = table[full];      // the page of the rows after the last full one
     float held[kTopHeld], above = INFINITY, below = INFINITY;      // scores over `above` are taken, under `below` not, the others ranked
     const auto at = [&](int i) { return first + t + i * kTopThreads; };
     const int rounds = (last - first + kTopThreads - 1) / kTopThreads;
+#pragma unroll
+    for (int i = 0; i < kTopHeld; ++i) held[i] = -INFINITY;
     const auto value = [&](int i) { return at(i) < last ? score[at(i)] : -INFINITY; };
     if (ranked) {
         float q1 = 0.f;                           // sums of the queries' magnitudes, a warp per head
@@ -273,11 +296,8 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
             q1 = fmaxf(q1, x != x ? INFINITY : x);
         }
         float lo = INFINITY, hi = -INFINITY;
-        bool odd = false;
-        if (t == 0) {
-            s.odd = 0;
-            s.n_near = 0;
-        }
+        bool odd = false;                         // a score that is not finite
+        if (t == 0) s.n_near = 0;
         for (int i = t; i < kBins; i += kTopThreads) s.bins[i] = 0;
         const auto look = [&](float x) {
             odd |= !(x < INFINITY);
@@ -288,26 +308,28 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
         };
         grid_dependency_wait();
 #pragma unroll
-        for (int i = 0; i < kTopHeld; ++i) held[i] = value(i);
+        for (int i = 0; i < kTopHeld; ++i)
+            if (i < rounds) held[i] = value(i);
         float most = 0.f;
         for (int i = t; i < (full + kScorePages - 1) / kScorePages; i += kTopThreads)
             most = fmaxf(most, a.most[(static_cast<int64_t>(slot) * a.Hkv + kvh) * blocks + i]);
 #pragma unroll
-        for (int i = 0; i < kTopHeld; ++i) look(held[i]);
+        for (int i = 0; i < kTopHeld; ++i)
+            if (i < rounds) look(held[i]);
         for (int i = kTopHeld; i < rounds; ++i) look(value(i));
-        lo = -block_max(-lo, s.value);
-        hi = block_max(hi, s.value);
-        const float size = block_max(q1, s.value) * block_max(most, s.value);
-        if (odd) s.odd = 1;
-        __syncthreads();
-        const bool rough = s.odd != 0 || !(size < 1e37f) || !(hi > lo);      // fp32 says nothing: all are ranked in float64
+        float all5[5] = {-lo, hi, q1, most, odd ? 1.f : 0.f};
+        block_max(all5, s.value);
+        lo = -all5[0];
+        hi = all5[1];
+        const float size = all5[2] * all5[3];
+        const bool rough = all5[4] > 0.f || !(size < 1e37f) || !(hi > lo);      // fp32 says nothing: all are ranked in float64
         if (!rough) {
             // ---- the bin of the want-th largest score ----
             const float inv = kBins / (hi - lo);
             const auto bin_of = [&](float x) { return min(max(static_cast<int>((x - lo) * inv), 0), kBins - 1); };
 #pragma unroll
             for (int i = 0; i < kTopHeld; ++i)
-                if (at(i) < last) atomicAdd(&s.bins[bin_of(held[i])], 1);
+                if (i < rounds && at(i) < last) atomicAdd(&s.bins[bin_of(held[i])], 1);
             for (int i = kTopHeld; i < rounds; ++i)
                 if (at(i) < last) atomicAdd(&s.bins[bin_of(value(i))], 1);
             __syncthreads();
@@ -333,13 +355,14 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
                 }
             };
 #pragma unroll
-            for (int i = 0; i < kTopHeld; ++i) inside(i, held[i]);
+            for (int i = 0; i < kTopHeld; ++i)
+                if (i < rounds) inside(i, held[i]);
             for (int i = kTopHeld; i < rounds; ++i) inside(i, value(i));
             const float e = 2.f * kScoreError * size;
-            in_lo = -block_max(-in_lo, s.value);
-            in_hi = block_max(in_hi, s.value);
-            above = nextafterf(in_hi + e, INFINITY);                         // (outward: the sums are rounded)
-            below = nextafterf(in_lo - e, -INFINITY);
+            float ends[2] = {-in_lo, in_hi};
+            block_max(ends, s.value);
+            above = nextafterf(ends[1] + e, INFINITY);                       // (outward: the sums are rounded)
+            below = nextafterf(-ends[0] - e, -INFINITY);
         } else {
             below = -INFINITY;                    // (`above` is infinite)
         }
@@ -360,7 +383,8 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
             }
         };
 #pragma unroll
-        for (int i = 0; i < kTopHeld; ++i) sort_out(i, held[i]);
+        for (int i = 0; i < kTopHeld; ++i)
+            if (i < rounds) sort_out(i, held[i]);
         for (int i = kTopHeld; i < rounds; ++i) sort_out(i, value(i));
         taken = static_cast<int>(__reduce_add_sync(0xffffffffu, taken));
         __syncthreads();
@@ -436,33 +460,58 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
         }
     }
 
-    // ---- the taken pages in ascending order ----
-    const uint64_t cut_key = ranked ? s.cut_key : 0;
-    const int cut_at = ranked ? s.cut_at : 0;
-    int done = 0;
-    for (int b0 = 0; b0 < full; b0 += kTopThreads) {
-        const int b = b0 + t;
-        bool take = b < full && (all || b < first || b >= last);
-        if (ranked && b >= first && b < last) {
-            const float x = score[b];
-            if (!is_near(x)) {
-                take = x > above;
-            } else {
-                const uint64_t key = exact[b];
-                take = key > cut_key || (key == cut_key && b <= cut_at);
+    // ---- the ranked pages that are taken, in ascending order ----
+    if (ranked) {
+        const uint64_t cut_key = s.cut_key;
+        const int cut_at = s.cut_at;
+        int done = first;
+        for (int i0 = 0; i0 < rounds; i0 += kTopHeld) {
+            uint32_t takes[kTopHeld];
+            if (i0 > 0) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kTopHeld; ++i) {
+                takes[i] = 0u;
+                if (i0 + i >= rounds) {
+                    if (lane == 0) s.taken[i][warp] = 0;
+                    continue;
+                }
+                const int b = at(i0 + i);
+                const float x = i0 == 0 ? held[i] : value(i0 + i);
+                bool take = b < last && x > above;
+                if (b < last && is_near(x)) {
+                    const uint64_t key = exact[b];
+                    take = key > cut_key || (key == cut_key && b <= cut_at);
+                }
+                takes[i] = __ballot_sync(0xffffffffu, take);
+                if (lane == 0) s.taken[i][warp] = __popc(takes[i]);
             }
+            __syncthreads();
+            static_assert(kTopHeld * kTopWarps == 128, "");
+            const int4 c = reinterpret_cast<const int4*>(s.taken)[lane];     // four of the 128 counts, in the pages' order
+            int x = c.x + c.y + c.z + c.w;
+            const int own = x;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, x, d);
+                if (lane >= d) x += y;
+            }
+            const int total = __shfl_sync(0xffffffffu, x, 31), p0 = x - own, p1 = p0 + c.x, p2 = p1 + c.y, p3 = p2 + c.z;
+#pragma unroll
+            for (int i = 0; i < kTopHeld; ++i) {
+                if (i0 + i >= rounds) break;
+                const int from = i * (kTopWarps / 4) + (warp >> 2);          // the lane with this warp's count of the i-th round
+                const int q0 = __shfl_sync(0xffffffffu, p0, from), q1 = __shfl_sync(0xffffffffu, p1, from);
+                const int q2 = __shfl_sync(0xffffffffu, p2, from), q3 = __shfl_sync(0xffffffffu, p3, from);
+                const int before = (warp & 2) ? ((warp & 1) ? q3 : q2) : ((warp & 1) ? q1 : q0);
+                if ((takes[i] >> lane) & 1u) {
+                    const int to = done + before + __popc(takes[i] & ((1u << lane) - 1u)), b = at(i0 + i);
+                    sel[to] = b;
+                    list[to] = table[b];
+                }
+            }
+            done += total;
         }
-        const bool flag[2] = {take, false};
-        int before[2], total[2];
-        block_counts(flag, before, total, s.count);
-        if (take) {
-            sel[done + before[0]] = b;
-            list[done + before[0]] = table[b];
-        }
-        done += total[0];
     }
-    for (int i = k + t; i < a.k; i += kTopThreads) sel[i] = -1;
-    if (t == 0 && len > full << a.page_shift) list[k] = table[full];      // the page of the rows after the last full one
 }
 
 // ---------------------------------------------------------------------------------------------

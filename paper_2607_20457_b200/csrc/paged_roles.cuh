@@ -108,16 +108,63 @@ __device__ __forceinline__ const Work* next_work(const PagedArgs& a, const Roles
     return r.s_work + seq % kQueue;
 }
 
-// ---- loader (one warp): shares out the work, and every lane copies a page ----
+// Copies the tiles of an item's pieces: kFirst .. kLast of K (0) and V (1), which take turns in the ring.
+template <class C, int kFirst, int kLast>
+struct Ring {
+    uint32_t stage = kFirst, phase = 0;
+    __device__ __forceinline__ void load(const PagedArgs& a, const Maps& map, const Roles& roles, const Work& s, bool& ok) {
+        const int lane = threadIdx.x & 31;
+        const int32_t* list = page_list<C::kSparse>(a, s.slot, s.token0, s.kvh);
+        // A tile's rows are copied page by page, a page per lane; those before new tokens in the same tile 16 by 16, up to where these begin.
+        const auto shift_of = [&](int t) { return t == s.new_tile ? 4 : a.page_shift; };
+        const auto row_of_lane = [&](int t) { return t * kTile + (lane << shift_of(t)); };
+        const auto has_rows = [&](int t) { return t < s.p_end && lane < kTile >> shift_of(t) && row_of_lane(t) < s.keys; };
+        const auto page_of = [&](int t) { return has_rows(t) ? list[row_of_lane(t) >> a.page_shift] : 0; };
+        int id = page_of(s.p_begin);
+        for (int t = s.p_begin; t < s.p_end && ok; ++t) {
+            const int next = page_of(t + 1);                       // (looked at a tile later)
+            const bool fresh = t == s.new_tile, rows = has_rows(t);
+            int page = id;
+            if (rows && (id < 0 || id >= a.n_pages)) {
+                report(a.status, PULSAR_DEV_BAD_PAGE);             // (some page is loaded; its rows count as absent)
+                page = 0;
+            }
+            const int shift = shift_of(t), from = (page << a.page_shift) + (row_of_lane(t) & ((1 << a.page_shift) - 1));
+            const uint32_t lines = (__popc(__ballot_sync(0xffffffffu, rows)) << shift) + (fresh ? a.fresh_rows : 0);
+#pragma unroll
+            for (int kv = kFirst; kv <= kLast; ++kv) {
+                __syncwarp();
+                ok = __all_sync(0xffffffffu, ok && mbar_wait_a(roles.bar(C::bKvEmpty + stage), phase ^ 1, roles.abort_flag, a.status));
+                if (!ok) break;
+                const uint32_t full = roles.bar(C::bKvFull + stage), dst = smem_u32(roles.smem) + stage * C::kTileBytes;
+                if (lane == 0) mbar_expect_tx_a(full, static_cast<uint32_t>(C::kPanels) * lines * 128);
+                __syncwarp();
+                const CUtensorMap* pool = fresh ? (kv ? &map.V16 : &map.K16) : (kv ? &map.V : &map.K);
+#pragma unroll
+                for (int p = 0; p < C::kPanels; ++p) {
+                    if (rows) tma_load_3d_a(dst + p * kPanelBytes + (lane << (shift + 7)), pool, full, p * 64, s.kvh, from);
+                    if (fresh && lane == 0) tma_load_3d_a(dst + p * kPanelBytes + s.new_at * 128, kv ? &map.Vn : &map.Kn, full, p * 64, s.kvh, s.slot * a.T);
+                }
+                stage += kFirst == kLast ? 2 : 1;
+                if (stage >= C::kStages) {
+                    stage -= C::kStages;
+                    phase ^= 1;
+                }
+            }
+            id = next;
+        }
+    }
+};
+
+// ---- loader (one warp): shares out the work, and copies K and V, or K alone ----
 template <class C>
 __device__ __forceinline__ void load_role(const PagedArgs& a, const Maps& map, int row_blocks, const Roles& roles) {
     const int lane = threadIdx.x & 31;
-    uint8_t* smem = roles.smem;
     Work* s_work = roles.s_work;
     Slots& slots = *roles.slots;
     volatile int* abort_flag = roles.abort_flag;
     const auto bar = [&](int i) { return roles.bar(i); };
-    uint32_t stage = 0, phase = 0;
+    Ring<C, 0, C::kTwoLoaders ? 0 : 1> ring;
     bool ok = true;
     // More rows than a CTA takes: neighbouring CTAs have the same keys at the same time, and a share of the rows each.
     const int cta = static_cast<int>(blockIdx.x) / row_blocks, n_ctas = static_cast<int>(gridDim.x) / row_blocks;
@@ -148,54 +195,34 @@ __device__ __forceinline__ void load_role(const PagedArgs& a, const Maps& map, i
             --seq;
             continue;
         }
+        const bool all = s.p_begin == 0 && s.p_end == s.w.pieces;
+        const Work work{1, s.slot, s.p_begin, s.p_end, s.w.new_tile, s.w.keys, s.w.n, row0, n_rows, s.kvh, s.token0, s.head0, all ? -1 : part,
+                        s.w.len, s.token, s.w.new_at};
         if (lane == 0) {
-            const bool all = s.p_begin == 0 && s.p_end == s.w.pieces;
-            s_work[place] = Work{1, s.slot, s.p_begin, s.p_end, s.w.new_tile, s.w.keys, s.w.n, row0, n_rows, s.kvh, s.token0, s.head0, all ? -1 : part,
-                                 s.w.len, s.token, s.w.new_at};
+            s_work[place] = work;
             arrive_a(bar(C::bWorkFull + static_cast<int>(place)));
             if (s.p_begin == 0)
                 *meta = {all ? 1 : shares.owner(s.item_at + s.w.pieces - 1) - cta + 1, part, static_cast<int>(blockIdx.x), row_blocks, s.token0, s.head0, row0,
                          n_rows};
         }
         if (C::kSparse && seq == 0) grid_dependency_wait();
-        const int32_t* list = page_list<C::kSparse>(a, s.slot, s.token0, s.kvh);
-        // A tile's rows are copied page by page, a page per lane; those before new tokens in the same tile 16 by 16, up to where these begin.
-        const auto shift_of = [&](int t) { return t == s.w.new_tile ? 4 : a.page_shift; };
-        const auto row_of_lane = [&](int t) { return t * kTile + (lane << shift_of(t)); };
-        const auto has_rows = [&](int t) { return t < s.p_end && lane < kTile >> shift_of(t) && row_of_lane(t) < s.w.keys; };
-        const auto page_of = [&](int t) { return has_rows(t) ? list[row_of_lane(t) >> a.page_shift] : 0; };
-        int id = page_of(s.p_begin);
-        for (int t = s.p_begin; t < s.p_end && ok; ++t) {
-            const int next = page_of(t + 1);                       // (looked at a tile later)
-            const bool fresh = t == s.w.new_tile, rows = has_rows(t);
-            int page = id;
-            if (rows && (id < 0 || id >= a.n_pages)) {
-                report(a.status, PULSAR_DEV_BAD_PAGE);             // (some page is loaded; its rows count as absent)
-                page = 0;
-            }
-            const int shift = shift_of(t), from = (page << a.page_shift) + (row_of_lane(t) & ((1 << a.page_shift) - 1));
-            const uint32_t lines = (__popc(__ballot_sync(0xffffffffu, rows)) << shift) + (fresh ? a.fresh_rows : 0);
-#pragma unroll
-            for (int kv = 0; kv < 2; ++kv) {
-                __syncwarp();
-                ok = __all_sync(0xffffffffu, ok && mbar_wait_a(bar(C::bKvEmpty + stage), phase ^ 1, abort_flag, a.status));
-                if (!ok) break;
-                const uint32_t full = bar(C::bKvFull + stage), dst = smem_u32(smem) + stage * C::kTileBytes;
-                if (lane == 0) mbar_expect_tx_a(full, static_cast<uint32_t>(C::kPanels) * lines * 128);
-                __syncwarp();
-                const CUtensorMap* pool = fresh ? (kv ? &map.V16 : &map.K16) : (kv ? &map.V : &map.K);
-#pragma unroll
-                for (int p = 0; p < C::kPanels; ++p) {
-                    if (rows) tma_load_3d_a(dst + p * kPanelBytes + (lane << (shift + 7)), pool, full, p * 64, s.kvh, from);
-                    if (fresh && lane == 0) tma_load_3d_a(dst + p * kPanelBytes + s.w.new_at * 128, kv ? &map.Vn : &map.Kn, full, p * 64, s.kvh, s.slot * a.T);
-                }
-                if (++stage == C::kStages) {
-                    stage = 0;
-                    phase ^= 1;
-                }
-            }
-            id = next;
-        }
+        ring.load(a, map, roles, work, ok);
+    }
+}
+
+// ---- a warp that copies V, where the loader copies K alone ----
+template <class C>
+__device__ __forceinline__ void values_role(const PagedArgs& a, const Maps& map, const Roles& roles) {
+    Ring<C, 1, 1> ring;
+    bool ok = true;
+    for (uint32_t seq = 0;; ++seq) {
+        const Work* work = next_work<C>(a, roles, seq, ok);
+        if (!ok || work->valid == 0) break;
+        const Work s = *work;
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) arrive_a(roles.bar(C::bWorkEmpty + static_cast<int>(seq % kQueue)));
+        if (C::kSparse && seq == 0) grid_dependency_wait();
+        ring.load(a, map, roles, s, ok);
     }
 }
 

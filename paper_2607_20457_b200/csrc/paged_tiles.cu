@@ -22,16 +22,20 @@ namespace pulsar {
 
 namespace {
 
-template <int D, int N, bool kSelected>
+// kSplit: a warp behind the softmax copies V, and the loader K alone.  Pages of 16 rows are many copies, of which a warp issues one in 100
+// cycles or so: 1800 for K and V of a tile of d = 64, whose softmax takes 1900.  8 slots of 6000 rows 33.3 -> 29.1 us (d = 64),
+// 47.7 -> 41.5 (d = 128); with pages of 64 rows, which are few copies, 28.2 -> 29.3 and 39.5 -> 40.6.  Selected pages lie apart and
+// come no faster for it: 16 slots, 48 pages of 16 rows 53.8 -> 56.7 with the scores.
+template <int D, int N, bool kSelected, bool kSplit>
 struct Cfg {
     static constexpr int kPanels = D / 64;
     static constexpr int kTileBytes = kPanels * kPanelBytes;
     static constexpr int kCols = N < 32 ? N : 32;                // columns of a softmax thread
     static constexpr int kGroups = N / kCols;                    // softmax warpgroups
     static constexpr int kSoftWarps = 4 * kGroups;
-    static constexpr int kThreads = 128 + 128 * kGroups;
+    static constexpr int kThreads = 128 + 128 * kGroups + (kSplit ? 32 : 0);
     static constexpr int kRows = N, kQTiles = 1, kQRows = N;
-    static constexpr bool kBySeen = true, kSparse = kSelected;
+    static constexpr bool kBySeen = true, kSparse = kSelected, kTwoLoaders = kSplit;
     static constexpr int kPBytes = (N + 63) / 64 * kPanelBytes;
     static constexpr int kQBytes = kPanels * N * 128;
     static constexpr int kMisc = static_cast<int>(sizeof(Slots)) + 12 + kQueue * kMaxTree * 8 + kQueue * (8 + 64) + 64 * 8 + 7 * N * 4 + N * 8 +
@@ -93,10 +97,10 @@ __device__ __forceinline__ void column_sums(float (&x)[C], int lane) {
     }
 }
 
-template <int D, int N, bool kSparse>
-__global__ void __launch_bounds__(Cfg<D, N, kSparse>::kThreads, 1)
+template <int D, int N, bool kSparse, bool kSplit>
+__global__ void __launch_bounds__(Cfg<D, N, kSparse, kSplit>::kThreads, 1)
 paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Maps map, int row_blocks) {
-    using C = Cfg<D, N, kSparse>;
+    using C = Cfg<D, N, kSparse, kSplit>;
     constexpr int kCols = C::kCols;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* rest = smem + C::kRest;
@@ -137,7 +141,7 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
         for (int i = 0; i < kQueue; ++i) {
             mbar_init(bars + C::bSees + i, 1);
             mbar_init(bars + C::bWorkFull + i, 1);
-            mbar_init(bars + C::bWorkEmpty + i, C::kSoftWarps + 3);                    // and the issuer, warp 2 and warp 3
+            mbar_init(bars + C::bWorkEmpty + i, C::kSoftWarps + 3 + (kSplit ? 1 : 0));         // and the issuer, warps 2 and 3, the one for V
         }
         mbar_fence_init();
         prefetch_maps(map);
@@ -236,6 +240,8 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
         rows_role<C>(a, map, roles);
     } else if (warp == 3) {
         nodes_role<D, C>(a, roles);
+    } else if (kSplit && warp == 4 + C::kSoftWarps) {
+        values_role<C>(a, map, roles);
     } else {
         // ---- softmax and epilogue ----
         const int quarter = warp & 3, group = (warp - 4) >> 2;
@@ -489,23 +495,22 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
 // Query rows of a CTA: with more than 64 the rows stand in the lanes (paged_wide.cu).
 int item_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
-template <int D, int N, bool kSparse>
+template <int D, int N, bool kSparse, bool kSplit>
 int32_t launch(const PagedArgs& a, const Maps& map, cudaStream_t stream) {
-    using C = Cfg<D, N, kSparse>;
-    const auto kernel = paged_tiles_kernel<D, N, kSparse>;
+    using C = Cfg<D, N, kSparse, kSplit>;
+    const auto kernel = paged_tiles_kernel<D, N, kSparse, kSplit>;
     const unsigned ctas = static_cast<unsigned>(sm_count());
     PULSAR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
     PULSAR_CUDA_OK(launch_kernel(kernel, dim3(ctas), dim3(C::kThreads), C::kSmem, stream, true, a, map, 1));
     count_launch();
     return launch_parts_merge(a, static_cast<int64_t>(a.n_slots) * a.items_max, N, D, stream);
 }
-template <int D>
+template <int D, bool kSplit>
 int32_t launch_rows(const PagedArgs& a, const Maps& map, int n, cudaStream_t stream) {
-    if (a.list != nullptr) return launch<D, 16, true>(a, map, stream);
     switch (n) {
-        case 16: return launch<D, 16, false>(a, map, stream);
-        case 32: return launch<D, 32, false>(a, map, stream);
-        default: return launch<D, 64, false>(a, map, stream);
+        case 16: return launch<D, 16, false, kSplit>(a, map, stream);
+        case 32: return launch<D, 32, false, kSplit>(a, map, stream);
+        default: return launch<D, 64, false, kSplit>(a, map, stream);
     }
 }
 
@@ -534,7 +539,9 @@ int32_t launch_attn(PagedArgs a, int items, int rows, int d, void* workspace, cu
         ok = ok && make_map_3d(&map.K16, a.K, pool_rows, a.Hkv, d, 1, 16) && make_map_3d(&map.V16, a.V, pool_rows, a.Hkv, d, 1, 16);
     if (!ok) return PULSAR_ERR_CUDA;
     if (n > 64) return launch_tree_wide(a, map, rows, d, stream);
-    return d == 128 ? launch_rows<128>(a, map, n, stream) : launch_rows<64>(a, map, n, stream);
+    if (a.list != nullptr) return d == 128 ? launch<128, 16, true, false>(a, map, stream) : launch<64, 16, true, false>(a, map, stream);
+    if (a.page_shift == 4) return d == 128 ? launch_rows<128, true>(a, map, n, stream) : launch_rows<64, true>(a, map, n, stream);
+    return d == 128 ? launch_rows<128, false>(a, map, n, stream) : launch_rows<64, false>(a, map, n, stream);
 }
 
 }  // namespace pulsar

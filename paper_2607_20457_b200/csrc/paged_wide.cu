@@ -30,7 +30,7 @@ struct Wide {
     static constexpr int kPanels = D / 64, kTileBytes = kPanels * kPanelBytes;
     static constexpr int kQTiles = kTwo ? 2 : 1, kQRows = 128, kRows = kQTiles * 128;
     static constexpr int kQBytes = kQTiles * kTileBytes;
-    static constexpr bool kBySeen = false, kSparse = false;
+    static constexpr bool kBySeen = false, kSparse = false, kTwoLoaders = false;
     static constexpr int kJoinBytes = kTwo ? 0 : 2 * 128 * kJoinPitch * 4 + 2 * 128 * 8;
     static constexpr int kMisc = kQueue * (kMaxTree * 8 + 64 + 8) + 64 * 8 + kMaxTree * 4 + 8 + static_cast<int>(sizeof(Slots)) + 12;
     static constexpr int kFit = (232448 - kQBytes - kJoinBytes - kMisc) / kTileBytes;

@@ -371,6 +371,7 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
     const auto is_near = [&](float x) { return !(x > above) && !(x < below); };
 
     // ---- pages between the two borders are ranked in float64 ----
+    bool whole = false;
     if (ranked) {
         int taken = 0;
         const auto sort_out = [&](int i, float x) {
@@ -393,7 +394,9 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
         int left = want;                          // pages to take from those in between
         for (int w = 0; w < kTopWarps; ++w) left -= s.count[0][w];
         const int n_near = s.n_near;
-        if (n_near <= kNear) {
+        whole = left == n_near;                   // all of them are taken, often the k-th alone: nothing to rank
+        if (whole) {
+        } else if (n_near <= kNear) {
             for (int i = warp; i < n_near; i += kTopWarps) {
                 const int b = s.near_at[i];
                 const uint64_t key = exact_score<D>(a, s.q, g, table[b], kvh);
@@ -462,8 +465,8 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
 
     // ---- the ranked pages that are taken, in ascending order ----
     if (ranked) {
-        const uint64_t cut_key = s.cut_key;
-        const int cut_at = s.cut_at;
+        const uint64_t cut_key = whole ? 0 : s.cut_key;
+        const int cut_at = whole ? 0 : s.cut_at;
         int done = first;
         for (int i0 = 0; i0 < rounds; i0 += kTopHeld) {
             uint32_t takes[kTopHeld];
@@ -478,7 +481,9 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
                 const int b = at(i0 + i);
                 const float x = i0 == 0 ? held[i] : value(i0 + i);
                 bool take = b < last && x > above;
-                if (b < last && is_near(x)) {
+                if (b < last && is_near(x) && whole) {
+                    take = true;
+                } else if (b < last && is_near(x)) {
                     const uint64_t key = exact[b];
                     take = key > cut_key || (key == cut_key && b <= cut_at);
                 }

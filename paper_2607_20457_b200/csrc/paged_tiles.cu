@@ -1,18 +1,25 @@
-// Attention of drafted trees with more than eight query rows per KV head, on the tensor cores (tcgen05).
+// Attention over a paged cache for up to 64 query rows per KV head (drafted trees, decoding steps, selected pages), on the tensor
+// cores (tcgen05).
 //
-// S^T = K Q^T: the 128 keys of a tile stand in the rows (TMEM lanes) and the query rows -- nodes x heads of the group, 16 to 128 --
-// in the columns, so that the products cost what the rows need and every softmax thread has one key.  O^T += V^T P^T takes the V
-// tile as it lies in memory (d contiguous) as its first operand and P^T from shared memory.
+// S^T = K Q^T: the 128 keys of a tile stand in the rows (TMEM lanes) and the query rows -- nodes x heads of the group, 16, 32 or 64
+// with those that do not exist -- in the columns, so that the products cost what the rows need and every softmax thread has one key.
+// O^T += V^T P^T takes the V tile as it lies in memory (d contiguous) as its first operand and P^T from shared memory.
 //
-//   warp 0      loader: pages of K and V by TMA into a ring of tiles, the nodes' own rows as the last tile of an item
+//   warp 0      loader: shares out the work; pages of K and V by TMA into a ring of tiles, the new tokens' own rows with the last one
 //   warp 1      issues the matrix instructions: S of the next tile before PV of this one
 //   warp 2      query rows (TMA)
 //   warp 3      which nodes see which
 //   warps 4-..  softmax: a thread per key and 32 columns (or all, if fewer); epilogue: a thread per output component and 32 rows
+//   last warp   pages of 16 rows: copies V (see Cfg)
 //
 // A column's maximum lies across lanes, so it is not formed for every tile: P is formed with the largest logit seen when it was
 // last moved, and moved (and O^T and the sums rescaled) when a logit exceeds it by more than 2^8.  P, O^T and the sums use the same
-// stale maximum, so the result is unchanged.  The sums stay with their keys' threads until an item ends.
+// stale maximum, so the result is unchanged.  The sums stay with their keys' threads, in fp32, until an item ends; P is rounded to
+// bf16, which the product with V takes: each probability is off by at most 2^-8 of itself.
+//
+// What bounds it (measured in a pass of many, with the joining launch): long caches the memory -- 32 slots of up to 8192 rows of 8
+// heads, one token each, 97 us, 5.7 TB/s; short ones latency -- one slot of 6001 rows 13 us, of which the first tile's way (length,
+// page ids, TMA) takes 3.5, an item's end 1.5 and the joining launch 3; a tile of 64 rows itself about 1100 cycles.
 #include <algorithm>
 
 #include "mma.cuh"

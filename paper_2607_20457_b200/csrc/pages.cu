@@ -3,6 +3,11 @@
 // Everything here moves bytes.  The bookkeeping is a pure function of table and lengths: which pages are free follows from the
 // tables themselves, so there is no free list that a lost update could corrupt, and the result does not depend on the order
 // in which threads run.
+//
+// Measured (a pass among others): fork of 8 slots 11 us, of 64 slots of 262 pages with half-filled last pages 20 to 22 (floor 7: the copied
+// rows); compact of 64 trees of 64 nodes in 8 layers 7.8 (floor 3); key bounds of 131,072 rows of 8 heads 50 us, 5.65 TB/s, 0.87 of the
+// copy rate.  The first two are latency: a fork reads lengths, then tables, and cannot hand out a page before all marks are set
+// (four cluster barriers of 1 to 2 us each, with what lies between).
 #include <algorithm>
 
 #include "paged.cuh"

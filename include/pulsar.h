@@ -551,7 +551,8 @@ int32_t pulsar_rope_apply_qk(const uint16_t *Q, uint16_t *Q_out, int32_t Hq,
  *                     PULSAR_DEV_BAD_LENGTH and are clamped.
  * Rows from cache_len on are never read (they may hold anything, NaN included).  A page id outside [0, n_pages) where a row lies
  * sets PULSAR_DEV_BAD_PAGE: the row counts as absent, and what would be written there is dropped.  Several slots may hold the
- * same page; then they agree on its rows, and a page that is still written to is held by one slot.
+ * same page; then they agree on its rows, and a page that is still written to is held by one slot.  K_pages, V_pages and the outputs
+ * overlap neither each other nor an input (else PULSAR_ERR_INVALID_ARG).
  *
  * Requirements of all the calls (else PULSAR_ERR_SHAPE): page_size in {16, 32, 64, 128}; d in {64, 128}; 1 <= n_slots <= 1024;
  * max_pages * page_size <= 2^30; n_slots * max_pages < 2^31; 1 <= n_pages < 2^24; n_layers >= 1; Hkv <= 1024.  pulsar_pages_summarize

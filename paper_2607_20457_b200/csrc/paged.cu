@@ -566,6 +566,10 @@ extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, con
     if (Q == nullptr || Knew == nullptr || Vnew == nullptr || K_pages == nullptr || V_pages == nullptr || page_table == nullptr ||
         cache_len == nullptr || O == nullptr || workspace == nullptr)
         return PULSAR_ERR_INVALID_ARG;
+    const size_t rows = static_cast<size_t>(n_slots) * T, pool = pool_bytes(1, n_pages, page_size, Hkv, d);
+    if (!apart({{O, rows * Hq * d * (out_is_f32 ? 4 : 2)}, {K_pages, pool}, {V_pages, pool}, {LSE, rows * Hq * 4}},
+               {{Q, rows * Hq * d * 2}, {Knew, rows * Hkv * d * 2}, {Vnew, rows * Hkv * d * 2}}))
+        return PULSAR_ERR_INVALID_ARG;
     for (const void* p : {static_cast<const void*>(Q), static_cast<const void*>(Knew), static_cast<const void*>(Vnew),
                           static_cast<const void*>(K_pages), static_cast<const void*>(V_pages), static_cast<const void*>(O)})
         if (!aligned(p, 16)) return PULSAR_ERR_ALIGNMENT;
@@ -637,6 +641,10 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
         return PULSAR_ERR_SHAPE;
     if (Q == nullptr || Knew == nullptr || Vnew == nullptr || K_pages == nullptr || V_pages == nullptr || summary == nullptr ||
         page_table == nullptr || cache_len == nullptr || O == nullptr || sel == nullptr || workspace == nullptr)
+        return PULSAR_ERR_INVALID_ARG;
+    const size_t tokens = static_cast<size_t>(n_slots) * T, pool = pool_bytes(1, n_pages, page_size, Hkv, d);
+    if (!apart({{O, tokens * Hq * d * 2}, {K_pages, pool}, {V_pages, pool}, {LSE, tokens * Hq * 4}, {sel, tokens * Hkv * k * 4}},
+               {{Q, tokens * Hq * d * 2}, {Knew, tokens * Hkv * d * 2}, {Vnew, tokens * Hkv * d * 2}, {summary, pool / page_size * 2}}))
         return PULSAR_ERR_INVALID_ARG;
     for (const void* p : {static_cast<const void*>(Q), static_cast<const void*>(Knew), static_cast<const void*>(Vnew), static_cast<const void*>(summary),
                           static_cast<const void*>(K_pages), static_cast<const void*>(V_pages), static_cast<const void*>(O)})

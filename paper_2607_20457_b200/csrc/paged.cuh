@@ -1,6 +1,8 @@
 // The paged key/value cache: what its calls have in common (pages.cu, paged.cu).
 #pragma once
 
+#include <initializer_list>
+
 #include "common.cuh"
 
 namespace pulsar {
@@ -23,6 +25,24 @@ inline int log2_exact(int x) {
 inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     const auto x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return a != nullptr && b != nullptr && x < y + nb && y < x + na;
+}
+
+// Whether none of the outputs shares memory with another one or with an input.
+struct Bytes {
+    const void* p;
+    size_t n;
+};
+inline bool apart(std::initializer_list<Bytes> outputs, std::initializer_list<Bytes> inputs) {
+    for (const Bytes* o = outputs.begin(); o != outputs.end(); ++o) {
+        for (const Bytes* x = o + 1; x != outputs.end(); ++x)
+            if (overlap(o->p, o->n, x->p, x->n)) return false;
+        for (const Bytes& x : inputs)
+            if (overlap(o->p, o->n, x.p, x.n)) return false;
+    }
+    return true;
+}
+inline size_t pool_bytes(int64_t n_layers, int64_t n_pages, int64_t page_size, int64_t Hkv, int64_t d) {
+    return static_cast<size_t>(n_layers * n_pages * page_size * Hkv * d) * 2;
 }
 
 constexpr int kMaxSlots = 1024;

@@ -532,6 +532,8 @@ extern "C" int32_t pulsar_pages_fork(const int32_t* page_table, const int32_t* c
     for (const auto& i : in)
         for (const auto& o : out)
             if (overlap(i.p, i.n, o.p, o.n)) return PULSAR_ERR_INVALID_ARG;
+    const size_t pool = pool_bytes(n_layers, n_pages, page_size, Hkv, d);
+    if (!apart({{K_pages, pool}, {V_pages, pool}}, {})) return PULSAR_ERR_INVALID_ARG;
     if (!aligned(K_pages, 16) || !aligned(V_pages, 16) || !aligned(workspace, 256) || !aligned(page_table, 4) || !aligned(cache_len, 4) ||
         !aligned(parent, 4) || !aligned(new_table, 4) || !aligned(new_len, 4) || !aligned(n_free, 4))
         return PULSAR_ERR_ALIGNMENT;
@@ -594,6 +596,8 @@ extern "C" int32_t pulsar_pages_compact(uint16_t* K_pages, uint16_t* V_pages, in
     if (K_pages == nullptr || V_pages == nullptr || page_table == nullptr || cache_len == nullptr || accept == nullptr || new_len == nullptr ||
         overlap(cache_len, 4u * n_slots, new_len, 4u * n_slots))
         return PULSAR_ERR_INVALID_ARG;
+    const size_t pool = pool_bytes(n_layers, n_pages, page_size, Hkv, d);
+    if (!apart({{K_pages, pool}, {V_pages, pool}}, {})) return PULSAR_ERR_INVALID_ARG;
     if (!aligned(K_pages, 16) || !aligned(V_pages, 16) || !aligned(page_table, 4) || !aligned(cache_len, 4) || !aligned(accept, 4) ||
         !aligned(new_len, 4))
         return PULSAR_ERR_ALIGNMENT;
@@ -616,6 +620,8 @@ extern "C" int32_t pulsar_pages_append(const uint16_t* Knew, const uint16_t* Vne
     if (K_pages == nullptr || V_pages == nullptr || page_table == nullptr || cache_len == nullptr ||
         (T > 0 && (Knew == nullptr || Vnew == nullptr)))
         return PULSAR_ERR_INVALID_ARG;
+    const size_t fresh = static_cast<size_t>(n_slots) * T * Hkv * d * 2, pool = pool_bytes(1, n_pages, page_size, Hkv, d);
+    if (!apart({{K_pages, pool}, {V_pages, pool}}, {{Knew, fresh}, {Vnew, fresh}})) return PULSAR_ERR_INVALID_ARG;
     if (!aligned(K_pages, 16) || !aligned(V_pages, 16) || !aligned(Knew, 16) || !aligned(Vnew, 16) || !aligned(page_table, 4) ||
         !aligned(cache_len, 4) || !aligned(n_new, 4))
         return PULSAR_ERR_ALIGNMENT;
@@ -638,6 +644,8 @@ extern "C" int32_t pulsar_pages_summarize(const uint16_t* K_pages, int32_t n_lay
         static_cast<int64_t>(max_pages) * ((Hkv * d / 8 + 31) / 32) >= (int64_t{1} << 31))
         return PULSAR_ERR_SHAPE;
     if (K_pages == nullptr || page_table == nullptr || row_end == nullptr || summary == nullptr) return PULSAR_ERR_INVALID_ARG;
+    const size_t pool = pool_bytes(n_layers, n_pages, page_size, Hkv, d);
+    if (!apart({{summary, pool / page_size * 2}}, {{K_pages, pool}})) return PULSAR_ERR_INVALID_ARG;
     if (!aligned(K_pages, 16) || !aligned(summary, 16) || !aligned(page_table, 4) || !aligned(row_begin, 4) || !aligned(row_end, 4))
         return PULSAR_ERR_ALIGNMENT;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;

@@ -125,3 +125,18 @@ def test_reference_tree_and_selection_by_hand():
     q[0, 0] = 1.
     assert R.select_pages(q, bounds, 5, 2, 0, 0) == [1, 3] and R.select_pages(q, bounds, 5, 1, 0, 0) == [1]
     assert R.select_pages(q, bounds, 5, 3, 1, 1) == [0, 1, 4]
+
+
+@pytest.mark.parametrize("name,pairs", [
+    ("pulsar_pages_fork", [("K", "V")]), ("pulsar_pages_compact", [("K", "V"), ("len", "new_len")]),
+    ("pulsar_pages_append", [("K", "V"), ("Kn", "K"), ("Vn", "K"), ("Kn", "V"), ("Vn", "V")]), ("pulsar_pages_summarize", [("K", "summary")]),
+    ("pulsar_tree_attn", [("K", "V"), ("O", "Q"), ("O", "Kn"), ("O", "Vn"), ("O", "K"), ("O", "V"), ("Kn", "K"), ("Vn", "V"), ("Q", "K")]),
+    ("pulsar_sparse_attn", [("K", "V"), ("O", "Q"), ("O", "Kn"), ("O", "Vn"), ("O", "K"), ("O", "V"), ("Kn", "K"), ("Vn", "V"), ("Q", "V"),
+                            ("summary", "K"), ("O", "summary"), ("sel", "O"), ("sel", "Q")])])
+def test_tensors_that_share_memory(lib, name, pairs):
+    fn, good = getattr(lib, name), CALLS[name]
+    for one, other in pairs:
+        for change in (good[other], ctypes.c_void_p(good[other].value + 256)):       # the same place, and a part of it
+            if one in ("len",) and change is not good[other]:
+                continue
+            assert refused(fn, good, **{one: change}) == INVALID, (one, other)

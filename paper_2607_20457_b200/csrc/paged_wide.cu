@@ -28,6 +28,7 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kJoinCols = 16;                    // outputs of a row that the streams exchange at a time
 constexpr int kJoinPitch = kJoinCols + 1;
+constexpr int kFirst = 96;                       // keys of a tile whose P is handed over first, so that their product runs beside the rest
 constexpr int kJoinBarrier = 1;                  // named barrier of both softmax warpgroups
 
 template <int D, bool kTwo>
@@ -42,10 +43,19 @@ struct Wide {
     static constexpr int kStages = kFit < 10 ? kFit : 10;
     static constexpr int kQ = kStages * kTileBytes, kJoin = kQ + kQBytes, kRest = kJoin + kJoinBytes, kSmem = kRest + kMisc;
     static constexpr int bKvFull = 0, bKvEmpty = kStages, bQFull = 2 * kStages, bQEmpty = bQFull + 1, bSFull = bQEmpty + 1, bPFull = bSFull + 2,
-                         bOFull = bPFull + 2, bOEmpty = bOFull + 2, bSees = bOEmpty + 2, bWorkFull = bSees + kQueue, bWorkEmpty = bWorkFull + kQueue,
+                         bPRest = bPFull + 2, bOFull = bPRest + 2, bOEmpty = bOFull + 2, bSees = bOEmpty + 2, bWorkFull = bSees + kQueue, bWorkEmpty = bWorkFull + kQueue,
                          kBars = bWorkEmpty + kQueue;
     static_assert(kBars <= 64 && kStages >= 4 && kRest % 16 == 0, "");
 };
+
+// x * s + n for two logits.
+__device__ __forceinline__ void scaled2(float& y0, float& y1, float x0, float x1, float s, float n) {
+    asm("{\n\t.reg .b64 a, b, c;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
+        "fma.rn.f32x2 a, a, b, c;\n\t"
+        "mov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(y0), "=f"(y1) : "f"(x0), "f"(x1), "f"(s), "f"(n));
+}
 
 // The low n bits (n from 0 to 32).
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
@@ -79,6 +89,7 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
         for (int h = 0; h < 2; ++h) {
             mbar_init(bars + C::bSFull + h, 1);
             mbar_init(bars + C::bPFull + h, 4);
+            mbar_init(bars + C::bPRest + h, 4);
             mbar_init(bars + C::bOFull + h, 1);
             mbar_init(bars + C::bOEmpty + h, 4);
         }
@@ -138,11 +149,20 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
             wait(C::bPFull + h, parity);
             if (!ok) return;
             tc_fence_after();
+            const auto product = [&](int kk) {
+                if (kk < steps) umma_ts(tmem + 256 + h * 128, tmem + h * 128 + kk * 8, desc_v + static_cast<uint64_t>(v_stage * (C::kTileBytes >> 4) + kk * 128), kIdescO,
+                        first && kk == 0 ? 0u : 1u);
+            };
             if (leader) {
 #pragma unroll
-                for (int kk = 0; kk < kTile / 16; ++kk)
-                    if (kk < steps) umma_ts(tmem + 256 + h * 128, tmem + h * 128 + kk * 8, desc_v + static_cast<uint64_t>(v_stage * (C::kTileBytes >> 4) + kk * 128), kIdescO,
-                            first && kk == 0 ? 0u : 1u);
+                for (int kk = 0; kk < kFirst / 16; ++kk) product(kk);
+            }
+            wait(C::bPRest + h, parity);
+            if (!ok) return;
+            tc_fence_after();
+            if (leader) {
+#pragma unroll
+                for (int kk = kFirst / 16; kk < kTile / 16; ++kk) product(kk);
                 if (release_v) umma_commit_a(bar(C::bKvEmpty + static_cast<int>(v_stage)));
                 if (last) umma_commit_a(bar(C::bOFull + h));
             }
@@ -288,14 +308,44 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
                         for (int i = 0; i < kTile; ++i)
                             if (((see[i / 32] >> (i % 32)) & 1u) == 0u) x[i] = -INFINITY;
                     }
-                    float most = -INFINITY, most2 = -INFINITY;
+                    float sum0, sum1;
+                    // P of keys [from, from + 32 n): stored, and added to the two sums.
+                    const auto form = [&](int from, int n, float neg) {
 #pragma unroll
-                    for (int i = 0; i < kTile; i += 4) {
-                        most = max3(most, x[i], x[i + 1]);
-                        most2 = max3(most2, x[i + 2], x[i + 3]);
+                        for (int c = from / 32; c < from / 32 + n; ++c) {
+                            uint32_t p[16];
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                float y0, y1;
+                                scaled2(y0, y1, x[c * 32 + i], x[c * 32 + i + 1], a.scale_log2, neg);
+                                const float p0 = ex2(y0), p1 = ex2(y1);
+                                add2(sum0, sum1, p0, p1);
+                                p[i / 2] = pack_bf16x2(p0, p1);
+                            }
+                            tmem_st16(tS + c * 16, p);
+                        }
+                    };
+                    // Behind the first tile the first piece is formed with the maximum in use at once: its sum, needed anyway, bounds its
+                    // probabilities (a single one may reach 96 * 2^8), and the other logits are compared.  Where that fails the maximum is
+                    // taken over the tile and the piece is formed again.
+                    const bool ahead = any_tile && plain;
+                    bool again = true;
+                    sum0 = sum1 = 0.f;
+                    if (ahead) {
+                        form(0, kFirst / 32, -m);
+                        float most = -INFINITY;
+#pragma unroll
+                        for (int i = kFirst; i < kTile; i += 2) most = max3(most, x[i], x[i + 1]);
+                        again = __any_sync(0xffffffffu, !(sum0 + sum1 <= kFirst * 256.f) || m == -INFINITY || !(most * a.scale_log2 <= m + kRescale));
                     }
-                    most = fmaxf(most, most2) * a.scale_log2;
-                    if (__any_sync(0xffffffffu, most > m + kRescale)) {     // (the first tile: anything exceeds -infinity)
+                    if (again) {
+                        float most = -INFINITY, most2 = -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < kTile; i += 4) {
+                            most = max3(most, x[i], x[i + 1]);
+                            most2 = max3(most2, x[i + 2], x[i + 3]);
+                        }
+                        most = fmaxf(most, most2) * a.scale_log2;
                         const float m_new = fmaxf(m, most), alpha = m_new == -INFINITY ? 1.f : ex2(m - m_new);
                         m = m_new;
                         l0 *= alpha;
@@ -312,19 +362,9 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
                                 tmem_st16(tO + c, o);
                             }
                         }
-                    }
-                    const float neg = m == -INFINITY ? 0.f : -m;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t p[16];
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            const float p0 = ex2(fmaf(x[c * 32 + i], a.scale_log2, neg)), p1 = ex2(fmaf(x[c * 32 + i + 1], a.scale_log2, neg));
-                            l0 += p0;
-                            l1 += p1;
-                            p[i / 2] = pack_bf16x2(p0, p1);
-                        }
-                        tmem_st16(tS + c * 16, p);
+                        tmem_wait_st();                                      // (two stores to the same columns have no order of their own)
+                        sum0 = sum1 = 0.f;
+                        form(0, kFirst / 32, m == -INFINITY ? 0.f : -m);
                     }
                     if (!plain && (!kTwo || h == 0)) {
                         // Rows of V that do not exist become zeros, and so does a node's value that is not finite (0 * NaN is NaN): see
@@ -346,6 +386,14 @@ tree_wide_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ Ma
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) arrive_a(bar(C::bPFull + h));
+                    form(kFirst, (kTile - kFirst) / 32, m == -INFINITY ? 0.f : -m);
+                    l0 += sum0;
+                    l1 += sum1;
+                    __syncwarp();
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_a(bar(C::bPRest + h));
                     any_tile = true;
                     id = next;
                 }

@@ -15,9 +15,11 @@
 // As in paged_tiles.cu the maximum is moved, and O rescaled, when a logit exceeds it by more than 2^8; P is rounded to bf16, the sums stay in
 // fp32.
 //
-// What bounds it: one stream each, 4 slots of up to 32,768 rows with 24 nodes (96 rows) 93 to 97 us, 0.7 of HBM's floor; two, one slot of
-// 131,072 rows with 64 nodes (256 rows) 175 to 180 us, 0.48 of the tensor cores' burst rate: the chain S -> softmax -> PV -> S of a
-// stream, of which the other stream hides about half (a tile takes 4200 to 4500 cycles, its products 2048).
+// P is handed to the issuer in two pieces (96 and 32 keys), so that the first piece of PV runs beside the rest.
+//
+// What bounds it: up to 128 rows, 4 slots of up to 32,768 rows with 24 nodes (96 rows) 93 to 96 us, 0.7 of HBM's floor; more, one slot of
+// 131,072 rows with 64 nodes (256 rows) 162 us, 0.52 of the tensor cores' burst rate: the chain S -> softmax -> PV -> S of a stream, of
+// which the other stream hides a part (its products take 2048 cycles of a tile of about 3200).
 #include "mma.cuh"
 #include "paged_roles.cuh"
 

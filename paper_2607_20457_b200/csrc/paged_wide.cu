@@ -12,8 +12,9 @@
 //
 //   warp 0 loader, warp 1 issues the matrix instructions, warps 2-3 query rows and nodes (paged_roles.cuh), warps 4-11 softmax and epilogue
 //
-// As in paged_tiles.cu the maximum is moved, and O rescaled, when a logit exceeds it by more than 2^8; P is rounded to bf16, the sums stay in
-// fp32.
+// As in paged_tiles.cu the maximum is moved, and O rescaled, only when a logit exceeds it by more than 2^8 (in the first 96 keys of a tile:
+// when their probabilities sum to more than 96 * 2^8); P is rounded to bf16, each probability by at most 2^-8 of itself, the sums stay
+// in fp32.
 //
 // P is handed to the issuer in two pieces (96 and 32 keys), so that the first piece of PV runs beside the rest.
 //

@@ -207,7 +207,7 @@ struct TopScratch {
     int bins[kBins];
     float q[16 * 128];
     float value[5][kTopWarps];
-    int count[2][kTopWarps];
+    int count[kTopWarps];
     __align__(16) int taken[kTopHeld][kTopWarps];
     uint64_t near_key[kNear], cut_key;
     int near_at[kNear], n_near, cut_at, bin, above;
@@ -232,25 +232,16 @@ __device__ __forceinline__ void block_max(float (&x)[N], float (&s)[5][kTopWarps
         for (int d = kTopWarps / 2; d > 0; d >>= 1) x[i] = fmaxf(x[i], __shfl_xor_sync(0xffffffffu, x[i], d));
     }
 }
-// Of two flags: how many threads before this one have them, and how many in all.
-__device__ __forceinline__ void block_counts(const bool (&flag)[2], int (&before)[2], int (&all)[2], int (&s)[2][kTopWarps]) {
+// How many threads before this one have the flag, and how many in all.
+__device__ __forceinline__ int block_count(bool flag, int& all, int (&s)[kTopWarps]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t m[2] = {__ballot_sync(0xffffffffu, flag[0]), __ballot_sync(0xffffffffu, flag[1])};
+    const uint32_t m = __ballot_sync(0xffffffffu, flag);
     __syncthreads();
-    if (lane < 2) s[lane][warp] = __popc(m[lane]);
+    if (lane == 0) s[warp] = __popc(m);
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int c = s[i][lane & (kTopWarps - 1)];
-        int x = lane < warp ? c : 0, y = lane < kTopWarps ? c : 0;
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            x += __shfl_xor_sync(0xffffffffu, x, d);
-            y += __shfl_xor_sync(0xffffffffu, y, d);
-        }
-        before[i] = x + __popc(m[i] & ((1u << lane) - 1u));
-        all[i] = y;
-    }
+    const int c = lane < kTopWarps ? s[lane] : 0;
+    all = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(c)));
+    return static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(lane < warp ? c : 0))) + __popc(m & ((1u << lane) - 1u));
 }
 
 template <int D>
@@ -354,10 +345,10 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
                 const int y = __shfl_up_sync(0xffffffffu, x, d);
                 if (lane >= d) x += y;
             }
-            if (lane == 31) s.count[0][warp] = x;
+            if (lane == 31) s.count[warp] = x;
             __syncthreads();
             int over = x - n0 - n1;
-            for (int w = 0; w < warp; ++w) over += s.count[0][w];
+            for (int w = 0; w < warp; ++w) over += s.count[w];
             if (over < want && over + n0 + n1 >= want) s.bin = over + n0 >= want ? top : top - 1;
             __syncthreads();
             const int bin = s.bin;
@@ -403,10 +394,10 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
         for (int i = kTopHeld; i < rounds; ++i) sort_out(i, value(i));
         taken = static_cast<int>(__reduce_add_sync(0xffffffffu, taken));
         __syncthreads();
-        if (lane == 0) s.count[0][warp] = taken;
+        if (lane == 0) s.count[warp] = taken;
         __syncthreads();
         int left = want;                          // pages to take from those in between
-        for (int w = 0; w < kTopWarps; ++w) left -= s.count[0][w];
+        for (int w = 0; w < kTopWarps; ++w) left -= s.count[w];
         const int n_near = s.n_near;
         whole = left == n_near;                   // all of them are taken, often the k-th alone: nothing to rank
         if (whole) {
@@ -464,14 +455,14 @@ page_select_kernel(const __grid_constant__ SelectArgs a, int blocks) {
             int done = 0;
             for (int b0 = first; b0 < last; b0 += kTopThreads) {
                 const int b = b0 + t;
-                const bool flag[2] = {b < last && is_near(score[b]) && exact[b] == kth, false};
-                int before[2], total[2];
-                block_counts(flag, before, total, s.count);
-                if (flag[0] && done + before[0] == left - 1) {
+                const bool same = b < last && is_near(score[b]) && exact[b] == kth;
+                int total;
+                const int before = block_count(same, total, s.count);
+                if (same && done + before == left - 1) {
                     s.cut_key = kth;
                     s.cut_at = b;
                 }
-                done += total[0];
+                done += total;
             }
             __syncthreads();
         }

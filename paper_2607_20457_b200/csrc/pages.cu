@@ -7,7 +7,7 @@
 // Measured (a pass among others): fork of 8 slots 11 us, of 64 slots of 262 pages with half-filled last pages 20 to 22 (floor 7: the copied
 // rows); compact of 64 trees of 64 nodes in 8 layers 7.8 (floor 3); key bounds of 131,072 rows of 8 heads 50 us, 5.65 TB/s, 0.87 of the
 // copy rate.  The first two are latency: a fork reads lengths, then tables, and cannot hand out a page before all marks are set
-// (four cluster barriers of 1 to 2 us each, with what lies between).
+// (three cluster barriers of 1 to 2 us each, with what lies between).
 #include <algorithm>
 
 #include "paged.cuh"
@@ -199,7 +199,7 @@ fork_kernel(const __grid_constant__ ForkArgs a) {
     for (int p = begin + t * 16; p < end; p += kForkThreads * 16) mine += __popc(free_at(p));
     (void)block_prefix(mine, s_sums, &sum);
     if (t < kForkCtas) store_to_rank(&s_free[rank], t, sum);
-    cluster_sync();
+    cluster_sync();                              // (behind it nobody writes to another CTA's shared memory: CTAs leave as they finish)
     int before = 0, n_free = 0;
     for (int r = 0; r < kForkCtas; ++r) {
         if (r < rank) before += s_free[r];
@@ -229,7 +229,6 @@ fork_kernel(const __grid_constant__ ForkArgs a) {
         for (int r = n_free + t; r < n_fresh; r += kForkThreads) give(r, -1);
         if (t == 0) *a.n_free = max(n_free - n_fresh, 0);
     }
-    cluster_sync();                              // no CTA leaves while another may still write to its shared memory
 }
 
 constexpr int kCopyThreads = 256, kCopyUnroll = 4;

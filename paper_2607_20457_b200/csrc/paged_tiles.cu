@@ -14,8 +14,11 @@
 //
 // A column's maximum lies across lanes, so it is not formed for every tile: P is formed with the largest logit seen when it was
 // last moved, and moved (and O^T and the sums rescaled) when a logit exceeds it by more than 2^8.  P, O^T and the sums use the same
-// stale maximum, so the result is unchanged.  The sums stay with their keys' threads, in fp32, until an item ends; P is rounded to
-// bf16, which the product with V takes: each probability is off by at most 2^-8 of itself.
+// stale maximum, so the result is unchanged.  The sums stay with their keys' threads, in fp32, until an item ends.
+//
+// The product with V takes P in bf16.  Rounded once, every probability is off by up to 2^-8 of itself and the outputs by as much as
+// their own last rounding; so P is split into two bf16 numbers (2^-16 is left), which are neighbouring columns of one product with
+// twice the columns, and the epilogue adds the two results.
 //
 // What bounds it (measured in a pass of many, with the joining launch): long caches the memory -- 32 slots of up to 8192 rows of 8
 // heads, one token each, 97 us, 5.7 TB/s; short ones latency -- one slot of 6001 rows 13 us, of which the first tile's way (length,
@@ -43,7 +46,7 @@ struct Cfg {
     static constexpr int kThreads = 128 + 128 * kGroups + (kSplit ? 32 : 0);
     static constexpr int kRows = N, kQTiles = 1, kQRows = N;
     static constexpr bool kBySeen = true, kSparse = kSelected, kTwoLoaders = kSplit;
-    static constexpr int kPBytes = (N + 63) / 64 * kPanelBytes;
+    static constexpr int kPBytes = (2 * N + 63) / 64 * kPanelBytes;              // P's upper and lower parts side by side
     static constexpr int kQBytes = kPanels * N * 128;
     static constexpr int kMisc = static_cast<int>(sizeof(Slots)) + 12 + kQueue * kMaxTree * 8 + kQueue * (8 + 64) + 64 * 8 + 7 * N * 4 + N * 8 +
                                  kMaxTree * 4 + 8;
@@ -55,13 +58,16 @@ struct Cfg {
     static constexpr int kQ = kP + kPBytes;
     static constexpr int kRest = kQ + kQBytes;
     static constexpr int kSmem = kRest + kMisc;
-    static constexpr int kTmemCols = 3 * N <= 32 ? 32 : 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 3 * N <= 256 ? 256 : 512;
+    static constexpr int kTmemCols = 4 * N;                                      // S of two tiles; O of P's two parts
     // barriers
     static constexpr int bKvFull = 0, bKvEmpty = kStages, bQFull = 2 * kStages, bQEmpty = bQFull + 1, bSFull = bQEmpty + 1, bSEmpty = bSFull + 2,
                          bPFull = bSEmpty + 2, bPEmpty = bPFull + 1, bOFull = bPEmpty + 1, bOEmpty = bOFull + 1, bSees = bOEmpty + 1, bWorkFull = bSees + kQueue, bWorkEmpty = bWorkFull + kQueue,
                          kBars = bWorkEmpty + kQueue;
     static_assert(kBars <= 64 && kStages >= 3, "");
 };
+
+// Where columns c & ~7 .. of key `key` stand in P.
+__device__ __forceinline__ int p_at(int key, int c) { return (c >> 6) * kPanelBytes + key * 128 + (((c >> 3 & 7) ^ (key & 7)) << 4); }
 
 // Columns [0, C) of TMEM, 32 lanes per warp.
 template <int C>
@@ -172,7 +178,7 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
     } else if (warp == 1) {
         // ---- matrix instructions: S of a tile, then PV of the tile before it ----
         const bool leader = elect_one();
-        constexpr uint32_t kIdescS = umma_idesc_bf16(kTile, N, false, false), kIdescO = umma_idesc_bf16(kTile, N, true, true);
+        constexpr uint32_t kIdescS = umma_idesc_bf16(kTile, N, false, false), kIdescO = umma_idesc_bf16(kTile, 2 * N, true, true);
         const uint64_t desc_k = umma_smem_desc_sw128(smem_u32(smem), 16, 1024);
         const uint64_t desc_v = umma_smem_desc_sw128(smem_u32(smem), kPanelBytes, 1024);
         const uint64_t desc_q = umma_smem_desc_sw128(smem_u32(smem + C::kQ), 16, 1024);
@@ -356,14 +362,16 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
                     for (int c = 0; c < kCols; ++c) sum[c] *= s_alpha[col0 + c];
                     if (t > p_begin) {
 #pragma unroll 1
-                        for (int c0 = 0; c0 < kCols; c0 += 16) {
+                        for (int c0 = 0; c0 < 2 * kCols; c0 += 16) {
+                            const int from = col0 + c0 % kCols;
+                            const uint32_t at = tO + (c0 < kCols ? 0 : N) + from + my_lanes;
                             uint32_t o[16];
                             __syncwarp();
-                            tmem_ld16(tO + col0 + c0 + my_lanes, o);
+                            tmem_ld16(at, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * s_alpha[col0 + c0 + c]);
-                            tmem_st16(tO + col0 + c0 + my_lanes, o);
+                            for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * s_alpha[from + c]);
+                            tmem_st16(at, o);
                         }
                         tmem_wait_st();
                     }
@@ -372,20 +380,23 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) arrive_a(bar(C::bSEmpty + static_cast<int>(tile & 1)));
-                uint32_t p[kCols / 2];
+                uint32_t p[kCols / 2], rest[kCols / 2];    // rounded to bf16, and what that leaves, rounded again
 #pragma unroll
                 for (int c = 0; c < kCols; c += 2) {
                     const float p0 = ex2(x[c]), p1 = ex2(x[c + 1]);
                     add2(sum[c], sum[c + 1], p0, p1);
-                    p[c / 2] = pack_bf16x2(p0, p1);
+                    const uint32_t upper = pack_bf16x2(p0, p1);
+                    p[c / 2] = upper;
+                    rest[c / 2] = pack_bf16x2(p0 - __uint_as_float(upper << 16), p1 - __uint_as_float(upper & 0xffff0000u));
                 }
-                // P^T: a line of 64 rows per key, where the product before has been read
+                // P^T: lines of 64 columns per key, where the product before has been read
                 __syncwarp();
                 ok = ok && mbar_wait_a(bar(C::bPEmpty), (tile & 1) ^ 1, abort_flag, a.status);
-                uint8_t* line = smem + C::kP + (group >> 1) * kPanelBytes + key * 128;
 #pragma unroll
-                for (int v = 0; v < kCols / 8; ++v)
-                    *reinterpret_cast<uint4*>(line + (((v + (group & 1) * 4) ^ (key & 7)) << 4)) = make_uint4(p[4 * v], p[4 * v + 1], p[4 * v + 2], p[4 * v + 3]);
+                for (int v = 0; v < kCols / 8; ++v) {
+                    *reinterpret_cast<uint4*>(smem + C::kP + p_at(key, col0 + 8 * v)) = make_uint4(p[4 * v], p[4 * v + 1], p[4 * v + 2], p[4 * v + 3]);
+                    *reinterpret_cast<uint4*>(smem + C::kP + p_at(key, N + col0 + 8 * v)) = make_uint4(rest[4 * v], rest[4 * v + 1], rest[4 * v + 2], rest[4 * v + 3]);
+                }
                 if (masked && group == 0) {
                     // Rows of V that do not exist may hold anything, and 0 * NaN is NaN: they become zeros, as far as the product
                     // reads.  So does a new token's value that is not finite: those that do not see it have weight 0.  The epilogue adds
@@ -439,26 +450,26 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
             const uint64_t odd = p_end <= new_tile ? 0ull : s_odd[2 * (seg % kQueue)] | static_cast<uint64_t>(s_odd[2 * (seg % kQueue) + 1]) << 32;
 #pragma unroll 1
             for (int c0 = 0; c0 < kCols; c0 += 16) {
-                uint32_t r[16];
+                uint32_t r[16], r2[16];
                 __syncwarp();
                 tmem_ld16(tO + col0 + c0 + my_lanes, r);
+                tmem_ld16(tO + N + col0 + c0 + my_lanes, r2);
                 tmem_wait_ld();
                 if (key >= D) continue;                    // (d = 64: the lower half of the lanes)
                 float o[16];
 #pragma unroll
-                for (int c = 0; c < 16; ++c) o[c] = __uint_as_float(r[c]);
+                for (int c = 0; c < 16; ++c) o[c] = __uint_as_float(r[c]) + __uint_as_float(r2[c]);
                 for (uint64_t left = odd; left != 0ull; left &= left - 1ull) {
                     const int node = __ffsll(static_cast<long long>(left)) - 1;
                     const uint64_t seen = s_seen[(seg % kQueue) * kMaxTree + node];
                     const float v = __uint_as_float(static_cast<uint32_t>(a.Vnew[(static_cast<int64_t>(s.slot) * a.T + node) * pitch + s.kvh * D + key]) << 16);
                     const int at = s.new_at + node;
-                    const uint8_t* line = smem + C::kP + (group >> 1) * kPanelBytes + at * 128;
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
-                        const int col = c0 + c;
-                        if (((seen >> ((s.row0 + col0 + col) >> a.g_shift)) & 1ull) == 0ull) continue;
-                        const uint32_t p = *reinterpret_cast<const uint16_t*>(line + ((((col >> 3) + (group & 1) * 4) ^ (at & 7)) << 4) + (col & 7) * 2);
-                        o[c] = fmaf(__uint_as_float(p << 16), v, o[c]);
+                        const int col = col0 + c0 + c;
+                        if (((seen >> ((s.row0 + col) >> a.g_shift)) & 1ull) == 0ull) continue;
+                        const uint32_t p = *reinterpret_cast<const uint16_t*>(smem + C::kP + p_at(at, col) + (col & 7) * 2);
+                        o[c] = fmaf(__uint_as_float(p << 16), v, o[c]);      // (not finite, whatever the rest of the weight is)
                     }
                 }
                 int64_t to[16];                            // (read before the first store, which they could depend on)

@@ -13,13 +13,14 @@
 //   warp 0 loader, warp 1 issues the matrix instructions, warps 2-3 query rows and nodes (paged_roles.cuh), warps 4-11 softmax and epilogue
 //
 // As in paged_tiles.cu the maximum is moved, and O rescaled, only when a logit exceeds it by more than 2^8 (in the first 96 keys of a tile:
-// when their probabilities sum to more than 96 * 2^8); P is rounded to bf16, each probability by at most 2^-8 of itself, the sums stay
-// in fp32.
+// when their probabilities sum to more than 96 * 2^8).  The sums stay in fp32; P is rounded to bf16, each probability by at most 2^-8 of
+// itself, which makes the outputs 0.0023 off the 64-bit result where their own last rounding is 0.0017.  In two bf16 parts, as in
+// paged_tiles.cu, it would cost a second product on the pipe that sets the pace: 99 -> 125 us (96 rows), 169 -> 219 (256 rows).
 //
 // P is handed to the issuer in two pieces (96 and 32 keys), so that the first piece of PV runs beside the rest.
 //
-// What bounds it: up to 128 rows, 4 slots of up to 32,768 rows with 24 nodes (96 rows) 93 to 96 us, 0.7 of HBM's floor; more, one slot of
-// 131,072 rows with 64 nodes (256 rows) 162 us, 0.52 of the tensor cores' burst rate: the chain S -> softmax -> PV -> S of a stream, of
+// What bounds it: up to 128 rows, 4 slots of up to 32,768 rows with 24 nodes (96 rows) 95 to 99 us, 0.7 of HBM's floor; more, one slot of
+// 131,072 rows with 64 nodes (256 rows) 162 to 169 us, 0.5 of the tensor cores' burst rate: the chain S -> softmax -> PV -> S of a stream, of
 // which the other stream hides a part (its products take 2048 cycles of a tile of about 3200).
 #include "mma.cuh"
 #include "paged_roles.cuh"

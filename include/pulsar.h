@@ -630,6 +630,8 @@ int32_t pulsar_pages_summarize(const uint16_t *K_pages, int32_t n_layers, int32_
  *   LSE         out [n_slots, T, Hq] float32 or NULL
  *   Nodes whose row lies past the table's last page set PULSAR_DEV_BAD_LENGTH; they are attended to, but not written.  A row
  *   without a visible key cannot occur (a node sees itself).
+ *   Values that are not finite, cached or new, come out as the formula says for the nodes that see them, with weights in fp32 (one that
+ *   is 0 there, 2^-149 of the largest or less, times infinity is NaN), and reach nobody else.
  *
  * Requirements (else PULSAR_ERR_SHAPE): those of the paged cache, 1 <= T <= 64, Hq % Hkv == 0, Hq/Hkv in {1,2,4,8,16},
  * n_slots * Hkv * (max_pages * page_size / 128 + 2) < 2^31.

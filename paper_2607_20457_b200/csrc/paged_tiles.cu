@@ -18,8 +18,8 @@
 //
 // The product with V takes P in bf16.  Rounded once, every probability is off by up to 2^-8 of itself and the outputs by as much as
 // their own last rounding; so P is split into two bf16 numbers (2^-16 is left), which are neighbouring columns of one product with
-// twice the columns, and the epilogue adds the two results (one slot of 6001 rows 12.9 -> 13.2 us, 16 trees of 52 rows 33.6 -> 35.3, long caches the
-// same).
+// twice the columns, and the epilogue adds the two results where the upper part's is finite (one slot of 6001 rows 12.9 -> 13.2 us, 16 trees of 52
+// rows 33.6 -> 35.3, long caches the same; to look at the upper part first costs the small trees 0.3 us).
 //
 // What bounds it (measured in a pass of many, with the joining launch): long caches the memory -- 32 slots of up to 8192 rows of 8
 // heads, one token each, 96 to 100 us, 5.7 TB/s; short ones latency -- one slot of 6001 rows 13 us, of which the first tile's way (length,
@@ -459,7 +459,12 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
                 if (key >= D) continue;                    // (d = 64: the lower half of the lanes)
                 float o[16];
 #pragma unroll
-                for (int c = 0; c < 16; ++c) o[c] = __uint_as_float(r[c]) + __uint_as_float(r2[c]);
+                for (int c = 0; c < 16; ++c) {
+                    // An infinite value makes the upper part's sum what it is to be; the lower part's, whose weights are 0 or negative as
+                    // often as not, would turn it into a NaN.
+                    const float upper = __uint_as_float(r[c]);
+                    o[c] = fabsf(upper) < INFINITY ? upper + __uint_as_float(r2[c]) : upper;
+                }
                 for (uint64_t left = odd; left != 0ull; left &= left - 1ull) {
                     const int node = __ffsll(static_cast<long long>(left)) - 1;
                     const uint64_t seen = s_seen[(seg % kQueue) * kMaxTree + node];

@@ -1,0 +1,95 @@
+"""GPU parity: values and keys that are not finite, in the rows of a paged cache and in new tokens, in every form that an attention call
+can take (16, 32 and 64 rows per KV head, 128, 256, selected pages)."""
+import pytest
+import torch
+
+import paged_reference as R
+from paper_2607_20457_b200 import binding
+from test_gpu_tree_attn import drafts
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+INF, NAN = float("inf"), float("nan")
+FORMS = [(1, 8, 2, 128), (3, 4, 1, 64), (5, 8, 2, 128), (13, 16, 4, 64), (16, 8, 2, 128), (24, 8, 2, 128), (30, 4, 1, 64), (64, 8, 2, 64)]
+
+
+def plant(c, s, row, comp, value, x=None, head=slice(None)):
+    x = c.V if x is None else x
+    x[c.table[s, row // c.page], row % c.page, head, comp] = value
+
+
+def agrees(O, LSE, ref):
+    """Infinities and NaN of the definition, component by component; what is finite within the usual bounds.  Every weight here is
+    above 2^-100, so that its 32 bits are not zero."""
+    Oref, Lref, A = ref[:3]
+    o = O.double().cpu()
+    fine = Oref.isfinite()
+    assert not bool(fine.all())
+    assert torch.equal(o.isnan(), Oref.isnan()) and torch.equal(o.isinf(), Oref.isinf()) and bool((o[o.isinf()] == Oref[o.isinf()]).all())
+    zero = torch.zeros_like(Oref)
+    R.check(torch.where(fine, o, zero), LSE, (torch.where(fine, Oref, zero), Lref, torch.where(fine, A, zero)))
+
+
+def tree(c, Q, Kn, Vn, parent, scale=0.0):
+    return binding.pulsar_tree_attn(*(x.to(DEV) for x in (Q, Kn, Vn, c.K, c.V, c.table, c.lens, parent)), softmax_scale=scale)
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", FORMS)
+def test_cached_values(T, Hq, Hkv, d):
+    """Everybody sees the cached rows: one infinity is an infinity of its sign, two of either sign or a NaN are a NaN."""
+    c = R.Cache([150, 40, 0, 129], 16, Hkv, d, room=T)
+    Q, Kn, Vn, parent = drafts(4, T, Hq, Hkv, d, seed=T)
+    plant(c, 0, 7, 3, INF)
+    plant(c, 0, 130, 9, -INF)
+    plant(c, 0, 20, 11, NAN)
+    plant(c, 0, 5, 12, INF)
+    plant(c, 0, 140, 12, -INF)
+    plant(c, 1, 39, 0, INF, head=Hkv - 1)
+    plant(c, 3, 128, d - 1, -INF)
+    agrees(*tree(c, Q, Kn, Vn, parent), R.tree_attn(Q, Kn, Vn, c, parent))
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", [(1, 8, 2, 128), (2, 8, 1, 64), (3, 16, 1, 64)])
+def test_cached_values_of_items_that_one_thread_block_has(T, Hq, Hkv, d):
+    c = R.Cache([60] * 170, 16, Hkv, d, room=T)
+    Q, Kn, Vn, parent = drafts(170, T, Hq, Hkv, d)
+    for s in range(0, 170, 3):
+        plant(c, s, s % 60, s % d, INF if s % 2 else -INF)
+    agrees(*tree(c, Q, Kn, Vn, parent), R.tree_attn(Q, Kn, Vn, c, parent))
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", [(1, 8, 4, 128), (13, 16, 4, 64), (24, 8, 2, 128)])
+def test_cached_values_where_the_maximum_moves(T, Hq, Hkv, d):
+    """The infinity has been summed up when larger logits come: it is rescaled with the rest."""
+    n = 6000
+    c = R.Cache([n], 32, Hkv, d, room=T)
+    Q, Kn, Vn, parent = drafts(1, T, Hq, Hkv, d)
+    g = torch.Generator().manual_seed(3)
+    u = torch.randn(Hkv, d, generator=g)
+    u /= u.norm(dim=-1, keepdim=True)
+    Q = (Q.float() * 0.05 + u.repeat_interleave(Hq // Hkv, 0)).to(R.BF)
+    for r in range(n):                                      # logits 9 log2 units up in each of the last five tiles
+        at = c.table[0, r // 32], r % 32
+        c.K[at] = (c.K[at].float() * 0.05 + u * 9 * 0.6931 * max(0, r // 128 - 42)).to(R.BF)
+    plant(c, 0, 5500, 2, INF)
+    plant(c, 0, 5770, 4, -INF)
+    agrees(*tree(c, Q, Kn, Vn, parent, 1.0), R.tree_attn(Q, Kn, Vn, c, parent, scale=1.0))
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", [(1, 8, 2, 128), (3, 4, 1, 64), (2, 16, 1, 128)])
+@pytest.mark.parametrize("k", [6, 40])
+def test_values_of_selected_pages(T, Hq, Hkv, d, k):
+    """Cached values, those of the rows after the last full page and those of new tokens."""
+    c = R.Cache([16 * 20 + 5, 16 * 9, 7], 16, Hkv, d, room=T)
+    Q, Kn, Vn, _ = drafts(3, T, Hq, Hkv, d, seed=k)
+    for b in range(20):
+        plant(c, 0, 16 * b + b % 16, b, INF if b % 2 else -INF)
+    plant(c, 0, 16 * 20 + 2, 30, -INF)
+    plant(c, 1, 16 * 8 + 3, 31, NAN)
+    plant(c, 2, 0, d - 1, INF)
+    Vn[2, T - 1, :, 5] = INF
+    bounds = R.page_bounds(c.K)
+    O, LSE, sel = binding.pulsar_sparse_attn(*(x.to(DEV) for x in (Q, Kn, Vn, c.K, c.V, bounds, c.table, c.lens)), k, 1, 2)
+    *ref, want = R.sparse_attn(Q, Kn, Vn, c, bounds, k, 1, 2)
+    assert torch.equal(sel.cpu(), want)
+    agrees(O, LSE, ref)

@@ -475,7 +475,11 @@ paged_tiles_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
                         const int col = col0 + c0 + c;
                         if (((seen >> ((s.row0 + col) >> a.g_shift)) & 1ull) == 0ull) continue;
                         const uint32_t p = *reinterpret_cast<const uint16_t*>(smem + C::kP + p_at(at, col) + (col & 7) * 2);
-                        o[c] = fmaf(__uint_as_float(p << 16), v, o[c]);      // (not finite, whatever the rest of the weight is)
+                        o[c] = fmaf(__uint_as_float(p << 16), v, o[c]);
+                        if (fabsf(v) < INFINITY) {          // (a component beside the one that is not finite: both parts of its weight)
+                            const uint32_t lower = *reinterpret_cast<const uint16_t*>(smem + C::kP + p_at(at, N + col) + (col & 7) * 2);
+                            o[c] = fmaf(__uint_as_float(lower << 16), v, o[c]);
+                        }
                     }
                 }
                 int64_t to[16];                            // (read before the first store, which they could depend on)

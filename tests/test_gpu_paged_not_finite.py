@@ -93,3 +93,32 @@ def test_values_of_selected_pages(T, Hq, Hkv, d, k):
     *ref, want = R.sparse_attn(Q, Kn, Vn, c, bounds, k, 1, 2)
     assert torch.equal(sel.cpu(), want)
     agrees(O, LSE, ref)
+
+
+def close(O, LSE, ref, rows, rounded=False):
+    """Within what the weights' roundings and fp32 sums leave, for queries of a quarter (so that the products of a logit add up to less than
+    3 in magnitude after scaling): 2^-16 of A = softmax of |V| up to 64 rows per KV head, R.U of A with more.  fp32: a logit is a sum of up
+    to 128 products, off by less than 128 * 2^-23 * 3 = 4.6e-5, and so are two of them in a weight; the sums over up to 128 rows by
+    as little; 2e-4 of A covers them."""
+    Oref, Lref, A = ref[:3]
+    bound = (2.0 ** -16 if rows <= 64 else R.U) * A + 2e-4 * A + 1e-6 + (R.U * Oref.abs() if rounded else 0)
+    err = (O.double().cpu() - Oref).abs()
+    assert bool((err <= bound).all()), f"{float((err / bound).max()):.2f} of the bound"
+    assert float((LSE.double().cpu() - Lref).abs().max()) <= 2e-4
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", [f for f in FORMS if f[0] > 1])
+def test_finite_components_beside_one_that_is_not(T, Hq, Hkv, d):
+    """A node's value with an infinity in one component: the others count with their full weight, to float32 outputs.  Up to 64 rows
+    per KV head a weight is two bf16 numbers, within 2^-16 of itself; with more rows it is one, within R.U."""
+    c = R.Cache([6, 20], 16, Hkv, d, room=T)
+    Q, Kn, Vn, parent = drafts(2, T, Hq, Hkv, d, seed=T, scale=0.25)
+    Vn[0, 1, :, 3], Vn[1, 0, :, d - 1], Vn[1, T // 2, 0, 7] = INF, -INF, NAN
+    out = torch.empty(2, T, Hq, d, device=DEV)
+    O, LSE = binding.pulsar_tree_attn(*(x.to(DEV) for x in (Q, Kn, Vn, c.K, c.V, c.table, c.lens, parent)), out=out)
+    Oref, Lref, A = R.tree_attn(Q, Kn, Vn, c, parent)
+    fine = Oref.isfinite()
+    o = O.double().cpu()
+    assert torch.equal(o.isfinite(), fine) and not bool(fine.all())
+    zero = torch.zeros_like(Oref)
+    close(torch.where(fine, o, zero), LSE, (torch.where(fine, Oref, zero), Lref, torch.where(fine, A, zero)), T * Hq // Hkv)

@@ -551,8 +551,9 @@ int32_t pulsar_rope_apply_qk(const uint16_t *Q, uint16_t *Q_out, int32_t Hq,
  *                     PULSAR_DEV_BAD_LENGTH and are clamped.
  * Rows from cache_len on are never read (they may hold anything, NaN included).  A page id outside [0, n_pages) where a row lies
  * sets PULSAR_DEV_BAD_PAGE: the row counts as absent, and what would be written there is dropped.  Several slots may hold the
- * same page; then they agree on its rows, and a page that is still written to is held by one slot.  K_pages, V_pages and the outputs
- * overlap neither each other nor an input (else PULSAR_ERR_INVALID_ARG).
+ * same page; then they agree on its rows, and a page that is still written to is held by one slot.  K_pages, V_pages, the outputs,
+ * device_status and the workspace overlap neither each other nor an input, tables, lengths and lists among these (else
+ * PULSAR_ERR_INVALID_ARG).
  *
  * Requirements of all the calls (else PULSAR_ERR_SHAPE): page_size in {16, 32, 64, 128}; d in {64, 128}; 1 <= n_slots <= 1024;
  * max_pages * page_size <= 2^30; n_slots * max_pages < 2^31; 1 <= n_pages < 2^24; n_layers >= 1; Hkv <= 1024.  pulsar_pages_summarize
@@ -569,13 +570,12 @@ int32_t pulsar_rope_apply_qk(const uint16_t *Q, uint16_t *Q_out, int32_t Hq,
  * A page is free if and only if no slot of the result holds it from its parent: pages of slots that nobody continues are free
  * within the same call.  Free pages are handed out in ascending order to the slots in ascending order.  Where none is left, or
  * max_pages is too small, PULSAR_DEV_NO_PAGES is set and the entry is -1 (or missing).
- *   page_table, cache_len and parent must not overlap the outputs (else PULSAR_ERR_INVALID_ARG).  1 <= n_new <= 1024,
- *   reserve_rows >= 0.
+ *   1 <= n_new <= 1024, reserve_rows >= 0.
  *
  * pulsar_pages_compact  after a drafted tree was verified: the accepted nodes move up behind the sequence, in every layer
  *   accept      in  [n_slots, T] int32 device, 1 <= T <= 64: the accepted nodes of the slot's tree in ascending order, then -1.  Row
  *               cache_len + accept[j] moves to row cache_len + j.
- *   new_len     out [n_slots]: cache_len + accepted nodes (may not overlap cache_len)
+ *   new_len     out [n_slots]: cache_len + accepted nodes
  *
  * pulsar_pages_append   rows from packed tensors into one layer's pages: row u of slot s goes to row cache_len + u
  *   Knew, Vnew  in  [n_slots, T, Hkv, d] bf16, K_pages, V_pages [n_pages, page_size, Hkv, d] (one layer)

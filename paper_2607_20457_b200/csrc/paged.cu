@@ -557,10 +557,11 @@ extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, con
     if (Q == nullptr || Knew == nullptr || Vnew == nullptr || K_pages == nullptr || V_pages == nullptr || page_table == nullptr ||
         cache_len == nullptr || O == nullptr || workspace == nullptr)
         return PULSAR_ERR_INVALID_ARG;
-    const size_t rows = static_cast<size_t>(n_slots) * T, pool = pool_bytes(1, n_pages, page_size, Hkv, d);
-    if (!apart({{O, rows * Hq * d * (out_is_f32 ? 4 : 2)}, {K_pages, pool}, {V_pages, pool}, {LSE, rows * Hq * 4}},
-               {{Q, rows * Hq * d * 2}, {Knew, rows * Hkv * d * 2}, {Vnew, rows * Hkv * d * 2}}))
-        return PULSAR_ERR_INVALID_ARG;
+    const size_t slots = static_cast<size_t>(n_slots), rows = slots * T, pool = pool_bytes(1, n_pages, page_size, Hkv, d);
+    const Tensors in = {{Q, rows * Hq * d * 2}, {Knew, rows * Hkv * d * 2}, {Vnew, rows * Hkv * d * 2}, {page_table, 4 * slots * max_pages},
+                        {cache_len, 4 * slots}, {parent, 4 * rows}, {n_draft, 4 * slots}};
+    const Tensors out = {{O, rows * Hq * d * (out_is_f32 ? 4 : 2)}, {K_pages, pool}, {V_pages, pool}, {LSE, rows * Hq * 4}, {device_status, 4u}};
+    if (!apart(out, in)) return PULSAR_ERR_INVALID_ARG;
     for (const void* p : {static_cast<const void*>(Q), static_cast<const void*>(Knew), static_cast<const void*>(Vnew),
                           static_cast<const void*>(K_pages), static_cast<const void*>(V_pages), static_cast<const void*>(O)})
         if (!aligned(p, 16)) return PULSAR_ERR_ALIGNMENT;
@@ -568,7 +569,9 @@ extern "C" int32_t pulsar_tree_attn(const uint16_t* Q, const uint16_t* Knew, con
         !aligned(workspace, 256))
         return PULSAR_ERR_ALIGNMENT;
     if (!pieces_ok(n_slots, Hkv, static_cast<int64_t>(max_pages) * page_size)) return PULSAR_ERR_SHAPE;
-    if (workspace_bytes < pulsar_tree_attn_workspace_bytes(n_slots, T, Hq, Hkv, d)) return PULSAR_ERR_WORKSPACE;
+    const size_t scratch = pulsar_tree_attn_workspace_bytes(n_slots, T, Hq, Hkv, d);
+    if (workspace_bytes < scratch) return PULSAR_ERR_WORKSPACE;
+    if (!apart({{workspace, scratch}}, in) || !apart({{workspace, scratch}}, out)) return PULSAR_ERR_INVALID_ARG;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
     PagedArgs a{};
     a.Q = Q;
@@ -633,10 +636,12 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
     if (Q == nullptr || Knew == nullptr || Vnew == nullptr || K_pages == nullptr || V_pages == nullptr || summary == nullptr ||
         page_table == nullptr || cache_len == nullptr || O == nullptr || sel == nullptr || workspace == nullptr)
         return PULSAR_ERR_INVALID_ARG;
-    const size_t tokens = static_cast<size_t>(n_slots) * T, pool = pool_bytes(1, n_pages, page_size, Hkv, d);
-    if (!apart({{O, tokens * Hq * d * 2}, {K_pages, pool}, {V_pages, pool}, {LSE, tokens * Hq * 4}, {sel, tokens * Hkv * k * 4}},
-               {{Q, tokens * Hq * d * 2}, {Knew, tokens * Hkv * d * 2}, {Vnew, tokens * Hkv * d * 2}, {summary, pool / page_size * 2}}))
-        return PULSAR_ERR_INVALID_ARG;
+    const size_t slots = static_cast<size_t>(n_slots), tokens = slots * T, pool = pool_bytes(1, n_pages, page_size, Hkv, d);
+    const Tensors in = {{Q, tokens * Hq * d * 2}, {Knew, tokens * Hkv * d * 2}, {Vnew, tokens * Hkv * d * 2}, {summary, pool / page_size * 2},
+                        {page_table, 4 * slots * max_pages}, {cache_len, 4 * slots}, {n_draft, 4 * slots}};
+    const Tensors out = {{O, tokens * Hq * d * 2}, {K_pages, pool}, {V_pages, pool}, {LSE, tokens * Hq * 4}, {sel, tokens * Hkv * k * 4},
+                         {device_status, 4u}};
+    if (!apart(out, in)) return PULSAR_ERR_INVALID_ARG;
     for (const void* p : {static_cast<const void*>(Q), static_cast<const void*>(Knew), static_cast<const void*>(Vnew), static_cast<const void*>(summary),
                           static_cast<const void*>(K_pages), static_cast<const void*>(V_pages), static_cast<const void*>(O)})
         if (!aligned(p, 16)) return PULSAR_ERR_ALIGNMENT;
@@ -645,6 +650,7 @@ extern "C" int32_t pulsar_sparse_attn(const uint16_t* Q, const uint16_t* Knew, c
     const int64_t rows = static_cast<int64_t>(n_slots) * T * Hkv;
     const SparseScratch y(n_slots, T, Hkv, max_pages, k, Hq / Hkv, d);
     if (workspace_bytes < y.total) return PULSAR_ERR_WORKSPACE;
+    if (!apart({{workspace, y.total}}, in) || !apart({{workspace, y.total}}, out)) return PULSAR_ERR_INVALID_ARG;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
     auto* ws = static_cast<uint8_t*>(workspace);
     auto st = static_cast<cudaStream_t>(stream);

@@ -27,12 +27,13 @@ inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     return a != nullptr && b != nullptr && x < y + nb && y < x + na;
 }
 
-// Whether none of the outputs shares memory with another one or with an input.
 struct Bytes {
     const void* p;
     size_t n;
 };
-inline bool apart(std::initializer_list<Bytes> outputs, std::initializer_list<Bytes> inputs) {
+using Tensors = std::initializer_list<Bytes>;
+// Whether none of the outputs shares memory with another one or with an input.
+inline bool apart(Tensors outputs, Tensors inputs) {
     for (const Bytes* o = outputs.begin(); o != outputs.end(); ++o) {
         for (const Bytes* x = o + 1; x != outputs.end(); ++x)
             if (overlap(o->p, o->n, x->p, x->n)) return false;

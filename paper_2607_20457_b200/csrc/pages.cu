@@ -526,17 +526,15 @@ extern "C" int32_t pulsar_pages_fork(const int32_t* page_table, const int32_t* c
         new_len == nullptr || n_free == nullptr || workspace == nullptr || (parent == nullptr && n_new != n_slots))
         return PULSAR_ERR_INVALID_ARG;
     const size_t table_bytes = 4 * static_cast<size_t>(max_pages);
-    const struct { const void* p; size_t n; } in[] = {{page_table, n_slots * table_bytes}, {cache_len, 4u * n_slots}, {parent, 4u * n_new}},
-                                              out[] = {{new_table, n_new * table_bytes}, {new_len, 4u * n_new}, {n_free, 4u}};
-    for (const auto& i : in)
-        for (const auto& o : out)
-            if (overlap(i.p, i.n, o.p, o.n)) return PULSAR_ERR_INVALID_ARG;
-    const size_t pool = pool_bytes(n_layers, n_pages, page_size, Hkv, d);
-    if (!apart({{K_pages, pool}, {V_pages, pool}}, {})) return PULSAR_ERR_INVALID_ARG;
+    const size_t pool = pool_bytes(n_layers, n_pages, page_size, Hkv, d), scratch = ForkScratch::bytes(n_new, n_pages);
+    const Tensors in = {{page_table, n_slots * table_bytes}, {cache_len, 4u * n_slots}, {parent, 4u * n_new}};
+    const Tensors out = {{new_table, n_new * table_bytes}, {new_len, 4u * n_new}, {n_free, 4u}, {K_pages, pool}, {V_pages, pool}, {device_status, 4u}};
+    if (!apart(out, in)) return PULSAR_ERR_INVALID_ARG;
     if (!aligned(K_pages, 16) || !aligned(V_pages, 16) || !aligned(workspace, 256) || !aligned(page_table, 4) || !aligned(cache_len, 4) ||
         !aligned(parent, 4) || !aligned(new_table, 4) || !aligned(new_len, 4) || !aligned(n_free, 4))
         return PULSAR_ERR_ALIGNMENT;
-    if (workspace_bytes < ForkScratch::bytes(n_new, n_pages)) return PULSAR_ERR_WORKSPACE;
+    if (workspace_bytes < scratch) return PULSAR_ERR_WORKSPACE;
+    if (!apart({{workspace, scratch}}, in) || !apart({{workspace, scratch}}, out)) return PULSAR_ERR_INVALID_ARG;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;
 
     ForkArgs a{};
@@ -592,11 +590,12 @@ extern "C" int32_t pulsar_pages_compact(uint16_t* K_pages, uint16_t* V_pages, in
                                         int32_t max_pages, const int32_t* accept, int32_t T, int32_t* new_len, int32_t* device_status,
                                         void* stream) {
     if (!pool_ok(n_layers, n_pages, page_size, Hkv, d, n_slots, max_pages) || T < 1 || T > kMaxTree) return PULSAR_ERR_SHAPE;
-    if (K_pages == nullptr || V_pages == nullptr || page_table == nullptr || cache_len == nullptr || accept == nullptr || new_len == nullptr ||
-        overlap(cache_len, 4u * n_slots, new_len, 4u * n_slots))
+    if (K_pages == nullptr || V_pages == nullptr || page_table == nullptr || cache_len == nullptr || accept == nullptr || new_len == nullptr)
         return PULSAR_ERR_INVALID_ARG;
-    const size_t pool = pool_bytes(n_layers, n_pages, page_size, Hkv, d);
-    if (!apart({{K_pages, pool}, {V_pages, pool}}, {})) return PULSAR_ERR_INVALID_ARG;
+    const size_t pool = pool_bytes(n_layers, n_pages, page_size, Hkv, d), slots = static_cast<size_t>(n_slots);
+    if (!apart({{K_pages, pool}, {V_pages, pool}, {new_len, 4 * slots}, {device_status, 4u}},
+               {{page_table, 4 * slots * max_pages}, {cache_len, 4 * slots}, {accept, 4 * slots * T}}))
+        return PULSAR_ERR_INVALID_ARG;
     if (!aligned(K_pages, 16) || !aligned(V_pages, 16) || !aligned(page_table, 4) || !aligned(cache_len, 4) || !aligned(accept, 4) ||
         !aligned(new_len, 4))
         return PULSAR_ERR_ALIGNMENT;
@@ -619,8 +618,10 @@ extern "C" int32_t pulsar_pages_append(const uint16_t* Knew, const uint16_t* Vne
     if (K_pages == nullptr || V_pages == nullptr || page_table == nullptr || cache_len == nullptr ||
         (T > 0 && (Knew == nullptr || Vnew == nullptr)))
         return PULSAR_ERR_INVALID_ARG;
-    const size_t fresh = static_cast<size_t>(n_slots) * T * Hkv * d * 2, pool = pool_bytes(1, n_pages, page_size, Hkv, d);
-    if (!apart({{K_pages, pool}, {V_pages, pool}}, {{Knew, fresh}, {Vnew, fresh}})) return PULSAR_ERR_INVALID_ARG;
+    const size_t slots = static_cast<size_t>(n_slots), fresh = slots * T * Hkv * d * 2, pool = pool_bytes(1, n_pages, page_size, Hkv, d);
+    if (!apart({{K_pages, pool}, {V_pages, pool}, {device_status, 4u}},
+               {{Knew, fresh}, {Vnew, fresh}, {n_new, 4 * slots}, {page_table, 4 * slots * max_pages}, {cache_len, 4 * slots}}))
+        return PULSAR_ERR_INVALID_ARG;
     if (!aligned(K_pages, 16) || !aligned(V_pages, 16) || !aligned(Knew, 16) || !aligned(Vnew, 16) || !aligned(page_table, 4) ||
         !aligned(cache_len, 4) || !aligned(n_new, 4))
         return PULSAR_ERR_ALIGNMENT;
@@ -643,8 +644,10 @@ extern "C" int32_t pulsar_pages_summarize(const uint16_t* K_pages, int32_t n_lay
         static_cast<int64_t>(max_pages) * ((Hkv * d / 8 + 31) / 32) >= (int64_t{1} << 31))
         return PULSAR_ERR_SHAPE;
     if (K_pages == nullptr || page_table == nullptr || row_end == nullptr || summary == nullptr) return PULSAR_ERR_INVALID_ARG;
-    const size_t pool = pool_bytes(n_layers, n_pages, page_size, Hkv, d);
-    if (!apart({{summary, pool / page_size * 2}}, {{K_pages, pool}})) return PULSAR_ERR_INVALID_ARG;
+    const size_t pool = pool_bytes(n_layers, n_pages, page_size, Hkv, d), slots = static_cast<size_t>(n_slots);
+    if (!apart({{summary, pool / page_size * 2}, {device_status, 4u}},
+               {{K_pages, pool}, {page_table, 4 * slots * max_pages}, {row_begin, 4 * slots}, {row_end, 4 * slots}}))
+        return PULSAR_ERR_INVALID_ARG;
     if (!aligned(K_pages, 16) || !aligned(summary, 16) || !aligned(page_table, 4) || !aligned(row_begin, 4) || !aligned(row_end, 4))
         return PULSAR_ERR_ALIGNMENT;
     if (const int32_t rc = check_device(); rc != PULSAR_OK) return rc;

@@ -140,3 +140,53 @@ def test_tensors_that_share_memory(lib, name, pairs):
             if one in ("len",) and change is not good[other]:
                 continue
             assert refused(fn, good, **{one: change}) == INVALID, (one, other)
+
+
+# Every tensor of a call with what it takes up: (bytes, whether the call writes it).
+POOL, TABLE, SLOTS = 64 * 16 * 2 * 64 * 2, 4 * 8 * 4, 4 * 4
+FRESH, QUERY, SUMMARY = 16 * 2 * 64 * 2, 16 * 8 * 64 * 2, 64 * 2 * 2 * 64 * 2
+ALL = {
+    "pulsar_pages_fork": dict(K=(2 * POOL, 1), V=(2 * POOL, 1), new_table=(TABLE, 1), new_len=(SLOTS, 1), n_free=(4, 1), status=(4, 1),
+                              table=(TABLE, 0), len=(SLOTS, 0), parent=(SLOTS, 0)),
+    "pulsar_pages_compact": dict(K=(2 * POOL, 1), V=(2 * POOL, 1), new_len=(SLOTS, 1), status=(4, 1), table=(TABLE, 0), len=(SLOTS, 0),
+                                 accept=(64, 0)),
+    "pulsar_pages_append": dict(K=(POOL, 1), V=(POOL, 1), status=(4, 1), Kn=(FRESH, 0), Vn=(FRESH, 0), n_new=(SLOTS, 0), table=(TABLE, 0),
+                                len=(SLOTS, 0)),
+    "pulsar_pages_summarize": dict(summary=(SUMMARY, 1), status=(4, 1), K=(POOL, 0), table=(TABLE, 0), begin=(SLOTS, 0), end=(SLOTS, 0)),
+    "pulsar_tree_attn": dict(O=(QUERY, 1), K=(POOL, 1), V=(POOL, 1), LSE=(512, 1), status=(4, 1), Q=(QUERY, 0), Kn=(FRESH, 0), Vn=(FRESH, 0),
+                             table=(TABLE, 0), len=(SLOTS, 0), parent=(64, 0), n_draft=(SLOTS, 0)),
+    "pulsar_sparse_attn": dict(O=(QUERY, 1), K=(POOL, 1), V=(POOL, 1), LSE=(512, 1), sel=(512, 1), status=(4, 1), Q=(QUERY, 0), Kn=(FRESH, 0),
+                               Vn=(FRESH, 0), summary=(SUMMARY, 0), table=(TABLE, 0), len=(SLOTS, 0), n_draft=(SLOTS, 0)),
+}
+
+
+@pytest.mark.parametrize("name", ALL)
+def test_nothing_that_is_written_shares_memory_with_anything(lib, name):
+    """Whatever a call writes, beside every other tensor of it: at the same place, at its last word, and with its own last word at the
+    other's first; and one word further off, where it is the workspace or the alignment that is refused."""
+    fn, tensors = getattr(lib, name), ALL[name]
+    good = dict(CALLS[name])
+    for i, key in enumerate(tensors):
+        good[key] = at(20 + 2 * i)
+    if "ws" in good:
+        good["ws"], good["ws_bytes"] = at(200), 1 << 30
+    place = lambda base, by: ctypes.c_void_p(good[base].value + by)
+    # (an odd address or a workspace of no bytes ends a call behind these checks)
+    last = dict(ws_bytes=0) if "ws" in good else dict(len=place("len", 2)) if "len" in good else dict(end=place("end", 2))
+    assert refused(fn, good, **last) == (WORKSPACE if "ws" in good else ALIGNMENT)
+    for one, (size, written) in tensors.items():
+        if not written:
+            continue
+        for other, (other_size, _) in tensors.items():
+            if other == one:
+                continue
+            for by in {0, other_size - 4, 4 - size}:
+                assert refused(fn, good, **{one: place(other, by)}) == INVALID, (one, other, by)
+            for by in (other_size, -size):
+                if other not in last and one not in last:
+                    assert refused(fn, good, **{one: place(other, by)}, **last) in (WORKSPACE, ALIGNMENT), (one, other, by)
+    if "ws" in good:
+        for other, (size, _) in tensors.items():
+            assert refused(fn, good, ws=ctypes.c_void_p(good[other].value // 256 * 256)) == INVALID, other
+            good_ws = dict(good, ws=at(19), ws_bytes=1 << 30)
+            assert refused(fn, good_ws, **{other: ctypes.c_void_p(at(19).value + 256)}) == INVALID, other

@@ -122,3 +122,36 @@ def test_finite_components_beside_one_that_is_not(T, Hq, Hkv, d):
     assert torch.equal(o.isfinite(), fine) and not bool(fine.all())
     zero = torch.zeros_like(Oref)
     close(torch.where(fine, o, zero), LSE, (torch.where(fine, Oref, zero), Lref, torch.where(fine, A, zero)), T * Hq // Hkv)
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", [f for f in FORMS if f[0] > 1])
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+def test_keys_of_new_tokens(T, Hq, Hkv, d, value):
+    """A node's key that is not finite reaches the nodes that see it, by outputs and LSE, and nobody else.  (A logit of +infinity makes the
+    softmax NaN; one of -infinity is a weight of 0.)"""
+    c = R.Cache([50, 129], 16, Hkv, d, room=T)
+    Q, Kn, Vn, parent = drafts(2, T, Hq, Hkv, d, seed=T)
+    Kn[0, 1, :, 3], Kn[1, T // 2, 0, d - 1] = value, value
+    O, LSE = tree(c, Q, Kn, Vn, parent)
+    Oref, Lref, A = R.tree_attn(Q, Kn, Vn, c, parent)
+    o, l = O.double().cpu(), LSE.double().cpu()
+    fine = Oref.isfinite()
+    assert not bool(fine.all()) or value == -INF
+    assert torch.equal(o.isfinite(), fine) and bool(o[~fine].isnan().all())
+    row = fine.all(-1)
+    assert torch.equal(fine.any(-1), row) and not bool(l[~row].isfinite().any())
+    R.check(o[row], l[row], (Oref[row], Lref[row], A[row]))
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", FORMS)
+def test_cached_keys(T, Hq, Hkv, d):
+    """A NaN in a cached key is everybody's NaN for that KV head alone."""
+    c = R.Cache([300, 40], 16, Hkv, d, room=T)
+    Q, Kn, Vn, parent = drafts(2, T, Hq, Hkv, d, seed=T)
+    plant(c, 0, 7, 3, NAN, c.K, head=Hkv - 1)
+    O, LSE = tree(c, Q, Kn, Vn, parent)
+    g = Hq // Hkv
+    assert bool(O[0, :, -g:].isnan().all()) and bool(LSE[0, :, -g:].isnan().all())
+    clean = torch.ones(2, T, Hq, dtype=torch.bool)
+    clean[0, :, -g:] = False
+    R.check(O.cpu()[clean], LSE.cpu()[clean], [x[clean] for x in R.tree_attn(Q, Kn, Vn, c, parent)])

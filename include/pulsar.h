@@ -549,7 +549,7 @@ int32_t pulsar_rope_apply_qk(const uint16_t *Q, uint16_t *Q_out, int32_t Hq,
  *                     r % page_size of it.  Retained context KV [L, Hkv, d] is a run of L / page_size pages as it stands.
  *   cache_len         [n_slots] int32 device: rows that slot s holds.  Values outside [0, max_pages*page_size] set
  *                     PULSAR_DEV_BAD_LENGTH and are clamped.
- * Rows from cache_len on are never read (they may hold anything, NaN included).  A page id outside [0, n_pages) where a row lies
+ * Rows from cache_len on count for nothing (they may hold anything, NaN included).  A page id outside [0, n_pages) where a row lies
  * sets PULSAR_DEV_BAD_PAGE: the row counts as absent, and what would be written there is dropped.  Several slots may hold the
  * same page; then they agree on its rows, and a page that is still written to is held by one slot.  K_pages, V_pages, the outputs,
  * device_status and the workspace overlap neither each other nor an input, tables, lengths and lists among these (else
@@ -630,8 +630,9 @@ int32_t pulsar_pages_summarize(const uint16_t *K_pages, int32_t n_layers, int32_
  *   LSE         out [n_slots, T, Hq] float32 or NULL
  *   Nodes whose row lies past the table's last page set PULSAR_DEV_BAD_LENGTH; they are attended to, but not written.  A row
  *   without a visible key cannot occur (a node sees itself).
- *   Values that are not finite, cached or new, come out as the formula says for the nodes that see them, with weights in fp32 (one that
- *   is 0 there, 2^-149 of the largest or less, times infinity is NaN), and reach nobody else.
+ *   Values that are not finite, cached or new, come out as the formula says for the nodes that see them (a weight below 2^-126 of the
+ *   largest may count as 0, and 0 times infinity is NaN), and reach nobody else.  Logits are fp32: they and LSE are off by 2^-24 of their
+ *   magnitude at the least, and magnitudes from 2^30 on are not covered.
  *
  * Requirements (else PULSAR_ERR_SHAPE): those of the paged cache, 1 <= T <= 64, Hq % Hkv == 0, Hq/Hkv in {1,2,4,8,16},
  * n_slots * Hkv * (max_pages * page_size / 128 + 2) < 2^31.
@@ -663,6 +664,8 @@ int32_t pulsar_tree_attn(const uint16_t *Q, const uint16_t *Knew, const uint16_t
  *
  * Requirements (else PULSAR_ERR_SHAPE): those of pulsar_tree_attn, 1 <= k, 0 <= sink, 0 <= window, sink + window <= k <= 65536,
  * n_slots * T * Hkv <= 2^20, n_slots * T * Hkv * ((k + 1) * page_size / 128 + 2) < 2^31 (in place of the last one).
+ * The workspace holds 12 bytes per slot, token, KV head and entry of the table, whatever the lengths are: 200 MB for 64 slots of 4
+ * tokens and 8 heads whose tables have 8192 entries.
  * ------------------------------------------------------------------------------------------ */
 size_t pulsar_sparse_attn_workspace_bytes(int32_t n_slots, int32_t T, int32_t max_pages, int32_t k, int32_t Hq, int32_t Hkv,
                                           int32_t d);

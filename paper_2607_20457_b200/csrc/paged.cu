@@ -23,8 +23,8 @@ namespace {
 // same: a page whose fp32 score lies further from the k-th than both can be off is in or out, and the few others are formed again in
 // float64.  With the selection's launch the attention's starts, and waits for the list alone.
 //
-// Measured with the attention: one slot of 6001 rows, 32 pages of 16 18 us; of 131,072, 64 pages of 32 27; 16 slots of up to 45,011
-// with 4 tokens, 48 pages of 16 49 us (cold and one by one the scores take 14, the ranking 14, the attention 25, the joining 5).
+// Measured with the attention: one slot of 6001 rows, 32 pages of 16 19 us; of 131,072, 64 pages of 32 27; 16 slots of up to 45,011
+// with 4 tokens, 48 pages of 16 50 us (cold and one by one the scores take 17, the ranking 14, the attention 27, the joining 7).
 // A slot's ranking is a chain of steps over the block (largest and smallest, bins, border, places), each a microsecond.
 // ---------------------------------------------------------------------------------------------
 constexpr int kScoreThreads = 128, kScorePages = 64;     // of a CTA: 16 pages per warp

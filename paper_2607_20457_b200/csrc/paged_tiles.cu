@@ -22,7 +22,7 @@
 // rows 33.6 -> 35.3, long caches the same; to look at the upper part first costs the small trees 0.3 us).
 //
 // What bounds it (measured in a pass of many, with the joining launch): long caches the memory -- 32 slots of up to 8192 rows of 8
-// heads, one token each, 96 to 100 us, 5.7 TB/s; short ones latency -- one slot of 6001 rows 13 us, of which the first tile's way (length,
+// heads, one token each, 97 to 102 us, 5.4 to 5.7 TB/s; short ones latency -- one slot of 6001 rows 13 us, of which the first tile's way (length,
 // page ids, TMA) takes 3.5, an item's end 1.5 and the joining launch 3; a tile of 64 rows itself about 1100 cycles.
 #include <algorithm>
 

@@ -19,9 +19,10 @@
 //
 // P is handed to the issuer in two pieces (96 and 32 keys), so that the first piece of PV runs beside the rest.
 //
-// What bounds it: up to 128 rows, 4 slots of up to 32,768 rows with 24 nodes (96 rows) 95 to 99 us, 0.7 of HBM's floor; more, one slot of
-// 131,072 rows with 64 nodes (256 rows) 162 to 169 us, 0.5 of the tensor cores' burst rate: the chain S -> softmax -> PV -> S of a stream, of
-// which the other stream hides a part (its products take 2048 cycles of a tile of about 3200).
+// What bounds it: up to 128 rows, 4 slots of up to 32,768 rows with 24 nodes (96 rows) 94 to 101 us, 0.7 of HBM's rate; more, one slot of
+// 131,072 rows with 64 nodes (256 rows) 159 to 171 us, 0.5 of the tensor cores' burst rate: the chain S -> softmax -> PV -> S of a stream, of
+// which the other stream hides a part (its products take 2048 cycles of a tile of about 3200).  The twelve warps have 168 registers each,
+// and a row of 128 logits is most of them: up to 128 rows 72 bytes are spilled and 60 read back per thread, with more rows 28 and 12.
 #include "mma.cuh"
 #include "paged_roles.cuh"
 
